@@ -355,6 +355,97 @@ enum { SPLC_OP_PROJECT = 0, SPLC_OP_RECONSTRUCT = 1, SPLC_OP_REPROJECT_PASS1 = 2
 int sparseloco_subspace_kernel_choice(int op, int64_t rows, int d, int k, int tables, int matmul);
 
 /*
+ * The inner step (section 2.1, first line: theta_local <- InnerOpt(theta_outer; data), H steps of AdamW with clipped
+ * gradients between two outer steps): what a replica does around its model's forward and backward pass.  The entry points
+ * follow the conventions above and walk a plan's tensors whatever its layout and kappa.
+ *
+ * sparseloco_plan_num_flat_chunks: runs of SPLC_CHUNK consecutive elements of the tensors, sum over tensors of
+ * ceil(numel / SPLC_CHUNK) (a flat plan's chunks), numbered tensor by tensor.
+ */
+int64_t sparseloco_plan_num_flat_chunks(const sparseloco_plan* plan);
+
+/*
+ * The 2-norm of all gradients and the factor that clips it:
+ *     norm = sqrt(sum_i g_i^2),   factor = norm > max_norm ? max_norm / norm : 1;   NaN where norm is not finite.
+ *   grads: fp32 or bf16 binding; replica: which set.  max_norm > 0 (infinity: no clipping).
+ *   norm_out: two floats of device memory, {norm, factor}; the address of the second is what grad_scale below takes.
+ *   ws: SPLC_NORM_WS_BYTES of device memory, 8-byte aligned, need not be cleared.
+ * Squares are formed and added in fp64 in an order that depends on the plan alone.
+ */
+#define SPLC_NORM_WS_BYTES 16384
+int sparseloco_grad_norm(const sparseloco_plan* plan, const sparseloco_tensors* grads, int replica, float max_norm,
+                         float* norm_out, void* ws, void* stream);
+
+/*
+ * One AdamW step (decoupled weight decay) over every tensor of the plan, one launch, in place:
+ *     g     = grad_scale * grad
+ *     m     = beta1 m + (1 - beta1) g
+ *     v     = beta2 v + (1 - beta2) g^2
+ *     theta = theta (1 - lr weight_decay decay[tensor]) - lr m^ / (sqrt(v^) + eps),
+ *             m^ = m / (1 - beta1^step), v^ = v / (1 - beta2^step).
+ * The new term of a moment is multiplied and added in one rounding (fused); every other operation has its own.
+ *   theta, m, v: fp32 bindings; grads: fp32 or bf16.  replica: which set of each binding (one set serves every replica).
+ *   how: read during the call.  lr, eps, weight_decay >= 0, 0 <= beta < 1, step >= 1 (the first step is 1).
+ *   grad_scale: one float of device memory or NULL (1), read when the kernel runs.  If it is not finite the step leaves
+ *   everything as it is: a batch whose gradients overflowed is skipped without the host having to look.
+ *   decay: n_tensors floats of device memory or NULL (all 1): how much of the weight decay each tensor takes.
+ *   theta_bf16: NULL, or a bf16 binding that receives the new theta rounded to nearest even.
+ * A call recorded into a graph keeps its numbers.  Gradients must be finite where grad_scale is.
+ */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+} sparseloco_adamw;
+int sparseloco_adamw_step(const sparseloco_plan* plan, const sparseloco_tensors* theta, const sparseloco_tensors* grads,
+                          const sparseloco_tensors* m, const sparseloco_tensors* v, int replica, const sparseloco_adamw* how,
+                          const float* grad_scale, const float* decay, const sparseloco_tensors* theta_bf16, void* stream);
+
+/*
+ * The same step with both moments held in 8 bits.  Element i of flat chunk c (sparseloco_plan_num_flat_chunks of them) has
+ * m[4096 c + i] and v[4096 c + i], e4m3 numbers (1 sign, 4 exponent and 3 mantissa bits, largest 448, no infinities), and a
+ * block of 256 elements shares m_scale[16 c + i / 256] and v_scale[16 c + i / 256]:
+ *     m = m_scale * m[.],   sqrt(v) = v_scale * v[.].
+ * All zeros is the state before the first step.  The step works on these in fp32 and holds the new moments with
+ * scale = largest magnitude of the block / 448.  A value between two e4m3 numbers is rounded up where the fraction of
+ * the gap that it covers, plus t, reaches 1; t runs through [0, 1) with the element and the step, t = frac(p a1 + step a2)
+ * with p the element's place, a1 = 0.7548776..., a2 = 0.5698402... (1/q and 1/q^2 of q^3 = q + 1) for m, 1/2 further for v:
+ * over the steps a moment follows its average also where it changes by less than a gap per step, which rounding to
+ * nearest would not let it.  A root above zero is held as 2^-9 at least.
+ *   m, v: 4-byte aligned; elements of the last chunk of a tensor that lie behind its end become zero.
+ */
+int sparseloco_adamw_step_8bit(const sparseloco_plan* plan, const sparseloco_tensors* theta, const sparseloco_tensors* grads,
+                               int replica, uint8_t* m, float* m_scale, uint8_t* v, float* v_scale,
+                               const sparseloco_adamw* how, const float* grad_scale, const float* decay,
+                               const sparseloco_tensors* theta_bf16, void* stream);
+
+/*
+ * Token embeddings of the split table of section 2.4 (and of a plain one):
+ *     out[r] = scale * (table[token_ids[r]] + t_perp[token_ids[r]]) + pos_embed[r % seq_len],     r = 0 .. rows - 1,
+ * every operation rounded once in fp32, the result once to out's type.
+ *   table, t_perp (may be NULL): [vocab, d]; pos_embed (may be NULL): [seq_len, d]; all of table_dtype (SPLC_F32 or
+ *   SPLC_BF16).  token_ids: int32, clamped into [0, vocab).  out: [rows, d] of out_dtype, fully overwritten, must not
+ *   overlap the inputs.  Row-major device arrays, aligned to their elements.  rows < 2^31, d < 2^24.
+ */
+int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table_dtype, const int32_t* token_ids, int vocab,
+                                const void* pos_embed, int seq_len, float scale, void* out, int out_dtype, int64_t rows, int d,
+                                void* stream);
+
+/*
+ * Its gradient with respect to the table:
+ *     grad_table[x] = scale * sum_{r: token_ids[r] = x} grad_out[r]     (+ grad_table[x] if accumulate is not 0)
+ * grad_out: [rows, d] of grad_dtype, grad_table: [vocab, d] of table_dtype; sums in fp32, rounded once to grad_table's type.
+ * Without accumulate every row is written (zero where no token has it), with it only the rows that tokens have.
+ *   token_ids: as above; those equal to ignore_id (a padding token; negative: none) are left out.
+ *   ws: sparseloco_embedding_grad_ws_bytes(rows, vocab, d) bytes of device memory, 8-byte aligned, need not be cleared; a
+ *   workspace for more rows serves fewer.  vocab <= 327680.
+ * The tokens of a row are added in an order that depends on token_ids alone: the same call gives the same bits.
+ */
+int64_t sparseloco_embedding_grad_ws_bytes(int64_t rows, int vocab, int d);
+int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_t* token_ids, int64_t rows, int vocab, int d,
+                              float scale, int32_t ignore_id, void* grad_table, int table_dtype, int accumulate, void* ws,
+                              int64_t ws_bytes, void* stream);
+
+/*
  * Measurement aid: what the chip streams for the access patterns of the kernels above, with their launch shape
  * (one 256-lane workgroup per 4096 floats, 16-byte non-temporal accesses).  The practical ceiling next to which
  * the achieved bandwidths are read; not part of the method.

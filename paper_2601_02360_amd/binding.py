@@ -27,6 +27,7 @@ SPLC_QUANT_NONE, SPLC_QUANT_2BIT = 0, 1
 SPLC_SELECT_AUTO, SPLC_SELECT_RADIX = 0, 1
 SPLC_LAYOUT_FLAT, SPLC_LAYOUT_TILE64 = 0, 1
 SPLC_MATMUL_FP32, SPLC_MATMUL_BF16X3 = 0, 1
+SPLC_NORM_WS_BYTES = 16384
 
 EXPORTS = [
     "sparseloco_plan_create", "sparseloco_plan_create_2d", "sparseloco_plan_destroy", "sparseloco_plan_num_chunks",
@@ -40,6 +41,8 @@ EXPORTS = [
     "sparseloco_outer_step_batch",
     "sparseloco_reproject_embedding", "sparseloco_reproject_embedding_noalloc", "sparseloco_subspace_project",
     "sparseloco_subspace_reconstruct", "sparseloco_subspace_kernel_choice", "sparseloco_strerror",
+    "sparseloco_plan_num_flat_chunks", "sparseloco_grad_norm", "sparseloco_adamw_step", "sparseloco_adamw_step_8bit",
+    "sparseloco_embedding_lookup", "sparseloco_embedding_grad_ws_bytes", "sparseloco_embedding_grad",
 ]
 
 SPLC_OP_PROJECT, SPLC_OP_RECONSTRUCT, SPLC_OP_REPROJECT_PASS1, SPLC_OP_REPROJECT_PASS2 = 0, 1, 2, 3
@@ -47,6 +50,12 @@ SPLC_MAX_REPLICAS = 1024
 SPLC_STREAM_READ, SPLC_STREAM_WRITE, SPLC_STREAM_COPY, SPLC_STREAM_R2W1, SPLC_STREAM_R3W1 = 0, 1, 2, 3, 4
 
 _lib = None
+
+
+class _AdamW(ctypes.Structure):
+    """sparseloco_adamw: the numbers of one step."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64)]
 
 
 class SparseLoCoError(RuntimeError):
@@ -98,6 +107,13 @@ def lib():
             "sparseloco_subspace_reconstruct": (i32, [vp, vp, vp, i32, vp, i32, vp, vp, i64, i32, i32, i32, vp]),
             "sparseloco_subspace_kernel_choice": (i32, [i32, i64, i32, i32, i32, i32]),
             "sparseloco_strerror": (ctypes.c_char_p, [i32]),
+            "sparseloco_plan_num_flat_chunks": (i64, [vp]),
+            "sparseloco_grad_norm": (i32, [vp, vp, i32, f32, vp, vp, vp]),
+            "sparseloco_adamw_step": (i32, [vp, vp, vp, vp, vp, i32, ctypes.POINTER(_AdamW), vp, vp, vp, vp]),
+            "sparseloco_adamw_step_8bit": (i32, [vp, vp, vp, i32, vp, vp, vp, vp, ctypes.POINTER(_AdamW), vp, vp, vp, vp]),
+            "sparseloco_embedding_lookup": (i32, [vp, vp, i32, vp, i32, vp, i32, f32, vp, i32, i64, i32, vp]),
+            "sparseloco_embedding_grad_ws_bytes": (i64, [i64, i32, i32]),
+            "sparseloco_embedding_grad": (i32, [vp, i32, vp, i64, i32, i32, f32, i32, vp, i32, i32, vp, i64, vp]),
         }
         assert sorted(sig) == sorted(EXPORTS)
         for name, (res, args) in sig.items():
@@ -368,6 +384,17 @@ class Plan:
         pairs = torch.empty(nch * self.kappa, dtype=torch.int16, device=device)
         aux = torch.empty(nch * 2 if self.quant else nch * self.kappa, dtype=torch.float32, device=device)
         return pairs, aux
+
+    @property
+    def num_flat_chunks(self) -> int:
+        return int(lib().sparseloco_plan_num_flat_chunks(self._h))
+
+    def adamw_8bit_buffers(self, device="cuda"):
+        """(m, m_scale, v, v_scale) of sparseloco_adamw_step_8bit before the first step."""
+        n = self.num_flat_chunks
+        codes = [torch.zeros(n * SPLC_CHUNK, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
+        scales = [torch.zeros(n * (SPLC_CHUNK // 256), dtype=torch.float32, device=device) for _ in range(2)]
+        return codes[0], scales[0], codes[1], scales[1]
 
     def bind(self, sets, dtype=torch.float32, stream=None) -> Tensors:
         """Bind one list of tensors, or a list of per-replica lists (sets)."""
@@ -640,3 +667,137 @@ def sparseloco_subspace_reconstruct(x_tilde: torch.Tensor, u: torch.Tensor, out:
                                                out.data_ptr(), int(rows), int(d), int(k), int(matmul), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_subspace_reconstruct")
+
+
+def _dtype_of(tensors):
+    """The element type of a binding or of a list of tensors (fp32 where there is none)."""
+    if isinstance(tensors, Tensors):
+        return tensors.dtype
+    first = tensors[0] if len(tensors) and isinstance(tensors[0], (list, tuple)) else tensors
+    return next((t.dtype for t in first if isinstance(t, torch.Tensor)), torch.float32)
+
+
+def _check_flat(specs):
+    """specs: (tensor, numel, dtype, name): of all first what they are, then where they live."""
+    for device in (False, True):
+        for t, numel, dtype, what in specs:
+            _check_tensor(t, numel, dtype, what, device)
+
+
+def grad_norm_workspace(device="cuda") -> torch.Tensor:
+    """The workspace of sparseloco_grad_norm."""
+    return torch.empty(SPLC_NORM_WS_BYTES, dtype=torch.uint8, device=device)
+
+
+def sparseloco_grad_norm(plan: Plan, grads, norm_out: torch.Tensor, ws: torch.Tensor, *, max_norm: float = 1.0,
+                         replica: int = 0, stream=None) -> None:
+    """norm_out[0] = 2-norm of all gradients, norm_out[1] = the factor that clips it to max_norm (NaN where the norm is not
+    finite).  grads: a Tensors binding or a list of tensors, fp32 or bf16; ws: grad_norm_workspace()."""
+    _check_flat([(norm_out, 2, torch.float32, "norm_out"), (ws, SPLC_NORM_WS_BYTES, torch.uint8, "ws")])
+    rc = lib().sparseloco_grad_norm(plan.handle, _h(plan._tensors(grads, _dtype_of(grads), stream)), int(replica),
+                                    float(max_norm), norm_out.data_ptr(), ws.data_ptr(), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_grad_norm")
+
+
+def _check_step(plan, grad_scale, decay):
+    specs = []
+    if grad_scale is not None:
+        specs.append((grad_scale, 1, torch.float32, "grad_scale"))
+    if decay is not None:
+        specs.append((decay, len(plan.numels), torch.float32, "decay"))
+    return specs
+
+
+def sparseloco_adamw_step(plan: Plan, theta, grads, m, v, *, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95,
+                          eps: float = 1e-8, weight_decay: float = 0.1, grad_scale: Optional[torch.Tensor] = None,
+                          decay: Optional[torch.Tensor] = None, theta_bf16=None, replica: int = 0, stream=None) -> None:
+    """One AdamW step over all tensors, theta, m and v (fp32) in place.  Bindings, or lists bound on the fly; grads fp32 or
+    bf16.  grad_scale: one fp32 element on the GPU, the factor on the gradients (norm_out[1:] of sparseloco_grad_norm); if it
+    is not finite nothing changes.  decay: per tensor a factor on weight_decay.  theta_bf16: receives a bf16 copy."""
+    _check_flat(_check_step(plan, grad_scale, decay))
+    how = _AdamW(lr, beta1, beta2, eps, weight_decay, step)
+    rc = lib().sparseloco_adamw_step(plan.handle, _h(plan._tensors(theta, stream=stream)),
+                                     _h(plan._tensors(grads, _dtype_of(grads), stream)), _h(plan._tensors(m, stream=stream)),
+                                     _h(plan._tensors(v, stream=stream)), int(replica), ctypes.byref(how), _opt(grad_scale),
+                                     _opt(decay), _h(plan._tensors(theta_bf16, torch.bfloat16, stream)), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_adamw_step")
+
+
+def sparseloco_adamw_step_8bit(plan: Plan, theta, grads, m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor,
+                               v_scale: torch.Tensor, *, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95,
+                               eps: float = 1e-8, weight_decay: float = 0.1, grad_scale: Optional[torch.Tensor] = None,
+                               decay: Optional[torch.Tensor] = None, theta_bf16=None, replica: int = 0, stream=None) -> None:
+    """sparseloco_adamw_step with the moments in 8 bits: m, m_scale, v, v_scale as plan.adamw_8bit_buffers() makes them
+    (float8_e4m3fn and one fp32 scale per 256 elements, m = scale * value, sqrt(v) = scale * value), in place."""
+    n = plan.num_flat_chunks
+    codes, scales = n * SPLC_CHUNK, n * (SPLC_CHUNK // 256)
+    _check_flat([(m, codes, torch.float8_e4m3fn, "m"), (m_scale, scales, torch.float32, "m_scale"),
+                 (v, codes, torch.float8_e4m3fn, "v"), (v_scale, scales, torch.float32, "v_scale")]
+                + _check_step(plan, grad_scale, decay))
+    how = _AdamW(lr, beta1, beta2, eps, weight_decay, step)
+    rc = lib().sparseloco_adamw_step_8bit(plan.handle, _h(plan._tensors(theta, stream=stream)),
+                                          _h(plan._tensors(grads, _dtype_of(grads), stream)), int(replica), m.data_ptr(),
+                                          m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), ctypes.byref(how),
+                                          _opt(grad_scale), _opt(decay), _h(plan._tensors(theta_bf16, torch.bfloat16, stream)),
+                                          _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_adamw_step_8bit")
+
+
+_FLOATS = {torch.float32: SPLC_F32, torch.bfloat16: SPLC_BF16}
+
+
+def _check_embedding(matrix, table, token_ids, what):
+    """A [rows, d] matrix beside a [vocab, d] table and the ids of the rows; returns rows, vocab, d and the element types."""
+    for t, name in ((matrix, what), (table, "table")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            raise ValueError("%s must be a matrix" % name)
+        if t.dtype not in _FLOATS:
+            raise ValueError("%s: dtype %s, expected float32 or bfloat16" % (name, t.dtype))
+    (rows, d), vocab = matrix.shape, table.shape[0]
+    _check_matrices([(matrix, (rows, d), what, matrix.dtype), (table, (vocab, d), "table", table.dtype),
+                     (token_ids, (rows,), "token_ids", torch.int32)])
+    return rows, vocab, d, _FLOATS[matrix.dtype], _FLOATS[table.dtype]
+
+
+def sparseloco_embedding_lookup(table: torch.Tensor, token_ids: torch.Tensor, out: torch.Tensor, *, t_perp=None, pos_embed=None,
+                                scale: float = 1.0, stream=None) -> None:
+    """out[r] = scale * (table[token_ids[r]] + t_perp[token_ids[r]]) + pos_embed[r % len(pos_embed)].  table, t_perp: [vocab, d],
+    pos_embed: [seq_len, d], all fp32 or all bf16; token_ids: [rows] int32, clamped into the table; out: [rows, d] fp32 or bf16."""
+    rows, vocab, d, out_type, table_type = _check_embedding(out, table, token_ids, "out")
+    specs = [] if t_perp is None else [(t_perp, (vocab, d), "t_perp", table.dtype)]
+    if pos_embed is not None:
+        if pos_embed.dim() != 2 or pos_embed.shape[0] == 0:
+            raise ValueError("pos_embed must be a matrix of one row or more")
+        specs.append((pos_embed, (pos_embed.shape[0], d), "pos_embed", table.dtype))
+    _check_matrices(specs)
+    rc = lib().sparseloco_embedding_lookup(table.data_ptr(), _opt(t_perp), table_type, token_ids.data_ptr(), int(vocab),
+                                           _opt(pos_embed), 0 if pos_embed is None else int(pos_embed.shape[0]), float(scale),
+                                           out.data_ptr(), out_type, int(rows), int(d), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_embedding_lookup")
+
+
+def embedding_grad_workspace(rows: int, vocab: int, d: int, device="cuda") -> torch.Tensor:
+    """A workspace of sparseloco_embedding_grad for up to `rows` tokens."""
+    n = int(lib().sparseloco_embedding_grad_ws_bytes(int(rows), int(vocab), int(d)))
+    if n < 0:
+        raise SparseLoCoError(n, "sparseloco_embedding_grad_ws_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def sparseloco_embedding_grad(grad_out: torch.Tensor, token_ids: torch.Tensor, grad_table: torch.Tensor, ws: torch.Tensor, *,
+                              scale: float = 1.0, ignore_id: int = -1, accumulate: bool = False, stream=None) -> None:
+    """grad_table[x] = scale * sum of grad_out[r] over token_ids[r] == x, added to what is there with accumulate.  grad_out:
+    [rows, d], grad_table: [vocab, d], fp32 or bf16 each; ws: embedding_grad_workspace(rows or more, vocab, d)."""
+    rows, vocab, d, grad_type, table_type = _check_embedding(grad_out, grad_table, token_ids, "grad_out")
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.dim() != 1:
+        raise ValueError("ws: must be a contiguous uint8 tensor")
+    _check_matrices([(ws, ws.shape, "ws", torch.uint8)])
+    rc = lib().sparseloco_embedding_grad(grad_out.data_ptr(), grad_type, token_ids.data_ptr(), int(rows), int(vocab), int(d),
+                                         float(scale), int(ignore_id), grad_table.data_ptr(), table_type, 1 if accumulate else 0,
+                                         ws.data_ptr(), int(ws.numel()), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_embedding_grad")

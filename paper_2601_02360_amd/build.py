@@ -15,7 +15,8 @@ import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("sparseloco.hip", "subspace.hip", "stream_probe.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("sparseloco.hip", "subspace.hip", "stream_probe.hip", "inner.hip",
+                                                          "embedding.hip")]
 LIB = os.path.join(HERE, "libsparseloco.so")
 CALLS = os.path.join(HERE, "_calls.so")
 

@@ -26,30 +26,17 @@
 #include <vector>
 
 #include "launch_rules.h"
+#include "plan.h"
 #include "sparseloco.h"
 
 namespace {
 
-constexpr int kChunk = SPLC_CHUNK;
+using namespace splc;
+
 constexpr int kThreads = 256;            // one workgroup per chunk
 constexpr int kCandCap = 448;            // candidates the exact selection handles (seven per lane; two strip workgroups'
                                          // shares of the LDS end here)
 constexpr int kFilterKappaMax = 256;     // the candidate filter needs kappa <= number of lanes
-
-struct ChunkDesc {
-    uint32_t tensor;                     // index into the pointer tables
-    uint32_t n_c;                        // elements in this chunk (kChunk unless it is an edge chunk)
-    uint64_t offset;                     // element offset of local index 0 inside its tensor
-    uint32_t stride;                     // elements between local rows: 64 (flat) or the matrix's columns (tile)
-    uint8_t h;                           // local rows present (1..64)
-    uint8_t w;                           // width of every row but the last
-    uint8_t last_w;                      // width of the last row (flat tail), = w for a tile
-    uint8_t vec;                         // bit 0: complete (all 4096 elements present), every 4-element vector whole;
-                                         // bit 1: and every row of a bf16 array starts at a dword
-    uint32_t id;                         // chunk number (position of its message in pairs / scales / values)
-    uint32_t reserved;
-};
-static_assert(sizeof(ChunkDesc) == 32, "chunk table entries are 32 bytes");
 
 // Address of lane tid's 4-element vector in slot s (local rows 16 s + tid / 16, columns 4 (tid % 16)...).
 // The slot part is uniform and stays in scalar registers; the per-lane part is one 32-bit byte
@@ -103,33 +90,6 @@ __device__ __forceinline__ void pull(uint32_t n, float& a, float& b, float& c, f
 }
 enum { MODE_PARAMS_F32 = 0, MODE_DIRECT_F32 = 1, MODE_DIRECT_BF16 = 2 };
 
-// Streaming accesses: every dense array is touched exactly once per launch, so loads and stores
-// carry the non-temporal hint (measured on MI355X: 3 reads + 1 write streams at ~6.0 TB/s with
-// the hint against ~5.6 TB/s without).
-// The vector types promise only 4-byte alignment: rows of a tile start at any multiple of 4 bytes,
-// and global memory accepts dword-aligned multi-dword accesses.
-typedef float vfloat4 __attribute__((ext_vector_type(4), aligned(4)));
-
-// Every tensor lives in global memory; saying so lets the compiler emit global_ instead of flat_
-// instructions.
-#define SPLC_GLOBAL __attribute__((address_space(1)))
-typedef uint32_t vuint2 __attribute__((ext_vector_type(2), aligned(2)));        // rows of bf16 may start at any element
-__device__ __forceinline__ float4 stream_load4(const float* p) {
-    vfloat4 v = __builtin_nontemporal_load((const SPLC_GLOBAL vfloat4*)p);
-    return make_float4(v.x, v.y, v.z, v.w);
-}
-__device__ __forceinline__ uint2 stream_load4(const uint16_t* p) {       // four bf16
-    vuint2 v = __builtin_nontemporal_load((const SPLC_GLOBAL vuint2*)p);
-    return make_uint2(v.x, v.y);
-}
-__device__ __forceinline__ float4 cached_load4(const float* p) {
-    vfloat4 v = *(const SPLC_GLOBAL vfloat4*)p;
-    return make_float4(v.x, v.y, v.z, v.w);
-}
-__device__ __forceinline__ uint2 cached_load4(const uint16_t* p) {
-    vuint2 v = *(const SPLC_GLOBAL vuint2*)p;
-    return make_uint2(v.x, v.y);
-}
 __device__ __forceinline__ float4 edge_load4_narrow(const float* origin, EdgeVec v) {
     auto at = [&](uint32_t j) { return origin[v.from4 + j < 4 ? 0u : v.from4 + j - 4]; };
     return make_float4(at(0), at(1), at(2), at(3));
@@ -137,15 +97,6 @@ __device__ __forceinline__ float4 edge_load4_narrow(const float* origin, EdgeVec
 __device__ __forceinline__ uint2 edge_load4_narrow(const uint16_t* origin, EdgeVec v) {
     auto at = [&](uint32_t j) { return (uint32_t)origin[v.from4 + j < 4 ? 0u : v.from4 + j - 4]; };
     return make_uint2(at(0) | at(1) << 16, at(2) | at(3) << 16);
-}
-template <bool STREAM, class T>
-__device__ __forceinline__ auto load4(const T* p) {
-    if constexpr (STREAM) return stream_load4(p);
-    else return cached_load4(p);
-}
-__device__ __forceinline__ void stream_store4(float* p, float4 v) {
-    vfloat4 t = {v.x, v.y, v.z, v.w};
-    __builtin_nontemporal_store(t, (SPLC_GLOBAL vfloat4*)p);
 }
 template <bool STREAM>
 __device__ __forceinline__ void store4(float* p, float4 v) {
@@ -1499,46 +1450,6 @@ __global__ __launch_bounds__(kThreads) void outer_update_kernel(const ChunkDesc*
 
 // ------------------------------------------------------------------ host side
 
-struct sparseloco_plan {
-    int device = 0;
-    int n_tensors = 0;
-    int kappa = 0;
-    int quant = SPLC_QUANT_2BIT;
-    int select = SPLC_SELECT_AUTO;
-    uint32_t* radix_counter = nullptr;   // diagnostic (sparseloco_plan_set_radix_counter), normally null
-    int64_t n_chunks = 0;
-    int64_t n_params = 0;
-    std::vector<int64_t> numel;
-    int layout = SPLC_LAYOUT_FLAT;
-    // Chunk table, ordered [edge chunks | complete, odd row length | other complete ones]; every entry carries its chunk
-    // number.  The edge chunks, which take a little longer, come first so that they do not form the tail of the launch.
-    // The compression of a large tiled plan takes complete tiles four at a time where four lie side by side ("strips", one
-    // entry each: origin, stride and chunk number of the first tile); only the other chunks are in the table above.  Its
-    // outer update, which is element-wise, walks the tensors as flat chunks (a table of its own).
-    // One device allocation holds [chunks | strips | flat chunks of the update | every chunk one by one].
-    ChunkDesc* d_chunks = nullptr;
-    ChunkDesc* h_chunks = nullptr;       // pinned source of the asynchronous upload, kept until destroy
-    int64_t n_entries = 0;               // entries of the chunk table (= n_chunks unless there are strips)
-    int64_t n_gen = 0;                   // edge chunks among them
-    int64_t n_strips = 0;
-    ChunkDesc* d_strips = nullptr;       // inside d_chunks' allocation
-    ChunkDesc* d_update = nullptr;       // = d_chunks for a flat plan
-    int64_t n_update = 0, n_update_gen = 0;
-    ChunkDesc* d_all = nullptr;          // every chunk one by one, for all other kernels (= d_chunks without strips)
-    int64_t n_all_gen = 0;
-};
-
-// n_sets lists of n_tensors device pointers, set-major, resident on the device.
-struct sparseloco_tensors {
-    int device = 0;
-    int n_tensors = 0;
-    int n_sets = 0;
-    int dtype = SPLC_F32;
-    bool disjoint = false;               // no tensor shares memory with another (looked at where it matters: small plans)
-    void** d_table = nullptr;
-    void** h_table = nullptr;            // pinned source of the upload
-};
-
 // Message buffers of n_replicas replicas: device table [pairs: n_replicas][aux: n_replicas].
 struct sparseloco_messages {
     int device = 0;
@@ -1553,33 +1464,12 @@ struct sparseloco_messages {
 
 namespace {
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-bool finite(float v) { return v == v && v - v == 0.f; }
-
-int current_device_is(int device) {
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess) return SPLC_EHIP;
-    return dev == device ? SPLC_OK : SPLC_EPLAN;
-}
-
-// A binding fits the plan: same device, same tensor count, the wanted element type, enough sets.
-int check_tensors(const sparseloco_plan* plan, const sparseloco_tensors* t, int dtype, int min_sets) {
-    if (!t) return SPLC_EINVAL;
-    if (t->device != plan->device || t->n_tensors != plan->n_tensors || t->dtype != dtype) return SPLC_EPLAN;
-    return t->n_sets >= min_sets ? SPLC_OK : SPLC_EINVAL;
-}
 int check_messages(const sparseloco_plan* plan, const sparseloco_messages* m, int min_replicas) {
     if (!m) return SPLC_EINVAL;
     if (m->device != plan->device || m->quant != plan->quant || m->kappa != plan->kappa || m->n_chunks != plan->n_chunks)
         return SPLC_EPLAN;
     return m->n_replicas >= min_replicas ? SPLC_OK : SPLC_EINVAL;
 }
-// Device table of set `set` of a binding (a single-set binding serves every set index).
-template <class T>
-T const* set_table(const sparseloco_tensors* t, int set) {
-    return reinterpret_cast<T const*>(t->d_table + (size_t)(t->n_sets == 1 ? 0 : set) * (size_t)t->n_tensors);
-}
-
 // A small table of device pointers: pinned host copy + device copy, uploaded asynchronously on `stream`.
 int upload_table(size_t n_ptrs, void*** h_out, void*** d_out) {
     const size_t bytes = (n_ptrs ? n_ptrs : 1) * sizeof(void*);
@@ -1889,6 +1779,7 @@ int build_chunk_tables(int n_tensors, const int64_t* rows, const int64_t* cols, 
                 for (size_t pos = x; pos < seg.size(); pos += 8) t.strips[pos] = seg[next++];
         }
         for (int i = 0; i < n_tensors; ++i) append_chunks(t.update, (uint32_t)i, 1, rows[i] * cols[i], false);
+        for (size_t k = 0; k < t.update.size(); ++k) t.update[k].id = (uint32_t)k;
         order_for_launch(t.update, false);
     }
     order_for_launch(t.all, tiled);
