@@ -97,139 +97,165 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
 
 // ---------------------------------------------------------------- gradient: order of the tokens
 //
-// Row v of the table belongs to bucket v % buckets and is row v / buckets in it, so that the frequent tokens, which mostly
-// have low numbers, lie in different buckets.  One workgroup sorts a segment of 16384 tokens in LDS by (bucket, row in it),
-// stably: two counting passes, first by the row, then by the bucket.  In each a wave owns consecutive items and counts
-// them by itself, so that an item's place is the number of smaller ones, of equal ones in earlier waves, and of equal ones
-// before it in its own.
+// Entries (table row, token) are sorted by row, equal rows by token.  A workgroup sorts a block of 2048 in registers and LDS
+// (bitonic, on row * 2048 + place in the block); then up to eight sorted runs at a time become one, every entry finding its place
+// by itself: the number of smaller entries in each of the other runs, by binary search.  Tokens that are left out, and what fills the last
+// block, have row kNone and come last.
+//
+// Where the table is written whole, its zeros are written by further workgroups of these launches, which have little else to
+// do with the memory; rows that have tokens are written again later.
 
-constexpr int kSegment = 16384, kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kItems = kSegment / kSortThreads;              // items of a lane
-constexpr int kMaxBuckets = 2560, kMaxBucketRows = 128;
-constexpr int kWindow = 128;                                 // entries of the sorted order that one partial sum covers
-constexpr uint32_t kNone = 0xFFFFFFFFu;
+constexpr int kBlock = 2048, kBlockBits = 11, kSortThreads = 1024, kFanIn = 8;
+constexpr uint32_t kNone = 0xFFFFFFFFu, kMaxVocab = (1u << (32 - kBlockBits)) - 1;
 
-struct Entry {
-    uint32_t token;                      // position in token_ids
-    uint32_t key;                        // bucket * rows of a bucket + row in it
+// A launch's share of the zeros: 16-byte vectors from `at`, workgroup by workgroup.
+struct Zeros {
+    uint4* at;
+    uint64_t vectors;
 };
-
-struct SortShared {
-    uint16_t count[kSortWaves * kMaxBuckets];
-    uint16_t order[kSegment];            // after the first pass: the segment's tokens by row in their bucket
-    uint32_t wave_total[kSortWaves];
-};
-
-// From digit[j] of a lane's items (kNone: no item), item j of lane l of wave w being number (w * batches + j) * 64 + l: the
-// places place[j] in their stable order.  begins(digit, place) is told where each digit begins.  Returns the number of items.
-template <class Begins>
-__device__ __forceinline__ uint32_t stable_places(SortShared& sh, const uint32_t (&digit)[kItems], uint32_t (&place)[kItems],
-                                                  uint32_t batches, uint32_t digits, int bits, Begins begins) {
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pitch = (digits + 1) & ~1u;
-    uint32_t* words = reinterpret_cast<uint32_t*>(sh.count);
-    for (uint32_t i = tid; i < kSortWaves * pitch / 2; i += kSortThreads) words[i] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kItems; ++j)
-        if (digit[j] != kNone) atomicAdd(words + (wave * pitch + digit[j]) / 2, (digit[j] & 1) ? 1u << 16 : 1u);
-    __syncthreads();
-    const uint32_t each = (digits + kSortThreads - 1) / kSortThreads, first = tid * each;
-    uint32_t sum = 0;
-    for (uint32_t i = first; i < first + each && i < digits; ++i)
-        for (uint32_t w = 0; w < kSortWaves; ++w) sum += sh.count[w * pitch + i];
-    uint32_t upto = sum;                                     // inclusive over the wave
-    for (int step = 1; step < 64; step <<= 1) {
-        const uint32_t y = __shfl_up(upto, step);
-        if ((int)lane >= step) upto += y;
-    }
-    if (lane == 63) sh.wave_total[wave] = upto;
-    __syncthreads();
-    uint32_t run = upto - sum, total = 0;
-    for (uint32_t w = 0; w < kSortWaves; ++w) {
-        if (w < wave) run += sh.wave_total[w];
-        total += sh.wave_total[w];
-    }
-    for (uint32_t i = first; i < first + each && i < digits; ++i) {
-        begins(i, run);
-        for (uint32_t w = 0; w < kSortWaves; ++w) {
-            const uint32_t n = sh.count[w * pitch + i];
-            sh.count[w * pitch + i] = (uint16_t)run;         // (below 16384, the last ones at most 16384)
-            run += n;
-        }
-    }
-    __syncthreads();
-    volatile uint16_t* next = sh.count + wave * pitch;       // (this wave's alone: its LDS accesses keep their order)
-#pragma unroll
-    for (int j = 0; j < kItems; ++j) {
-        if ((uint32_t)j >= batches) break;
-        const bool there = digit[j] != kNone;
-        uint64_t same = __ballot(there);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t ones = __ballot((digit[j] >> b) & 1);
-            same &= ((digit[j] >> b) & 1) ? ones : ~ones;
-        }
-        const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0u));
-        place[j] = kNone;
-        if (there) {
-            place[j] = next[digit[j]] + before;
-            if (before == 0) next[digit[j]] = (uint16_t)(place[j] + __popcll(same));
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
-    return total;
+constexpr int kZeroSpan = 2048;          // vectors a workgroup writes
+__device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group) {
+    typedef uint32_t vuint4 __attribute__((ext_vector_type(4)));
+    const uint64_t from = (uint64_t)group * kZeroSpan;
+    for (uint32_t i = threadIdx.x; i < kZeroSpan; i += blockDim.x)
+        if (from + i < z.vectors) __builtin_nontemporal_store(vuint4{0, 0, 0, 0}, (SPLC_GLOBAL vuint4*)(z.at + from + i));
 }
 
+// The value that lane (this one ^ STRIDE) has.  Below 16 lanes by the vector ALU's own lane moves; through LDS, whose pipe 16
+// waves share, those steps took most of the sort.
+template <int STRIDE>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+    auto move = [](uint32_t v, auto control) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, 0xF, 0xF, true);
+    };
+    using std::integral_constant;
+    if constexpr (STRIDE == 1) return move(x, integral_constant<int, 0xB1>{});           // quads: 1 0 3 2
+    else if constexpr (STRIDE == 2) return move(x, integral_constant<int, 0x4E>{});      // quads: 2 3 0 1
+    else if constexpr (STRIDE == 4)                                                      // 7 - lane of eight, quads: 3 2 1 0
+        return move(move(x, integral_constant<int, 0x141>{}), integral_constant<int, 0x1B>{});
+    else if constexpr (STRIDE == 8) return move(x, integral_constant<int, 0x128>{});     // rows of 16 turned by eight
+    else return __shfl_xor(x, STRIDE);
+}
+// One bitonic step on a lane's two elements, y what the elements `stride` apart hold: the smaller one stays if this is the first of
+// a pair that ascends, or the second of one that descends.
+__device__ __forceinline__ void keep(uint32_t (&x)[2], const uint32_t (&y)[2], const uint32_t (&at)[2], uint32_t size, uint32_t stride) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const bool smaller = ((at[k] & size) == 0) == ((at[k] & stride) == 0);
+        x[k] = smaller == (x[k] < y[k]) ? x[k] : y[k];
+    }
+}
+template <int STRIDE>
+__device__ __forceinline__ void wave_steps(uint32_t (&x)[2], const uint32_t (&at)[2], uint32_t size) {
+    if (STRIDE < (int)size) keep(x, {lane_xor<STRIDE>(x[0]), lane_xor<STRIDE>(x[1])}, at, size, STRIDE);
+    if constexpr (STRIDE > 1) wave_steps<STRIDE / 2>(x, at, size);
+}
+
+// edges: the elements before and behind the 16-byte vectors of the table, written here.
+template <class O>
 __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t* __restrict__ ids, uint32_t rows, int vocab,
-                                                                   int32_t ignore_id, uint32_t buckets, uint32_t bucket_rows,
-                                                                   int bucket_bits, int row_bits, uint32_t* __restrict__ begin,
-                                                                   Entry* __restrict__ entries) {
-    __shared__ SortShared sh;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t base = blockIdx.x * (uint32_t)kSegment, n = rows - base < kSegment ? rows - base : kSegment;
-    ids += base;
-    begin += (uint64_t)blockIdx.x * (buckets + 1);
-    entries += base;
-    uint32_t digit[kItems], place[kItems];
-    uint32_t batches = (n + kSortThreads - 1) / kSortThreads;
-#pragma unroll
-    for (int j = 0; j < kItems; ++j) {
-        const uint32_t t = (wave * batches + j) * 64 + lane;
-        digit[j] = kNone;
-        if ((uint32_t)j < batches && t < n) {
-            const int32_t id = ids[t];
-            if (ignore_id < 0 || id != ignore_id) digit[j] = (uint32_t)row_of(id, vocab) / buckets;
+                                                                   int32_t ignore_id, uint32_t blocks, uint32_t* __restrict__ row,
+                                                                   uint32_t* __restrict__ token, Zeros zeros, O* table,
+                                                                   uint64_t table_size, uint32_t head, uint32_t tail) {
+    const uint32_t tid = threadIdx.x;
+    if (blockIdx.x >= blocks) {
+        if (blockIdx.x == blocks) {
+            if (tid < head) table[tid] = O(0);
+            if (tid < tail) table[table_size - 1 - tid] = O(0);
         }
+        write_zeros(zeros, blockIdx.x - blocks);
+        return;
     }
-    const uint32_t m = stable_places(sh, digit, place, batches, bucket_rows, row_bits, [](uint32_t, uint32_t) {});
+    __shared__ uint32_t shared[kBlock];
+    // element p of the block: lane p % 64 of wave p / 128, its first or second by p / 64 % 2
+    const uint32_t at[2] = {(tid >> 6) * 128 + (tid & 63), (tid >> 6) * 128 + (tid & 63) + 64};
+    const uint32_t base = blockIdx.x * (uint32_t)kBlock;
+    uint32_t x[2];
 #pragma unroll
-    for (int j = 0; j < kItems; ++j)
-        if ((uint32_t)j < batches && place[j] != kNone) sh.order[place[j]] = (uint16_t)((wave * batches + j) * 64 + lane);
+    for (int k = 0; k < 2; ++k) {
+        uint32_t v = kNone;
+        if (base + at[k] < rows) {
+            const int32_t id = ids[base + at[k]];
+            if (ignore_id < 0 || id != ignore_id) v = (uint32_t)row_of(id, vocab) << kBlockBits | at[k];
+        }
+        x[k] = v == kNone ? kMaxVocab << kBlockBits | at[k] : v;
+    }
+    for (uint32_t size = 2; size <= kBlock; size *= 2) {
+        for (uint32_t stride = size / 2; stride >= 128; stride /= 2) {
+            __syncthreads();
+            shared[at[0]] = x[0];
+            shared[at[1]] = x[1];
+            __syncthreads();
+            keep(x, {shared[at[0] ^ stride], shared[at[1] ^ stride]}, at, size, stride);
+        }
+        if (size >= 128) keep(x, {x[1], x[0]}, at, size, 64);
+        wave_steps<32>(x, at, size);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t r = x[k] >> kBlockBits;
+        row[base + at[k]] = r == kMaxVocab ? kNone : r;
+        token[base + at[k]] = base + (x[k] & (kBlock - 1));
+    }
+}
+
+// Sorted runs of `length` entries (the last one of all may be shorter), kFanIn of them at a time, to one run.  Of every run 256
+// entries at equal distances lie in LDS for the first steps of the search; from a distance of 32 on the others are in one cache line.
+constexpr uint32_t kSamples = 256;
+__global__ __launch_bounds__(256) void merge_runs_kernel(const uint32_t* __restrict__ row, const uint32_t* __restrict__ token,
+                                                         uint32_t entries, uint32_t length, uint32_t* __restrict__ row_out,
+                                                         uint32_t* __restrict__ token_out, uint32_t groups, Zeros zeros) {
+    if (blockIdx.x >= groups) {
+        write_zeros(zeros, blockIdx.x - groups);
+        return;
+    }
+    __shared__ uint32_t sample[kFanIn * kSamples];           // the last entry of each stretch
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x;       // (the number of entries is a multiple of 2048, as is a run's)
+    const uint32_t run = blockIdx.x * 256 / length, first = run / kFanIn * kFanIn, stretch = length / kSamples;
+    uint32_t some[kFanIn * kSamples / 256];
+#pragma unroll
+    for (uint32_t s = 0; s < kFanIn * kSamples / 256; ++s) {
+        const uint64_t at = (uint64_t)first * length + (uint64_t)(s * 256 + threadIdx.x + 1) * stretch - 1;
+        some[s] = at < entries ? row[at] : kNone;
+    }
+    const uint32_t r = row[i], t = token[i];
+#pragma unroll
+    for (uint32_t s = 0; s < kFanIn * kSamples / 256; ++s) sample[s * 256 + threadIdx.x] = some[s];
     __syncthreads();
-    batches = (m + kSortThreads - 1) / kSortThreads;
-    uint32_t token[kItems], key[kItems];
+    uint32_t below[kFanIn] = {};                             // entries that go before this one; the searches go side by side
+    auto before = [&](uint32_t seen, uint32_t k) { return seen < r || (seen == r && first + k < run); };     // (of equal rows)
+#pragma unroll 1
+    for (uint32_t step = kSamples / 2; step > 0; step /= 2)
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) {
-        const uint32_t i = (wave * batches + j) * 64 + lane;
-        digit[j] = kNone;
-        if ((uint32_t)j < batches && i < m) {
-            token[j] = sh.order[i];
-            const uint32_t v = (uint32_t)row_of(ids[token[j]], vocab);
-            digit[j] = v % buckets;
-            key[j] = digit[j] * bucket_rows + v / buckets;
+        for (uint32_t k = 0; k < kFanIn; ++k)
+            if (before(sample[k * kSamples + below[k] + step - 1], k)) below[k] += step;
+    // (255 stretches at most are counted: whether the last one goes before is for the steps below to find)
+#pragma unroll
+    for (uint32_t k = 0; k < kFanIn; ++k) below[k] *= stretch;
+    for (uint32_t step = stretch; step > 0; step /= 2) {
+        uint32_t seen[kFanIn];
+        bool inside[kFanIn];
+#pragma unroll
+        for (uint32_t k = 0; k < kFanIn; ++k) {
+            const uint64_t at = (uint64_t)(first + k) * length + below[k] + step - 1;
+            inside[k] = below[k] + step <= length && at < entries;
+            seen[k] = inside[k] ? row[at] : kNone;
         }
-    }
-    const uint32_t all = stable_places(sh, digit, place, batches, buckets, bucket_bits,
-                                       [&](uint32_t bucket, uint32_t at) { begin[bucket] = at; });
-    if (tid == 0) begin[buckets] = all;
 #pragma unroll
-    for (int j = 0; j < kItems; ++j)
-        if ((uint32_t)j < batches && place[j] != kNone) entries[place[j]] = Entry{base + token[j], key[j]};
+        for (uint32_t k = 0; k < kFanIn; ++k)
+            if (inside[k] && before(seen[k], k)) below[k] += step;
+    }
+    uint32_t place = first * length + (i - run * length);
+#pragma unroll
+    for (uint32_t k = 0; k < kFanIn; ++k) place += first + k == run ? 0 : below[k];
+    row_out[place] = r;
+    token_out[place] = t;
 }
 
 // ---------------------------------------------------------------- gradient: sums
 //
-// A wave takes one bucket's rows in one span of columns.  A lane has VEC consecutive columns: four, or one where the table
-// is narrow.
+// A wave takes the runs of equal rows that begin in one piece of 16 entries, in one span of columns.  A lane has VEC consecutive
+// columns: four, or one where the table is narrow.
 
 // The lane's columns of a slice.  The last vector of a row whose length is no multiple of four holds fewer: it is read as the
 // four elements that end with the row (`back` elements earlier), and its elements are brought to the front.
@@ -239,7 +265,7 @@ struct Columns {
     __device__ __forceinline__ Columns(int d, int slice, int slices, int lane) {
         const int vecs = (d + VEC - 1) / VEC, each = (vecs + slices - 1) / slices, at = slice * each + lane;
         const bool mine = lane < each && at < vecs;
-        col = at * VEC;
+        col = mine ? at * VEC : 0;                           // (a lane without columns reads the first and writes nothing)
         n = mine ? (d - col < VEC ? d - col : VEC) : 0;
         back = mine ? VEC - n : 0;
     }
@@ -252,7 +278,7 @@ template <int VEC, class G>
 __device__ __forceinline__ Sums<VEC> load_grad(const G* grad, uint64_t token, int d, const Columns<VEC>& at) {
     Sums<VEC> s;
     if constexpr (VEC == 4) {
-        const float4 x = widened(stream_load4(grad + token * (uint64_t)d + at.col - at.back));
+        const float4 x = widened(cached_load4(grad + token * (uint64_t)d + at.col - at.back));
         s.v[0] = x.x; s.v[1] = x.y; s.v[2] = x.z; s.v[3] = x.w;
     } else {
         s.v[0] = widened(grad[token * (uint64_t)d + at.col]);
@@ -265,180 +291,188 @@ __device__ __forceinline__ void add(Sums<VEC>& a, const Sums<VEC>& b) {
     for (int j = 0; j < VEC; ++j) a.v[j] += b.v[j];
 }
 
-constexpr int kBatch = 16;               // rows of grad_out in flight
+constexpr int kWaves = 4;                // independent waves of a workgroup: neighbouring columns of the same rows
+constexpr int kPiece = 16;               // entries of a piece: rows of grad_out in flight
+constexpr int kWindow = 64;              // entries that one partial sum covers: those a wave looks at together
+static_assert(kWindow <= 64 && kBlock % kWindow == 0 && kWindow % kPiece == 0, "a wave walks whole windows");
 
-// Windows of the sorted order that lie inside one row's run: their sums, so that a frequent token's run is not left to one wave.
+// Windows of entries that lie inside one run: their sums, so that a frequent token's run is not left to one wave.
 template <int VEC, class G>
-__global__ __launch_bounds__(64) void window_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ begin,
-                                                         const Entry* __restrict__ entries, uint32_t buckets, int d, int slices,
-                                                         float* __restrict__ partial) {
-    const uint32_t window = blockIdx.x, segment = window / (kSegment / kWindow);
-    const uint32_t first = window * kWindow, last = first + kWindow - 1;
-    if (last - segment * kSegment >= begin[(uint64_t)segment * (buckets + 1) + buckets]) return;
-    if (entries[first].key != entries[last].key) return;
-    const Columns<VEC> at(d, blockIdx.y, slices, threadIdx.x);
-    if (at.n == 0) return;
-    Sums<VEC> sum = {};
-    for (int e = 0; e < kWindow; e += kBatch) {
-        Sums<VEC> x[kBatch];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) x[k] = load_grad<VEC>(grad, entries[first + e + k].token, d, at);
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) add(sum, x[k]);
+__global__ __launch_bounds__(64) void window_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
+                                                         const uint32_t* __restrict__ token, int d, int slices,
+                                                         float* __restrict__ partial, uint32_t groups, Zeros zeros) {
+    if (blockIdx.x >= groups) {
+        write_zeros(zeros, blockIdx.x - groups);
+        return;
     }
-    float* to = partial + (uint64_t)window * slices * 64 * VEC + ((uint64_t)blockIdx.y * 64 + threadIdx.x) * VEC;
+    const uint32_t window = blockIdx.x / (uint32_t)slices, slice = blockIdx.x % (uint32_t)slices, first = window * kWindow;
+    if (row[first] != row[first + kWindow - 1] || row[first] == kNone) return;
+    const Columns<VEC> at(d, (int)slice, slices, (int)threadIdx.x);
+    Sums<VEC> sum = {};
+    for (int e = 0; e < kWindow; e += kPiece) {
+        Sums<VEC> x[kPiece];
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) x[k] = load_grad<VEC>(grad, token[first + e + k], d, at);
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) add(sum, x[k]);
+    }
+    float* to = partial + ((uint64_t)blockIdx.x * 64 + threadIdx.x) * VEC;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) to[j] = sum.v[j];
 }
 
 // Writes a row's columns: scale * sum, added to what is there if asked to.
 template <int VEC, class O>
-__device__ __forceinline__ void store_row(O* out, const Columns<VEC>& at, Sums<VEC> s, float scale, bool accumulate) {
+__device__ __forceinline__ void store_row(O* out, const Columns<VEC>& at, Sums<VEC> s, float scale, const Sums<VEC>* was) {
     if constexpr (VEC == 4) {
         if (at.back & 1) { s.v[0] = s.v[1]; s.v[1] = s.v[2]; s.v[2] = s.v[3]; }
         if (at.back & 2) { s.v[0] = s.v[2]; s.v[1] = s.v[3]; }
         float4 x = make_float4(s.v[0] * scale, s.v[1] * scale, s.v[2] * scale, s.v[3] * scale);
-        if (accumulate) {
-            const float4 was = load_some(out + at.col, at.n);
-            x = make_float4(was.x + x.x, was.y + x.y, was.z + x.z, was.w + x.w);
-        }
+        if (was) x = make_float4(was->v[0] + x.x, was->v[1] + x.y, was->v[2] + x.z, was->v[3] + x.w);
         store_some(out + at.col, at.n, x);
     } else {
-        store1(out + at.col, accumulate ? widened(out[at.col]) + s.v[0] * scale : s.v[0] * scale);
+        store1(out + at.col, was ? was->v[0] + s.v[0] * scale : s.v[0] * scale);
     }
 }
+template <int VEC, class O>
+__device__ __forceinline__ Sums<VEC> load_row(const O* out, const Columns<VEC>& at) {
+    Sums<VEC> s;
+    if constexpr (VEC == 4) {
+        const float4 x = load_some(out + at.col, at.n);
+        s.v[0] = x.x; s.v[1] = x.y; s.v[2] = x.z; s.v[3] = x.w;
+    } else {
+        s.v[0] = widened(out[at.col]);
+    }
+    return s;
+}
 
-template <int VEC, bool MANY, class G, class O>
-__global__ __launch_bounds__(64) void row_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ begin,
-                                                      const Entry* __restrict__ entries, const float* __restrict__ partial,
-                                                      uint32_t segments, uint32_t buckets, uint32_t bucket_rows, int vocab, int d,
-                                                      int slices, float scale, bool accumulate, O* __restrict__ out) {
-    extern __shared__ float held[];                          // MANY: [row in the bucket][VEC][64]
-    const uint32_t bucket = blockIdx.x / (uint32_t)slices, slice = blockIdx.x % (uint32_t)slices, lane = threadIdx.x;
+template <int VEC, bool ADDED, class G, class O>
+__global__ __launch_bounds__(kWaves * 64) void row_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
+                                                      const uint32_t* __restrict__ token, const float* __restrict__ partial,
+                                                      uint32_t entries, int d, int slices, float scale,
+                                                      O* __restrict__ out) {
+    const uint32_t unit = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const uint32_t piece = unit / (uint32_t)slices, slice = unit % (uint32_t)slices;
+    if (piece * kPiece >= entries) return;
+    // the piece's window, an entry a lane (their number is a multiple of 2048); the piece begins at entry q of it
+    uint32_t e = piece * kPiece / kWindow * kWindow;
+    const uint32_t q = piece * kPiece % kWindow;
+    uint32_t rows = row[e + lane % kWindow], tokens = token[e + lane % kWindow];
+    auto row_at = [&](uint32_t k) { return __builtin_amdgcn_readlane(rows, k); };
+    uint32_t now = q > 0 ? row_at(q - 1) : (e > 0 ? row[e - 1] : kNone);         // the run that `sum` belongs to
+    const uint32_t last = row_at(q + kPiece - 1);
+    if (row_at(q) == kNone || (piece > 0 && last == now)) return;                // nothing begins here
     const Columns<VEC> at(d, (int)slice, slices, (int)lane);
-    if (at.n == 0) return;
-    uint64_t touched[kMaxBucketRows / 64] = {};
-    uint32_t row = kNone, next = 0;                          // the run that `sum` belongs to; first row not yet written
     Sums<VEC> sum = {};
-    auto out_row = [&](uint32_t r) { return out + ((uint64_t)r * buckets + bucket) * (uint64_t)d; };
-    auto empty_rows = [&](uint32_t upto) {                   // rows next .. upto - 1 got nothing
-        if (!accumulate)
-            for (uint32_t r = next; r < upto && (uint64_t)r * buckets + bucket < (uint64_t)vocab; ++r)
-                store_row<VEC>(out_row(r), at, Sums<VEC>{}, 0.f, false);
-    };
-    auto done = [&]() {                                      // the run ends
-        if (row == kNone) return;
-        if constexpr (MANY) {
-            const bool more = (touched[row / 64] >> (row % 64)) & 1;
+    auto out_row = [&](uint32_t r) { return out + (uint64_t)r * (uint64_t)d; };
+    // Rows of grad_out of entries k .. k + 15 of the window at hand; those from `end` on are read as the last one before it.
+    auto load = [&](Sums<VEC> (&x)[kPiece], uint32_t k, uint32_t end) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                float* h = held + (row * VEC + j) * 64 + lane;
-                *h = more ? *h + sum.v[j] : sum.v[j];
-            }
-            touched[row / 64] |= 1ull << (row % 64);
-        } else {
-            empty_rows(row);
-            store_row<VEC>(out_row(row), at, sum, scale, accumulate);
-            next = row + 1;
+        for (uint32_t i = 0; i < kPiece; ++i)
+            x[i] = load_grad<VEC>(grad, __builtin_amdgcn_readlane(tokens, k + i < end ? k + i : end - 1), d, at);
+    };
+    // How far the entries from k on belong to `now`.
+    auto run_end = [&](uint32_t k) {
+        const uint64_t others = k < kWindow ? __ballot(rows != now && lane < kWindow) >> k << k : 0;
+        return others == 0 ? kWindow : (uint32_t)__builtin_ctzll(others);
+    };
+    auto add_run = [&](uint32_t k, uint32_t end) {
+        for (; k < end; k += kPiece) {
+            Sums<VEC> x[kPiece];
+            load(x, k, end);
+#pragma unroll
+            for (uint32_t i = 0; i < kPiece; ++i)
+                if (k + i < end) add(sum, x[i]);
         }
     };
-    for (uint32_t segment = 0; segment < segments; ++segment) {
-        const uint32_t* b = begin + (uint64_t)segment * (buckets + 1) + bucket;
-        const uint32_t origin = segment * kSegment, end = origin + b[1];
-        uint32_t e = origin + b[0];
-        row = kNone;
-        while (e < end) {
-            const uint32_t r = entries[e].key - bucket * bucket_rows;
-            if (partial && e % kWindow == 0 && e + kWindow <= end && entries[e + kWindow - 1].key == entries[e].key) {
-                const float* from = partial + (uint64_t)(e / kWindow) * slices * 64 * VEC + ((uint64_t)slice * 64 + lane) * VEC;
-                Sums<VEC> x;
+    {
+        Sums<VEC> x[kPiece];
+        uint32_t r[kPiece];
+        load(x, q, q + kPiece);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) x.v[j] = from[j];
-                if (r == row) {
-                    add(sum, x);
-                } else {
-                    done();
-                    row = r;
-                    sum = x;
+        for (uint32_t i = 0; i < kPiece; ++i) r[i] = row_at(q + i);
+        // x becomes the sums of the runs up to here: those that end inside the piece are written, unless they began before it
+#pragma unroll
+        for (uint32_t i = 1; i < kPiece; ++i)
+            if (r[i] == r[i - 1]) {
+                Sums<VEC> upto = x[i - 1];
+                add(upto, x[i]);
+                x[i] = upto;
+            }
+        auto written = [&](uint32_t i) { return r[i] != now && r[i] != kNone && r[i] != last; };
+#pragma unroll
+        for (uint32_t half = 0; half < kPiece; half += kPiece / 2) {
+            Sums<VEC> was[kPiece / 2];
+            if (ADDED && at.n > 0)
+#pragma unroll
+                for (uint32_t i = 0; i < kPiece / 2; ++i)
+                    if (i + half + 1 < kPiece && r[half + i] != r[half + i + 1] && written(half + i))
+                        was[i] = load_row<VEC>(out_row(r[half + i]), at);
+            if (at.n > 0)
+#pragma unroll
+                for (uint32_t i = 0; i < kPiece / 2; ++i)
+                    if (i + half + 1 < kPiece && r[half + i] != r[half + i + 1] && written(half + i))
+                        store_row<VEC>(out_row(r[half + i]), at, x[half + i], scale, ADDED ? &was[i] : nullptr);
+        }
+        sum = x[kPiece - 1];
+    }
+    if (last == kNone) return;
+    now = last;
+    uint32_t end = run_end(q + kPiece);
+    add_run(q + kPiece, end);
+    while (end == kWindow && (e += kWindow) < entries) {     // the run goes on in the next window
+        if (partial) {                                       // and in whole ones, up to 16 at a time
+            const uint32_t w = e + lane * kWindow;
+            const bool whole = lane < kPiece && w < entries && row[w] == now && row[w + kWindow - 1] == now;
+            const uint32_t n = (uint32_t)__builtin_ctzll(~__ballot(whole));
+            if (n > 0) {
+                Sums<VEC> x[kPiece];
+#pragma unroll
+                for (uint32_t i = 0; i < kPiece; ++i) {
+                    const float* from = partial + ((((uint64_t)(e / kWindow) + (i < n ? i : n - 1)) * slices + slice) * 64 + lane) * VEC;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) x[i].v[j] = from[j];
                 }
-                e += kWindow;
+#pragma unroll
+                for (uint32_t i = 0; i < kPiece; ++i)
+                    if (i < n) add(sum, x[i]);
+                e += (n - 1) * kWindow;
                 continue;
             }
-            const uint32_t n = kBatch - e % kBatch < end - e ? kBatch - e % kBatch : end - e;
-            Sums<VEC> x[kBatch];
-            uint32_t rows[kBatch];
-#pragma unroll
-            for (uint32_t k = 0; k < kBatch; ++k) {
-                const Entry entry = entries[e + (k < n ? k : n - 1)];
-                rows[k] = entry.key - bucket * bucket_rows;
-                x[k] = load_grad<VEC>(grad, entry.token, d, at);
-            }
-#pragma unroll
-            for (uint32_t k = 0; k < kBatch; ++k) {
-                if (k >= n) break;
-                if (rows[k] == row) {
-                    add(sum, x[k]);
-                } else {
-                    done();
-                    row = rows[k];
-                    sum = x[k];
-                }
-            }
-            e += n;
         }
-        done();
+        rows = row[e + lane % kWindow];
+        tokens = token[e + lane % kWindow];
+        end = run_end(0);
+        add_run(0, end);
     }
-    if constexpr (MANY) {
-        for (uint32_t r = 0; r < bucket_rows && (uint64_t)r * buckets + bucket < (uint64_t)vocab; ++r) {
-            Sums<VEC> s = {};
-            const bool some = (touched[r / 64] >> (r % 64)) & 1;
-            if (!some && accumulate) continue;
-            if (some)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) s.v[j] = held[(r * VEC + j) * 64 + lane];
-            store_row<VEC>(out_row(r), at, s, scale, accumulate);
-        }
-    } else {
-        empty_rows(bucket_rows);
+    if (at.n > 0) {
+        Sums<VEC> was;
+        if (ADDED) was = load_row<VEC>(out_row(now), at);
+        store_row<VEC>(out_row(now), at, sum, scale, ADDED ? &was : nullptr);
     }
 }
 
 // ---------------------------------------------------------------- host side
 
-int bits_of(uint32_t values) {           // bits that tell 0 .. values - 1 apart
-    int bits = 0;
-    while (bits < 31 && (1u << bits) < values) ++bits;
-    return bits;
-}
-
-// How a table's rows are dealt to buckets.
-struct Buckets {
-    uint32_t rows_each, count;
-    explicit Buckets(int vocab) {
-        rows_each = ((uint32_t)vocab + kMaxBuckets - 1) / kMaxBuckets;
-        count = ((uint32_t)vocab + rows_each - 1) / rows_each;
-    }
-};
-constexpr int64_t kMaxVocab = (int64_t)kMaxBuckets * kMaxBucketRows;
-
 int vec_of(int d) { return d < 256 ? 1 : 4; }
 int slices_of(int d) { return ((d + vec_of(d) - 1) / vec_of(d) + 63) / 64; }
 
-// The workspace: where every segment's buckets begin, the entries, the windows' sums.
+// The workspace: entries (rows and tokens) of two stages of the sort in turn, the windows' sums.
 struct GradSpace {
-    int64_t segments, begin, entries, partial, bytes;
-    GradSpace(int64_t rows, int vocab, int d) {
-        const Buckets b(vocab);
-        segments = (rows + kSegment - 1) / kSegment;
-        begin = 0;
-        entries = (segments * (b.count + 1) * 4 + 255) / 256 * 256;
-        partial = entries + (rows * (int64_t)sizeof(Entry) + 255) / 256 * 256;
-        bytes = partial + segments * (kSegment / kWindow) * slices_of(d) * 64 * vec_of(d) * 4;
+    int64_t entries, row[2], token[2], partial, bytes;
+    GradSpace(int64_t rows, int d) {
+        entries = (rows + kBlock - 1) / kBlock * kBlock;
+        row[0] = 0;
+        token[0] = row[0] + 4 * entries;
+        row[1] = token[0] + 4 * entries;
+        token[1] = row[1] + 4 * entries;
+        partial = token[1] + 4 * entries;
+        bytes = partial + entries / kWindow * slices_of(d) * 64 * vec_of(d) * 4;
     }
 };
 
 bool grad_sizes_fit(int64_t rows, int vocab, int d) {
-    return rows >= 0 && rows < (int64_t)1 << 31 && vocab >= 1 && vocab <= kMaxVocab && d >= 1 && d < 1 << 24;
+    return rows >= 0 && rows < ((int64_t)1 << 31) - kBlock && vocab >= 1 && vocab < (int)kMaxVocab && d >= 1 && d < 1 << 24;
 }
 
 }  // namespace
@@ -475,7 +509,7 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
 
 int64_t sparseloco_embedding_grad_ws_bytes(int64_t rows, int vocab, int d) {
     if (!grad_sizes_fit(rows, vocab, d)) return SPLC_EINVAL;
-    return GradSpace(rows, vocab, d).bytes;
+    return GradSpace(rows, d).bytes;
 }
 
 int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_t* token_ids, int64_t rows, int vocab, int d,
@@ -488,42 +522,68 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     if (!aligned(grad_out, grad_dtype == SPLC_BF16 ? 2 : 4) || !aligned(grad_table, table_dtype == SPLC_BF16 ? 2 : 4) ||
         !aligned(token_ids, 4) || !aligned(ws, 8))
         return SPLC_EALIGN;
-    const GradSpace space(rows, vocab, d);
+    const GradSpace space(rows, d);
     if (ws_bytes < space.bytes) return SPLC_EINVAL;
-    const Buckets b(vocab);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    char* at = static_cast<char*>(ws);
-    uint32_t* begin = reinterpret_cast<uint32_t*>(at + space.begin);
-    Entry* entries = reinterpret_cast<Entry*>(at + space.entries);
-    float* partial = reinterpret_cast<float*>(at + space.partial);
     const int slices = slices_of(d);
-    const uint32_t segments = (uint32_t)space.segments;
-    if (segments > 0)
-        hipLaunchKernelGGL(sort_tokens_kernel, dim3(segments), dim3(kSortThreads), 0, st, token_ids, (uint32_t)rows, vocab, ignore_id,
-                           b.count, b.rows_each, bits_of(b.count), bits_of(b.rows_each), begin, entries);
-    const bool windows = rows >= 2048;
-    auto launch = [&](auto vec, auto gradient, auto result) {
+    const uint32_t entries = (uint32_t)space.entries, blocks = entries / kBlock;
+    const bool many = blocks > 1;        // to be merged, and runs worth more than a wave
+    uint32_t *row[2], *token[2];
+    for (int k = 0; k < 2; ++k) {
+        row[k] = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + space.row[k]);
+        token[k] = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + space.token[k]);
+    }
+    float* partial = reinterpret_cast<float*>(static_cast<char*>(ws) + space.partial);
+
+    // the table in elements before its 16-byte vectors, vectors, and elements behind them; and the launches' shares of these
+    const uint64_t size = (uint64_t)vocab * (uint64_t)d, element = table_dtype == SPLC_BF16 ? 2 : 4;
+    uint64_t head = (16 - (reinterpret_cast<uintptr_t>(grad_table) & 15)) % 16 / element;
+    if (head > size) head = size;
+    const uint64_t vectors = accumulate ? 0 : (size - head) * element / 16;
+    const uint64_t tail = size - head - vectors * 16 / element;
+    uint4* vector = reinterpret_cast<uint4*>(static_cast<char*>(grad_table) + head * element);
+    const uint64_t sort_share = many ? vectors / 2 : vectors, merge_share = many ? vectors / 4 : 0;
+    const Zeros shares[3] = {{vector, sort_share}, {vector + sort_share, merge_share},
+                             {vector + sort_share + merge_share, vectors - sort_share - merge_share}};
+    auto groups_of = [](const Zeros& z) { return (uint32_t)((z.vectors + kZeroSpan - 1) / kZeroSpan); };
+
+    auto sort = [&](auto result) {
+        using O = decltype(result);
+        const uint32_t more = accumulate ? 0 : groups_of(shares[0]) + (shares[0].vectors == 0 ? 1 : 0);
+        if (blocks + more > 0)
+            hipLaunchKernelGGL(sort_tokens_kernel<O>, dim3(blocks + more), dim3(kSortThreads), 0, st, token_ids, (uint32_t)rows, vocab,
+                               ignore_id, blocks, row[0], token[0], shares[0], static_cast<O*>(grad_table), size, (uint32_t)head,
+                               (uint32_t)tail);
+    };
+    if (table_dtype == SPLC_F32) sort(float{});
+    else sort(uint16_t{});
+    if (rows == 0) return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
+    int in = 0;
+    for (uint64_t length = kBlock; length < entries; length *= kFanIn, in ^= 1) {
+        const Zeros share = length == kBlock ? shares[1] : Zeros{nullptr, 0};
+        hipLaunchKernelGGL(merge_runs_kernel, dim3(entries / 256 + groups_of(share)), dim3(256), 0, st, row[in], token[in], entries,
+                           (uint32_t)length, row[in ^ 1], token[in ^ 1], entries / 256, share);
+    }
+    auto sums = [&](auto vec, auto gradient, auto result) {
         constexpr int VEC = decltype(vec)::value;
         using G = decltype(gradient);
         using O = decltype(result);
-        if (windows)
-            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3((unsigned)(rows / kWindow), (unsigned)slices), dim3(64), 0, st,
-                               static_cast<const G*>(grad_out), begin, entries, b.count, d, slices, partial);
-        const dim3 grid((unsigned)(b.count * (uint32_t)slices));
-        if (segments > 1)
-            hipLaunchKernelGGL((row_sums_kernel<VEC, true, G, O>), grid, dim3(64), b.rows_each * VEC * 64 * sizeof(float), st,
-                               static_cast<const G*>(grad_out), begin, entries, windows ? partial : nullptr, segments, b.count,
-                               b.rows_each, vocab, d, slices, scale, accumulate != 0, static_cast<O*>(grad_table));
-        else
-            hipLaunchKernelGGL((row_sums_kernel<VEC, false, G, O>), grid, dim3(64), 0, st, static_cast<const G*>(grad_out), begin,
-                               entries, windows ? partial : nullptr, segments, b.count, b.rows_each, vocab, d, slices, scale,
-                               accumulate != 0, static_cast<O*>(grad_table));
+        if (many)
+            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(entries / kWindow * (uint32_t)slices + groups_of(shares[2])), dim3(64), 0,
+                               st, static_cast<const G*>(grad_out), row[in], token[in], d, slices, partial,
+                               entries / kWindow * (uint32_t)slices, shares[2]);
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((entries / kPiece * (uint32_t)slices + kWaves - 1) / kWaves), dim3(kWaves * 64), 0, st,
+                               static_cast<const G*>(grad_out), row[in], token[in], many ? partial : nullptr, entries, d, slices, scale, static_cast<O*>(grad_table));
+        };
+        if (accumulate) launch(row_sums_kernel<VEC, true, G, O>);
+        else launch(row_sums_kernel<VEC, false, G, O>);
     };
     auto by_type = [&](auto vec) {
-        if (grad_dtype == SPLC_F32 && table_dtype == SPLC_F32) launch(vec, float{}, float{});
-        else if (grad_dtype == SPLC_F32) launch(vec, float{}, uint16_t{});
-        else if (table_dtype == SPLC_F32) launch(vec, uint16_t{}, float{});
-        else launch(vec, uint16_t{}, uint16_t{});
+        if (grad_dtype == SPLC_F32 && table_dtype == SPLC_F32) sums(vec, float{}, float{});
+        else if (grad_dtype == SPLC_F32) sums(vec, float{}, uint16_t{});
+        else if (table_dtype == SPLC_F32) sums(vec, uint16_t{}, float{});
+        else sums(vec, uint16_t{}, uint16_t{});
     };
     if (vec_of(d) == 4) by_type(std::integral_constant<int, 4>{});
     else by_type(std::integral_constant<int, 1>{});

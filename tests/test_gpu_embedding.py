@@ -121,10 +121,11 @@ def test_gradient_of_few_tokens(rows, vocab, d):
 
 
 @pytest.mark.parametrize("rows,vocab,d", [(2048, 4000, 260), (4097, 300, 513), (16384, 32000, 64), (16383, 2000, 300), (16385, 2561, 257),
-                                          (40000, 999, 65), (33000, 9000, 270), (50000, 3, 258)])
+                                          (40000, 999, 65), (33000, 9000, 270), (50000, 3, 258), (2049, 40, 64),
+                                          (65537, 700, 80), (140000, 5000, 66)])
 @pytest.mark.parametrize("how", ["text", "same", "spread"])
 def test_gradient_of_many_tokens(rows, vocab, d, how):
-    """Long runs of one token, more than one segment of the sort, rows of a bucket that no segment holds."""
+    """Long runs of one token, several blocks of the sort, one and two rounds of merging."""
     check_grad(rows, vocab, d, how)
 
 
@@ -136,7 +137,7 @@ def test_gradient_types_accumulation_and_padding(rows, vocab, d, grad_type, tabl
         check_grad(rows, vocab, d, how, grad_type, table_type, accumulate, ignore, scale=-0.7)
 
 
-@pytest.mark.parametrize("rows,vocab,d", [(3000, 50304, 768), (17000, 32001, 2050), (300, 262144, 300), (18000, 262144, 256), (20, 327680, 8)])
+@pytest.mark.parametrize("rows,vocab,d", [(3000, 50304, 768), (17000, 32001, 2050), (300, 262144, 300), (18000, 262144, 256), (20, 2 ** 21 - 2, 3)])
 def test_gradient_at_the_models_sizes_and_the_largest_tables(rows, vocab, d):
     check_grad(rows, vocab, d, "text")
 
@@ -223,7 +224,7 @@ def test_refusals():
     for call in (lambda: B.sparseloco_embedding_lookup(table, ids, x, scale=float("nan")),
                  lambda: B.sparseloco_embedding_grad(x, ids, table, ws, scale=float("inf")),
                  lambda: B.sparseloco_embedding_grad(x, ids, table, ws[:8]),
-                 lambda: B.embedding_grad_workspace(8, 327681, 16), lambda: B.embedding_grad_workspace(8, 0, 16),
+                 lambda: B.embedding_grad_workspace(8, 2 ** 21 - 1, 16), lambda: B.embedding_grad_workspace(8, 0, 16),
                  lambda: B.embedding_grad_workspace(-1, 5, 16)):
         with pytest.raises(B.SparseLoCoError) as e:
             call()

@@ -46,7 +46,7 @@ def test_gradient_arguments():
         return B.lib().sparseloco_embedding_grad(g, gt, ids, rows, vocab, d, scale, ignore, table, tt, acc, ws, n, None)
 
     for bad in (dict(g=None), dict(ids=None), dict(table=None), dict(ws=None), dict(gt=2), dict(tt=7), dict(rows=-1), dict(vocab=0),
-                dict(vocab=327681), dict(d=0), dict(scale=float("nan")), dict(n=size(4, 5, 8) - 1)):
+                dict(vocab=2 ** 21 - 1), dict(d=0), dict(scale=float("nan")), dict(n=size(4, 5, 8) - 1)):
         assert call(**bad) == B.SPLC_EINVAL, bad
     for bad in (dict(g=ctypes.c_void_p(4098)), dict(table=ctypes.c_void_p(4097), tt=1), dict(ids=ctypes.c_void_p(4098)),
                 dict(ws=ctypes.c_void_p(4100))):
