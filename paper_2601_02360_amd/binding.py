@@ -333,6 +333,7 @@ class Plan:
         self.kappa = int(kappa)
         self.quant = bool(quant)
         self._num_chunks = int(lib().sparseloco_plan_num_chunks(self._h))
+        self._num_flat_chunks = int(lib().sparseloco_plan_num_flat_chunks(self._h))
         self._temps = []           # bindings made on the fly by the convenience wrappers below
 
     def close(self):
@@ -387,7 +388,9 @@ class Plan:
 
     @property
     def num_flat_chunks(self) -> int:
-        return int(lib().sparseloco_plan_num_flat_chunks(self._h))
+        if not self._h.value:                    # closed
+            return int(lib().sparseloco_plan_num_flat_chunks(self._h))
+        return self._num_flat_chunks
 
     def adamw_8bit_buffers(self, device="cuda"):
         """(m, m_scale, v, v_scale) of sparseloco_adamw_step_8bit before the first step."""
@@ -693,6 +696,10 @@ def sparseloco_grad_norm(plan: Plan, grads, norm_out: torch.Tensor, ws: torch.Te
                          replica: int = 0, stream=None) -> None:
     """norm_out[0] = 2-norm of all gradients, norm_out[1] = the factor that clips it to max_norm (NaN where the norm is not
     finite).  grads: a Tensors binding or a list of tensors, fp32 or bf16; ws: grad_norm_workspace()."""
+    if type(grads) is Tensors:
+        rc = _native().grad_norm(plan._h.value, grads._h.value, replica, max_norm, norm_out, ws, _given(stream))
+        if _done(rc, "sparseloco_grad_norm"):
+            return
     _check_flat([(norm_out, 2, torch.float32, "norm_out"), (ws, SPLC_NORM_WS_BYTES, torch.uint8, "ws")])
     rc = lib().sparseloco_grad_norm(plan.handle, _h(plan._tensors(grads, _dtype_of(grads), stream)), int(replica),
                                     float(max_norm), norm_out.data_ptr(), ws.data_ptr(), _stream(stream))
@@ -715,6 +722,13 @@ def sparseloco_adamw_step(plan: Plan, theta, grads, m, v, *, lr: float, step: in
     """One AdamW step over all tensors, theta, m and v (fp32) in place.  Bindings, or lists bound on the fly; grads fp32 or
     bf16.  grad_scale: one fp32 element on the GPU, the factor on the gradients (norm_out[1:] of sparseloco_grad_norm); if it
     is not finite nothing changes.  decay: per tensor a factor on weight_decay.  theta_bf16: receives a bf16 copy."""
+    if (type(theta) is Tensors and type(grads) is Tensors and type(m) is Tensors and type(v) is Tensors
+            and (theta_bf16 is None or type(theta_bf16) is Tensors)):
+        rc = _native().adamw_step(plan._h.value, theta._h.value, grads._h.value, m._h.value, v._h.value, replica, lr, beta1,
+                                  beta2, eps, weight_decay, step, grad_scale, len(plan.numels), decay,
+                                  None if theta_bf16 is None else theta_bf16._h.value, _given(stream))
+        if _done(rc, "sparseloco_adamw_step"):
+            return
     _check_flat(_check_step(plan, grad_scale, decay))
     how = _AdamW(lr, beta1, beta2, eps, weight_decay, step)
     rc = lib().sparseloco_adamw_step(plan.handle, _h(plan._tensors(theta, stream=stream)),
@@ -731,6 +745,12 @@ def sparseloco_adamw_step_8bit(plan: Plan, theta, grads, m: torch.Tensor, m_scal
                                decay: Optional[torch.Tensor] = None, theta_bf16=None, replica: int = 0, stream=None) -> None:
     """sparseloco_adamw_step with the moments in 8 bits: m, m_scale, v, v_scale as plan.adamw_8bit_buffers() makes them
     (float8_e4m3fn and one fp32 scale per 256 elements, m = scale * value, sqrt(v) = scale * value), in place."""
+    if type(theta) is Tensors and type(grads) is Tensors and (theta_bf16 is None or type(theta_bf16) is Tensors):
+        rc = _native().adamw_step_8bit(plan._h.value, theta._h.value, grads._h.value, replica, plan._num_flat_chunks, m, m_scale,
+                                       v, v_scale, lr, beta1, beta2, eps, weight_decay, step, grad_scale, len(plan.numels), decay,
+                                       None if theta_bf16 is None else theta_bf16._h.value, _given(stream))
+        if _done(rc, "sparseloco_adamw_step_8bit"):
+            return
     n = plan.num_flat_chunks
     codes, scales = n * SPLC_CHUNK, n * (SPLC_CHUNK // 256)
     _check_flat([(m, codes, torch.float8_e4m3fn, "m"), (m_scale, scales, torch.float32, "m_scale"),
@@ -766,6 +786,9 @@ def sparseloco_embedding_lookup(table: torch.Tensor, token_ids: torch.Tensor, ou
                                 scale: float = 1.0, stream=None) -> None:
     """out[r] = scale * (table[token_ids[r]] + t_perp[token_ids[r]]) + pos_embed[r % len(pos_embed)].  table, t_perp: [vocab, d],
     pos_embed: [seq_len, d], all fp32 or all bf16; token_ids: [rows] int32, clamped into the table; out: [rows, d] fp32 or bf16."""
+    if _done(_native().embedding_lookup(table, token_ids, out, t_perp, pos_embed, scale, _given(stream)),
+             "sparseloco_embedding_lookup"):
+        return
     rows, vocab, d, out_type, table_type = _check_embedding(out, table, token_ids, "out")
     specs = [] if t_perp is None else [(t_perp, (vocab, d), "t_perp", table.dtype)]
     if pos_embed is not None:
@@ -792,6 +815,9 @@ def sparseloco_embedding_grad(grad_out: torch.Tensor, token_ids: torch.Tensor, g
                               scale: float = 1.0, ignore_id: int = -1, accumulate: bool = False, stream=None) -> None:
     """grad_table[x] = scale * sum of grad_out[r] over token_ids[r] == x, added to what is there with accumulate.  grad_out:
     [rows, d], grad_table: [vocab, d], fp32 or bf16 each; ws: embedding_grad_workspace(rows or more, vocab, d)."""
+    if _done(_native().embedding_grad(grad_out, token_ids, grad_table, ws, scale, ignore_id, 1 if accumulate else 0,
+                                      _given(stream)), "sparseloco_embedding_grad"):
+        return
     rows, vocab, d, grad_type, table_type = _check_embedding(grad_out, grad_table, token_ids, "grad_out")
     if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.dim() != 1:
         raise ValueError("ws: must be a contiguous uint8 tensor")

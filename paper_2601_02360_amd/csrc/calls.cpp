@@ -50,6 +50,12 @@ struct Args {
         ok = false;
         return 0.f;
     }
+    double real() {
+        PyObject* o = next();
+        if (PyFloat_CheckExact(o)) return PyFloat_AS_DOUBLE(o);
+        ok = false;
+        return 0.0;
+    }
     // A contiguous GPU tensor of this type; what it is otherwise is left to Python.
     const at::Tensor* tensor(at::ScalarType type) {
         PyObject* o = next();
@@ -62,6 +68,20 @@ struct Args {
         const at::Tensor* t = tensor(type);
         if (!t || t->numel() != numel) { ok = false; return nullptr; }
         return t->data_ptr();
+    }
+    void* flat_or_none(at::ScalarType type, int64_t numel) { return none() ? nullptr : flat(type, numel); }
+    // A contiguous GPU matrix of fp32 or bf16 elements, of the shape given as below; its type as SPLC_F32 or SPLC_BF16.
+    void* float_matrix(int64_t& rows, int64_t& cols, int& dtype) {
+        PyObject* o = next();
+        if (!ok || !THPVariable_CheckExact(o)) { ok = false; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        const at::ScalarType type = t.scalar_type();
+        if ((type != at::kFloat && type != at::kBFloat16) || !t.is_cuda() || !t.is_contiguous() || t.dim() != 2) { ok = false; return nullptr; }
+        dtype = type == at::kFloat ? SPLC_F32 : SPLC_BF16;
+        if (rows < 0) rows = t.size(0);
+        if (cols < 0) cols = t.size(1);
+        if (t.size(0) != rows || t.size(1) != cols) { ok = false; return nullptr; }
+        return t.data_ptr();
     }
     // A matrix; rows, cols < 0: whatever they are, and they are written back.
     float* matrix(int64_t& rows, int64_t& cols, at::ScalarType type = at::kFloat) {
@@ -233,6 +253,120 @@ PyObject* reproject(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        const auto* plan = a.handle<sparseloco_plan>();
+        const auto* grads = a.handle<sparseloco_tensors>();
+        const int replica = a.integer();
+        const float max_norm = a.number();
+        auto* out = static_cast<float*>(a.flat(at::kFloat, 2));
+        void* ws = a.flat(at::kByte, SPLC_NORM_WS_BYTES);
+        void* stream = a.stream();
+        return finish(a, [&] { return sparseloco_grad_norm(plan, grads, replica, max_norm, out, ws, stream); });
+    });
+}
+
+// The arguments that both forms of the step end with: the step's numbers, the factor and the decays (of `tensors` tensors), the copy.
+struct Step {
+    sparseloco_adamw how;
+    const float *grad_scale, *decay;
+    const sparseloco_tensors* copy;
+};
+Step step_of(Args& a) {
+    Step s;
+    s.how.lr = a.real();
+    s.how.beta1 = a.real();
+    s.how.beta2 = a.real();
+    s.how.eps = a.real();
+    s.how.weight_decay = a.real();
+    s.how.step = a.integer(INT64_MIN, INT64_MAX);
+    s.grad_scale = static_cast<const float*>(a.flat_or_none(at::kFloat, 1));
+    const int64_t tensors = a.integer(0, INT_MAX);
+    s.decay = static_cast<const float*>(a.flat_or_none(at::kFloat, tensors));
+    s.copy = a.handle<sparseloco_tensors>();
+    return s;
+}
+
+PyObject* adamw_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        const auto* plan = a.handle<sparseloco_plan>();
+        const auto *theta = a.handle<sparseloco_tensors>(), *grads = a.handle<sparseloco_tensors>(),
+                   *m = a.handle<sparseloco_tensors>(), *v = a.handle<sparseloco_tensors>();
+        const int replica = a.integer();
+        const Step s = step_of(a);
+        void* stream = a.stream();
+        return finish(a, [&] {
+            return sparseloco_adamw_step(plan, theta, grads, m, v, replica, &s.how, s.grad_scale, s.decay, s.copy, stream);
+        });
+    });
+}
+
+PyObject* adamw_step_8bit(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        const auto* plan = a.handle<sparseloco_plan>();
+        const auto *theta = a.handle<sparseloco_tensors>(), *grads = a.handle<sparseloco_tensors>();
+        const int replica = a.integer();
+        const int64_t chunks = a.integer(0, INT_MAX), codes = chunks * SPLC_CHUNK, scales = chunks * (SPLC_CHUNK / 256);
+        auto* m = static_cast<uint8_t*>(a.flat(at::kFloat8_e4m3fn, codes));
+        auto* m_scale = static_cast<float*>(a.flat(at::kFloat, scales));
+        auto* v = static_cast<uint8_t*>(a.flat(at::kFloat8_e4m3fn, codes));
+        auto* v_scale = static_cast<float*>(a.flat(at::kFloat, scales));
+        const Step s = step_of(a);
+        void* stream = a.stream();
+        return finish(a, [&] {
+            return sparseloco_adamw_step_8bit(plan, theta, grads, replica, m, m_scale, v, v_scale, &s.how, s.grad_scale, s.decay,
+                                              s.copy, stream);
+        });
+    });
+}
+
+PyObject* embedding_lookup(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        int64_t rows = -1, vocab = -1, d = -1, seq = -1;
+        int in = 0, other = 0, result = 0;
+        const void* table = a.float_matrix(vocab, d, in);
+        const auto* ids = a.tensor(at::kInt);
+        void* out = a.float_matrix(rows, d, result);
+        if (!ids || ids->dim() != 1 || ids->size(0) != rows) a.ok = false;
+        const void *t_perp = nullptr, *pos = nullptr;
+        if (!a.none()) {
+            t_perp = a.float_matrix(vocab, d, other);
+            if (other != in) a.ok = false;
+        }
+        if (!a.none()) {
+            pos = a.float_matrix(seq, d, other);
+            if (other != in || seq < 1) a.ok = false;
+        }
+        const float scale = a.number();
+        void* stream = a.stream();
+        if (vocab > INT_MAX || d > INT_MAX || seq > INT_MAX) a.ok = false;
+        return finish(a, [&] {
+            return sparseloco_embedding_lookup(table, t_perp, in, static_cast<const int32_t*>(ids->data_ptr()), (int)vocab, pos,
+                                               (int)(pos ? seq : 0), scale, out, result, rows, (int)d, stream);
+        });
+    });
+}
+
+PyObject* embedding_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        int64_t rows = -1, vocab = -1, d = -1;
+        int gradient = 0, result = 0;
+        const void* grad = a.float_matrix(rows, d, gradient);
+        const auto* ids = a.tensor(at::kInt);
+        void* table = a.float_matrix(vocab, d, result);
+        const auto* ws = a.tensor(at::kByte);
+        if (!ids || ids->dim() != 1 || ids->size(0) != rows || !ws || ws->dim() != 1) a.ok = false;
+        const float scale = a.number();
+        const int ignore = (int)a.integer(INT_MIN, INT_MAX), accumulate = a.integer();
+        void* stream = a.stream();
+        if (vocab > INT_MAX || d > INT_MAX) a.ok = false;
+        return finish(a, [&] {
+            return sparseloco_embedding_grad(grad, gradient, static_cast<const int32_t*>(ids->data_ptr()), rows, (int)vocab, (int)d,
+                                             scale, ignore, table, result, accumulate, ws->data_ptr(), ws->numel(), stream);
+        });
+    });
+}
+
 using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
 PyCFunction method(Fast f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
@@ -248,6 +382,11 @@ PyMODINIT_FUNC PyInit__calls() {
         {"project", method(boundary<true>), METH_FASTCALL, nullptr},
         {"reconstruct", method(boundary<false>), METH_FASTCALL, nullptr},
         {"reproject", method(reproject), METH_FASTCALL, nullptr},
+        {"grad_norm", method(grad_norm), METH_FASTCALL, nullptr},
+        {"adamw_step", method(adamw_step), METH_FASTCALL, nullptr},
+        {"adamw_step_8bit", method(adamw_step_8bit), METH_FASTCALL, nullptr},
+        {"embedding_lookup", method(embedding_lookup), METH_FASTCALL, nullptr},
+        {"embedding_grad", method(embedding_grad), METH_FASTCALL, nullptr},
         {nullptr, nullptr, 0, nullptr}};
     static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
     return PyModule_Create(&module);
