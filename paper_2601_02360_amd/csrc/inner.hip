@@ -9,6 +9,7 @@
 
 #include <cmath>
 
+#include "launch_rules.h"
 #include "plan.h"
 #include "sparseloco.h"
 
@@ -21,12 +22,6 @@ constexpr int kNormGroups = SPLC_NORM_WS_BYTES / 8;
 
 typedef __bf16 vbf16x2 __attribute__((ext_vector_type(2)));
 
-// Elements of a chunk's vector at `first` that are present.
-template <bool WHOLE>
-__device__ __forceinline__ uint32_t present(const ChunkDesc& d, uint32_t first) {
-    if constexpr (WHOLE) return 4;
-    return d.n_c > first ? (d.n_c - first < 4u ? d.n_c - first : 4u) : 0u;
-}
 __device__ __forceinline__ float4 widened(float4 v) { return v; }
 __device__ __forceinline__ float4 widened(uint2 v) {
     return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
@@ -34,26 +29,39 @@ __device__ __forceinline__ float4 widened(uint2 v) {
 }
 __device__ __forceinline__ float widened(float v) { return v; }
 __device__ __forceinline__ float widened(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-// The first n of four elements at p, +0 for the others.
+
+// Which of a vector's four elements are present: those from `from` to `to`.  WHOLE: all.
+struct Present {
+    uint32_t from, to;
+    __device__ __forceinline__ bool all() const { return from == 0 && to == 4; }
+    __device__ __forceinline__ bool has(uint32_t j) const { return from <= j && j < to; }
+};
+// Of the vector at place `at`, where the places lo .. hi - 1 hold elements.
+__device__ __forceinline__ Present present(uint32_t at, uint32_t lo, uint32_t hi) {
+    return {lo > at ? (lo - at < 4u ? lo - at : 4u) : 0u, hi > at ? (hi - at < 4u ? hi - at : 4u) : 0u};
+}
+// Four elements at p, +0 for those that are not present.
 template <bool WHOLE, class T>
-__device__ __forceinline__ float4 load_present(const T* p, uint32_t n) {
+__device__ __forceinline__ float4 load_present(const T* p, Present n) {
     if (WHOLE) return widened(stream_load4(p));
-    if (n == 4) return widened(cached_load4(p));
+    if (n.all()) return widened(cached_load4(p));
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (n > 0) v.x = widened(p[0]);
-    if (n > 1) v.y = widened(p[1]);
-    if (n > 2) v.z = widened(p[2]);
+    if (n.has(0)) v.x = widened(p[0]);
+    if (n.has(1)) v.y = widened(p[1]);
+    if (n.has(2)) v.z = widened(p[2]);
+    if (n.has(3)) v.w = widened(p[3]);
     return v;
 }
 template <bool WHOLE>
-__device__ __forceinline__ void store_present(float* p, uint32_t n, float4 v) {
-    if (WHOLE || n == 4) {
+__device__ __forceinline__ void store_present(float* p, Present n, float4 v) {
+    if (WHOLE || n.all()) {
         stream_store4(p, v);
         return;
     }
-    if (n > 0) p[0] = v.x;
-    if (n > 1) p[1] = v.y;
-    if (n > 2) p[2] = v.z;
+    if (n.has(0)) p[0] = v.x;
+    if (n.has(1)) p[1] = v.y;
+    if (n.has(2)) p[2] = v.z;
+    if (n.has(3)) p[3] = v.w;
 }
 // Rounded to nearest, ties to even.
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
@@ -61,16 +69,17 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     return __builtin_bit_cast(uint32_t, v);
 }
 template <bool WHOLE>
-__device__ __forceinline__ void store_present(uint16_t* p, uint32_t n, float4 v) {
+__device__ __forceinline__ void store_present(uint16_t* p, Present n, float4 v) {
     const uint32_t lo = bf16_pair(v.x, v.y), hi = bf16_pair(v.z, v.w);
-    if (WHOLE || n == 4) {
+    if (WHOLE || n.all()) {
         const vuint2 t = {lo, hi};
         __builtin_nontemporal_store(t, (SPLC_GLOBAL vuint2*)p);
         return;
     }
-    if (n > 0) p[0] = (uint16_t)lo;
-    if (n > 1) p[1] = (uint16_t)(lo >> 16);
-    if (n > 2) p[2] = (uint16_t)hi;
+    if (n.has(0)) p[0] = (uint16_t)lo;
+    if (n.has(1)) p[1] = (uint16_t)(lo >> 16);
+    if (n.has(2)) p[2] = (uint16_t)hi;
+    if (n.has(3)) p[3] = (uint16_t)(hi >> 16);
 }
 
 // ---------------------------------------------------------------- norm
@@ -100,11 +109,11 @@ __global__ __launch_bounds__(kThreads) void norm_partial_kernel(const ChunkDesc*
         float4 x[4];
         if (d.n_c == kChunk) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) x[s] = load_present<true>(g + s * 1024 + tid * 4, 4);
+            for (int s = 0; s < 4; ++s) x[s] = load_present<true>(g + s * 1024 + tid * 4, {0, 4});
         } else {
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                x[s] = load_present<false>(g + s * 1024 + tid * 4, present<false>(d, (uint32_t)s * 1024 + tid * 4));
+                x[s] = load_present<false>(g + s * 1024 + tid * 4, present((uint32_t)s * 1024 + tid * 4, 0, d.n_c));
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -159,39 +168,24 @@ __device__ __forceinline__ bool gradient_factor(const float* grad_scale, float& 
     return factor - factor == 0.f;
 }
 
-template <bool WHOLE, class G>
-__device__ __forceinline__ void adamw_body(const ChunkDesc& d, float* theta, const G* grad, float* m, float* v, uint16_t* copy,
-                                           const StepNumbers& numbers, float factor, float keep) {
-    const uint32_t tid = threadIdx.x;
-    float4 t4[4], g4[4], m4[4], v4[4];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        const uint32_t at = (uint32_t)s * 1024 + tid * 4, n = present<WHOLE>(d, at);
-        g4[s] = load_present<WHOLE>(grad + at, n);
-        m4[s] = load_present<WHOLE>(m + at, n);
-        v4[s] = load_present<WHOLE>(v + at, n);
-        t4[s] = load_present<WHOLE>(theta + at, n);
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        const uint32_t at = (uint32_t)s * 1024 + tid * 4, n = present<WHOLE>(d, at);
-        auto one = [&](float& th, float g, float& mm, float& vv) {
-            moments(numbers, factor * g, mm, vv);
-            th = stepped(numbers, keep, th, mm, sqrtf(vv));
-        };
-        one(t4[s].x, g4[s].x, m4[s].x, v4[s].x);
-        one(t4[s].y, g4[s].y, m4[s].y, v4[s].y);
-        one(t4[s].z, g4[s].z, m4[s].z, v4[s].z);
-        one(t4[s].w, g4[s].w, m4[s].w, v4[s].w);
-        store_present<WHOLE>(m + at, n, m4[s]);
-        store_present<WHOLE>(v + at, n, v4[s]);
-        store_present<WHOLE>(theta + at, n, t4[s]);
-        if (copy) store_present<WHOLE>(copy + at, n, t4[s]);
-    }
+// Four elements.
+__device__ __forceinline__ void adamw4(const StepNumbers& n, float keep, float factor, float4 g, float4& t, float4& m, float4& v) {
+    auto one = [&](float& th, float gradient, float& mm, float& vv) {
+        moments(n, factor * gradient, mm, vv);
+        th = stepped(n, keep, th, mm, sqrtf(vv));
+    };
+    one(t.x, g.x, m.x, v.x);
+    one(t.y, g.y, m.y, v.y);
+    one(t.z, g.z, m.z, v.z);
+    one(t.w, g.w, m.w, v.w);
 }
 
+// A workgroup's elements begin where theta has a multiple of 256 bytes, up to 63 elements before its chunk, and end as many
+// before the next one's; the first of a tensor begins with it, and the last ends with it, up to 63 elements beyond 4096.  With
+// tensors packed into flat buffers, the usual case of others than aligned ones, that holds for all arrays.  (0.9B parameters
+// packed at multiples of eight bytes, bf16 gradients and copy: 5.16 ms with chunks as they lie, 4.57 so.)
 template <class G>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const ChunkDesc* __restrict__ chunks, uint32_t n_gen,
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const ChunkDesc* __restrict__ chunks, const int64_t* __restrict__ numel,
                                                          float* const* __restrict__ theta_tab,
                                                          const G* const* __restrict__ grad_tab,
                                                          float* const* __restrict__ m_tab, float* const* __restrict__ v_tab,
@@ -202,11 +196,48 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const ChunkDesc* __rest
     float factor;
     if (!gradient_factor(grad_scale, factor)) return;
     const float keep = 1.f - (decay ? numbers.shrink * decay[d.tensor] : numbers.shrink);
-    float *theta = theta_tab[d.tensor] + d.offset, *m = m_tab[d.tensor] + d.offset, *v = v_tab[d.tensor] + d.offset;
-    const G* grad = grad_tab[d.tensor] + d.offset;
-    uint16_t* copy = copy_tab ? copy_tab[d.tensor] + d.offset : nullptr;
-    if (blockIdx.x >= n_gen) adamw_body<true>(d, theta, grad, m, v, copy, numbers, factor, keep);
-    else adamw_body<false>(d, theta, grad, m, v, copy, numbers, factor, keep);
+    const uint32_t tid = threadIdx.x;
+    float* theta = theta_tab[d.tensor];
+    const uint32_t lead = (uint32_t)(reinterpret_cast<uintptr_t>(theta) / 4) & 63u;
+    const bool first = d.offset == 0, last = (int64_t)d.offset + d.n_c == numel[d.tensor];
+    const int64_t from = (int64_t)d.offset - lead;           // element at place 0
+    theta += from;
+    float *m = m_tab[d.tensor] + from, *v = v_tab[d.tensor] + from;
+    const G* grad = grad_tab[d.tensor] + from;
+    uint16_t* copy = copy_tab ? copy_tab[d.tensor] + from : nullptr;
+    if (d.n_c == kChunk && (lead == 0 || !(first || last))) {
+        float4 t4[4], g4[4], m4[4], v4[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const uint32_t at = (uint32_t)s * 1024 + tid * 4;
+            g4[s] = widened(stream_load4(grad + at));
+            m4[s] = stream_load4(m + at);
+            v4[s] = stream_load4(v + at);
+            t4[s] = stream_load4(theta + at);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const uint32_t at = (uint32_t)s * 1024 + tid * 4;
+            adamw4(numbers, keep, factor, g4[s], t4[s], m4[s], v4[s]);
+            stream_store4(m + at, m4[s]);
+            stream_store4(v + at, v4[s]);
+            stream_store4(theta + at, t4[s]);
+            if (copy) store_present<true>(copy + at, {0, 4}, t4[s]);
+        }
+        return;
+    }
+    const uint32_t lo = first ? lead : 0, hi = last ? d.n_c + lead : (uint32_t)kChunk;
+    for (uint32_t at = tid * 4; at < hi; at += 1024) {
+        const Present n = present(at, lo, hi);
+        if (n.from >= n.to) continue;
+        float4 g4 = load_present<false>(grad + at, n), m4 = load_present<false>(m + at, n), v4 = load_present<false>(v + at, n),
+               t4 = load_present<false>(theta + at, n);
+        adamw4(numbers, keep, factor, g4, t4, m4, v4);
+        store_present<false>(m + at, n, m4);
+        store_present<false>(v + at, n, v4);
+        store_present<false>(theta + at, n, t4);
+        if (copy) store_present<false>(copy + at, n, t4);
+    }
 }
 
 // ---------------------------------------------------------------- AdamW, moments in 8 bits
@@ -261,7 +292,8 @@ __device__ __forceinline__ void adamw_8bit_body(const ChunkDesc& d, float* theta
     float ms[4], vs[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-        const uint32_t at = (uint32_t)s * 1024 + tid * 4, n = present<WHOLE>(d, at);
+        const uint32_t at = (uint32_t)s * 1024 + tid * 4;
+        const Present n = present(at, 0, d.n_c);
         g4[s] = load_present<WHOLE>(grad + at, n);
         mc[s] = __builtin_nontemporal_load((SPLC_GLOBAL uint32_t*)(m_codes + s * 256 + tid));
         vc[s] = __builtin_nontemporal_load((SPLC_GLOBAL uint32_t*)(v_codes + s * 256 + tid));
@@ -271,9 +303,10 @@ __device__ __forceinline__ void adamw_8bit_body(const ChunkDesc& d, float* theta
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-        const uint32_t at = (uint32_t)s * 1024 + tid * 4, n = present<WHOLE>(d, at);
+        const uint32_t at = (uint32_t)s * 1024 + tid * 4;
+        const Present n = present(at, 0, d.n_c);
         if (!WHOLE) {                                         // what lies behind a tensor's end counts as zero
-            const uint32_t mask = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+            const uint32_t mask = n.to == 4 ? 0xFFFFFFFFu : (1u << (8 * n.to)) - 1u;
             mc[s] &= mask;
             vc[s] &= mask;
         }
@@ -318,7 +351,7 @@ __device__ __forceinline__ void adamw_8bit_body(const ChunkDesc& d, float* theta
 }
 
 template <class G>
-__global__ __launch_bounds__(kThreads) void adamw_8bit_kernel(const ChunkDesc* __restrict__ chunks, uint32_t n_gen,
+__global__ __launch_bounds__(kThreads) void adamw_8bit_kernel(const ChunkDesc* __restrict__ chunks,
                                                               float* const* __restrict__ theta_tab,
                                                               const G* const* __restrict__ grad_tab,
                                                               uint8_t* __restrict__ m_codes, float* __restrict__ m_scale,
@@ -336,7 +369,7 @@ __global__ __launch_bounds__(kThreads) void adamw_8bit_kernel(const ChunkDesc* _
     const uint64_t chunk = d.id;
     uint32_t *mc = reinterpret_cast<uint32_t*>(m_codes + chunk * kChunk), *vc = reinterpret_cast<uint32_t*>(v_codes + chunk * kChunk);
     float *ms = m_scale + chunk * 16, *vs = v_scale + chunk * 16;
-    if (blockIdx.x >= n_gen) adamw_8bit_body<true>(d, theta, grad, mc, ms, vc, vs, copy, numbers, now, factor, keep);
+    if (d.n_c == kChunk) adamw_8bit_body<true>(d, theta, grad, mc, ms, vc, vs, copy, numbers, now, factor, keep);
     else adamw_8bit_body<false>(d, theta, grad, mc, ms, vc, vs, copy, numbers, now, factor, keep);
 }
 
@@ -418,8 +451,9 @@ int sparseloco_adamw_step(const sparseloco_plan* plan, const sparseloco_tensors*
     }
     if (plan->n_update == 0) return SPLC_OK;
     auto launch = [&](auto kernel, auto grad_tab) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)plan->n_update), dim3(kThreads), 0, static_cast<hipStream_t>(stream),
-                           plan->d_update, (uint32_t)plan->n_update_gen, set_table<float*>(theta, replica), grad_tab,
+        hipLaunchKernelGGL(kernel, dim3((unsigned)plan->n_update), dim3(kThreads),
+                           plan->n_update >= splc::kFewStreamsAdamw ? reserve_lds(1, 0) : 0u, static_cast<hipStream_t>(stream),
+                           plan->d_update, plan->d_numel, set_table<float*>(theta, replica), grad_tab,
                            set_table<float*>(m, replica), set_table<float*>(v, replica),
                            theta_bf16 ? set_table<uint16_t*>(theta_bf16, replica) : nullptr, numbers, grad_scale, decay);
     };
@@ -440,8 +474,9 @@ int sparseloco_adamw_step_8bit(const sparseloco_plan* plan, const sparseloco_ten
     if (!aligned(m, 4) || !aligned(m_scale, 4) || !aligned(v, 4) || !aligned(v_scale, 4)) return SPLC_EALIGN;
     const uint32_t now = (uint32_t)how->step * kTimeStep;
     auto launch = [&](auto kernel, auto grad_tab) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)plan->n_update), dim3(kThreads), 0, static_cast<hipStream_t>(stream),
-                           plan->d_update, (uint32_t)plan->n_update_gen, set_table<float*>(theta, replica), grad_tab, m, m_scale,
+        hipLaunchKernelGGL(kernel, dim3((unsigned)plan->n_update), dim3(kThreads),
+                           reserve_lds(splc::kAdamw8GroupsPerUnit, 0), static_cast<hipStream_t>(stream),
+                           plan->d_update, set_table<float*>(theta, replica), grad_tab, m, m_scale,
                            v, v_scale, theta_bf16 ? set_table<uint16_t*>(theta_bf16, replica) : nullptr, numbers, now,
                            grad_scale, decay);
     };

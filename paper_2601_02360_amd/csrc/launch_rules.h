@@ -246,7 +246,13 @@ constexpr bool strips_pay(int64_t strips, int kappa, bool params) { return kappa
 //   one-launch step: 37,105 chunks (150M parameters), kappa 32, 8 replicas: 2862 -> 2833, 2: 832 -> 799; 8192, 8: 625 ->
 //     601, 2: 179 -> 179; 2000, 2: 48.4 -> 51.6;
 //   outer update, two per unit: 228,000 chunks (0.9B model): 1866 -> 1803, 120,000: 959 -> 945; 24,000 to 37,105: the same.
-constexpr int64_t kFewStreams = 8192, kFewStreamsUpdate = 24000;
+//   AdamW, fp32 moments, one per unit: 32,768 chunks, bf16 gradients and copy / fp32: 668 -> 649 / 647 -> 647, 50,000: 1002 -> 987 /
+//     996 -> 990, 100,000: 2046 -> 2022 / 2011 -> 1989, 217,000: 4573 -> 4423 / 4560 -> 4385; two per unit the same as without a limit;
+//     16,384 and 24,000: 321 -> 322 / 322 -> 316, 477 -> 475 / 465 -> 464; 1024: 22.2 -> 24.0;
+//   AdamW, moments in 8 bits, four per unit (six fit): 1024 chunks 15.6 -> 15.6, 8192: 96 -> 92.5 ... 98, 32,768: 390 -> 363, 100,000:
+//     1184 -> 1136; three per unit: 217,000 chunks 2525 -> 2644, four 2467.
+constexpr int64_t kFewStreams = 8192, kFewStreamsUpdate = 24000, kFewStreamsAdamw = 32768;
+constexpr int kAdamw8GroupsPerUnit = 4;
 constexpr bool few_streams(int64_t chunks, int kappa, bool from_params, bool general_path) {
     return chunks >= kFewStreams && kappa <= 128 && from_params && !general_path;
 }

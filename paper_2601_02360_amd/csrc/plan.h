@@ -83,7 +83,7 @@ struct sparseloco_plan {
     // The compression of a large tiled plan takes complete tiles four at a time where four lie side by side ("strips", one
     // entry each: origin, stride and chunk number of the first tile); only the other chunks are in the table above.  Its
     // outer update, which is element-wise, walks the tensors as flat chunks (a table of its own).
-    // One device allocation holds [chunks | strips | flat chunks of the update | every chunk one by one].
+    // One device allocation holds [chunks | strips | flat chunks of the update | every chunk one by one | numel].
     splc::ChunkDesc* d_chunks = nullptr;
     splc::ChunkDesc* h_chunks = nullptr; // pinned source of the asynchronous upload, kept until destroy
     int64_t n_entries = 0;               // entries of the chunk table (= n_chunks unless there are strips)
@@ -94,6 +94,7 @@ struct sparseloco_plan {
     int64_t n_update = 0, n_update_gen = 0;
     splc::ChunkDesc* d_all = nullptr;    // every chunk one by one, for all other kernels (= d_chunks without strips)
     int64_t n_all_gen = 0;
+    int64_t* d_numel = nullptr;          // elements of each tensor
 };
 
 // n_sets lists of n_tensors device pointers, set-major, resident on the device.
@@ -128,6 +129,13 @@ inline int check_tensors(const sparseloco_plan* plan, const sparseloco_tensors* 
 template <class T>
 T const* set_table(const sparseloco_tensors* t, int set) {
     return reinterpret_cast<T const*>(t->d_table + (size_t)(t->n_sets == 1 ? 0 : set) * (size_t)t->n_tensors);
+}
+
+// LDS that a launch reserves so that only `groups_per_unit` of its workgroups, which use `used` bytes
+// each, fit on a compute unit.  LDS is handed out in 1280-byte units.
+inline unsigned reserve_lds(int groups_per_unit, size_t used) {
+    const size_t share = 160 * 1024 / (size_t)groups_per_unit / 1280 * 1280;
+    return used < share ? (unsigned)(share - used) : 0u;
 }
 
 }  // namespace splc

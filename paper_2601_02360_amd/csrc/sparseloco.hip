@@ -1496,12 +1496,6 @@ bool on_small_plan_disjoint(const sparseloco_plan* plan, Collect collect) {
     }
 }
 
-// LDS that a launch on a large plan reserves so that only `groups_per_unit` of its workgroups, which use `used` bytes
-// each, fit on a compute unit (splc::few_streams).  LDS is handed out in 1280-byte units.
-unsigned reserve_lds(int groups_per_unit, size_t used) {
-    const size_t share = 160 * 1024 / (size_t)groups_per_unit / 1280 * 1280;
-    return used < share ? (unsigned)(share - used) : 0u;
-}
 unsigned reserve_lds_compress(const sparseloco_plan* plan, int64_t entries, bool from_params, size_t used) {
     return splc::few_streams(entries, plan->kappa, from_params, plan->select == SPLC_SELECT_RADIX) ? reserve_lds(3, used) : 0u;
 }
@@ -1823,11 +1817,11 @@ int plan_build(sparseloco_plan** out, int n_tensors, const int64_t* rows, const 
     plan->n_update = tiled ? (int64_t)t.update.size() : plan->n_entries;
     plan->n_update_gen = tiled ? count_class0(t.update) : plan->n_gen;
     plan->n_all_gen = count_class0(t.all);
-    // device layout: [main table | strips | update table (tiled) | every chunk (with strips)]
+    // device layout: [main table | strips | update table (tiled) | every chunk (with strips) | numel]
     const size_t n_main = main_table.size(), n_str = t.strips.size(), n_upd = tiled ? t.update.size() : 0,
                  n_all = with_strips ? t.all.size() : 0, total = n_main + n_str + n_upd + n_all;
     if (total > 0) {
-        const size_t bytes = total * sizeof(ChunkDesc);
+        const size_t bytes = total * sizeof(ChunkDesc) + plan->numel.size() * sizeof(int64_t);
         if (hipHostMalloc(reinterpret_cast<void**>(&plan->h_chunks), bytes, hipHostMallocDefault) != hipSuccess ||
             hipMalloc(reinterpret_cast<void**>(&plan->d_chunks), bytes) != hipSuccess) {
             rc = SPLC_ENOMEM;
@@ -1836,6 +1830,8 @@ int plan_build(sparseloco_plan** out, int n_tensors, const int64_t* rows, const 
             std::copy(t.strips.begin(), t.strips.end(), plan->h_chunks + n_main);
             if (tiled) std::copy(t.update.begin(), t.update.end(), plan->h_chunks + n_main + n_str);
             if (with_strips) std::copy(t.all.begin(), t.all.end(), plan->h_chunks + n_main + n_str + n_upd);
+            std::copy(plan->numel.begin(), plan->numel.end(), reinterpret_cast<int64_t*>(plan->h_chunks + total));
+            plan->d_numel = reinterpret_cast<int64_t*>(plan->d_chunks + total);
             plan->d_strips = plan->d_chunks + n_main;
             plan->d_update = tiled ? plan->d_chunks + n_main + n_str : plan->d_chunks;
             plan->d_all = with_strips ? plan->d_chunks + n_main + n_str + n_upd : plan->d_chunks;
