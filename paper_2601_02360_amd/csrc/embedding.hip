@@ -60,38 +60,41 @@ __device__ __forceinline__ int row_of(int32_t id, int vocab) { return id < 0 ? 0
 
 // ---------------------------------------------------------------- lookup
 
-constexpr int kLookupSpan = 1024;        // columns a wave takes: four vectors of four a lane
-
+// A wave takes one token in one span of columns.  Workgroups go to the eight XCDs round-robin by number, and spans go with
+// them: with four spans an XCD's L2 is asked for one fourth of every table row and of PosEmbed, and holds four times as many of them.
 template <class T, class O>
 __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table, const T* __restrict__ t_perp,
                                                      const int32_t* __restrict__ ids, int vocab, const T* __restrict__ pos,
-                                                     int seq, float scale, O* __restrict__ out, int64_t rows, int d) {
+                                                     int seq, float scale, O* __restrict__ out, int64_t rows, int d, int spans,
+                                                     int width) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+    const int span = (int)(blockIdx.x % (unsigned)spans);
+    const int64_t row = (int64_t)(blockIdx.x / (unsigned)spans) * 4 + wave;
     if (row >= rows) return;
     const int64_t from = (int64_t)row_of(ids[row], vocab) * d;
-    const int col = (int)blockIdx.y * kLookupSpan + lane * 4;
-    const T* a = table + from;
-    const T* b = t_perp ? t_perp + from : nullptr;
-    const T* p = pos ? pos + (row % seq) * d : nullptr;
-    float4 x[4], y[4], z[4];
+    const T *a = table + from, *b = t_perp ? t_perp + from : nullptr;
+    const T* p = pos ? pos + (int64_t)((uint32_t)row % (uint32_t)seq) * d : nullptr;
+    const int end = (span + 1) * width < d ? (span + 1) * width : d;
+    for (int c = span * width + lane * 4; c < end; c += 512) {
+        float4 x[2], y[2], z[2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int c = col + 256 * k, n = d - c < 4 ? d - c : 4;
-        if (n <= 0) continue;
-        x[k] = load_some(a + c, n);
-        if (b) y[k] = load_some(b + c, n);
-        if (p) z[k] = load_some(p + c, n);
-    }
+        for (int k = 0; k < 2; ++k) {
+            const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
+            if (at >= end) continue;
+            x[k] = load_some(a + at, n);
+            if (b) y[k] = load_some(b + at, n);
+            if (p) z[k] = load_some(p + at, n);
+        }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int c = col + 256 * k, n = d - c < 4 ? d - c : 4;
-        if (n <= 0) continue;
-        float4 v = x[k];
-        if (b) v = make_float4(v.x + y[k].x, v.y + y[k].y, v.z + y[k].z, v.w + y[k].w);
-        v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
-        if (p) v = make_float4(v.x + z[k].x, v.y + z[k].y, v.z + z[k].z, v.w + z[k].w);
-        store_some(out + row * d + c, n, v);
+        for (int k = 0; k < 2; ++k) {
+            const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
+            if (at >= end) continue;
+            float4 v = x[k];
+            if (b) v = make_float4(v.x + y[k].x, v.y + y[k].y, v.z + y[k].z, v.w + y[k].w);
+            v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
+            if (p) v = make_float4(v.x + z[k].x, v.y + z[k].y, v.z + z[k].z, v.w + z[k].w);
+            store_some(out + row * d + at, n, v);
+        }
     }
 }
 
@@ -492,13 +495,16 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
         !aligned(out, out_dtype == SPLC_BF16 ? 2 : 4))
         return SPLC_EALIGN;
     if (rows == 0) return SPLC_OK;
-    const dim3 grid((unsigned)((rows + 3) / 4), (unsigned)((d + kLookupSpan - 1) / kLookupSpan));
+    int spans = 1;                                            // 1, 2 or 4, of whole vectors
+    while (spans < 4 && spans * 256 < d) spans *= 2;
+    const int width = ((d + spans - 1) / spans + 3) / 4 * 4;
+    const int64_t groups = (rows + 3) / 4 * spans;            // (below 2^31)
     auto launch = [&](auto element, auto result) {
         using T = decltype(element);
         using O = decltype(result);
-        hipLaunchKernelGGL((lookup_kernel<T, O>), grid, dim3(256), 0, static_cast<hipStream_t>(stream),
+        hipLaunchKernelGGL((lookup_kernel<T, O>), dim3((unsigned)groups), dim3(256), 0, static_cast<hipStream_t>(stream),
                            static_cast<const T*>(table), static_cast<const T*>(t_perp), token_ids, vocab,
-                           static_cast<const T*>(pos_embed), seq_len, scale, static_cast<O*>(out), rows, d);
+                           static_cast<const T*>(pos_embed), seq_len, scale, static_cast<O*>(out), rows, d, spans, width);
     };
     if (table_dtype == SPLC_F32 && out_dtype == SPLC_F32) launch(float{}, float{});
     else if (table_dtype == SPLC_F32) launch(float{}, uint16_t{});
