@@ -109,6 +109,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
 // do with the memory; rows that have tokens are written again later.
 
 constexpr int kBlock = 2048, kBlockBits = 11, kSortThreads = 1024, kFanIn = 8;
+constexpr int kItems = kBlock / kSortThreads;                // elements of a lane while it sorts
 constexpr uint32_t kNone = 0xFFFFFFFFu, kMaxVocab = (1u << (32 - kBlockBits)) - 1;
 
 // A launch's share of the zeros: 16-byte vectors from `at`, workgroup by workgroup.
@@ -116,7 +117,7 @@ struct Zeros {
     uint4* at;
     uint64_t vectors;
 };
-constexpr int kZeroSpan = 2048;          // vectors a workgroup writes
+constexpr int kZeroSpan = 512;           // vectors a workgroup writes (50304 rows of 768: 26.6 us, 1024: 28.3, 2048: 30.4, 256: 36.7)
 __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group) {
     typedef uint32_t vuint4 __attribute__((ext_vector_type(4)));
     const uint64_t from = (uint64_t)group * kZeroSpan;
@@ -139,19 +140,29 @@ __device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
     else if constexpr (STRIDE == 8) return move(x, integral_constant<int, 0x128>{});     // rows of 16 turned by eight
     else return __shfl_xor(x, STRIDE);
 }
-// One bitonic step on a lane's two elements, y what the elements `stride` apart hold: the smaller one stays if this is the first of
-// a pair that ascends, or the second of one that descends.
-__device__ __forceinline__ void keep(uint32_t (&x)[2], const uint32_t (&y)[2], const uint32_t (&at)[2], uint32_t size, uint32_t stride) {
+// One bitonic step on a lane's elements (numbers first + 64 k), y what the elements `stride` apart hold: the smaller one stays if this
+// is the first of a pair that ascends, or the second of one that descends.
+using Items = uint32_t[kItems];
+__device__ __forceinline__ void keep(Items& x, const Items& y, uint32_t first, uint32_t size, uint32_t stride) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const bool smaller = ((at[k] & size) == 0) == ((at[k] & stride) == 0);
+    for (int k = 0; k < kItems; ++k) {
+        const uint32_t at = first + 64 * k;
+        const bool smaller = ((at & size) == 0) == ((at & stride) == 0);
         x[k] = smaller == (x[k] < y[k]) ? x[k] : y[k];
     }
 }
 template <int STRIDE>
-__device__ __forceinline__ void wave_steps(uint32_t (&x)[2], const uint32_t (&at)[2], uint32_t size) {
-    if (STRIDE < (int)size) keep(x, {lane_xor<STRIDE>(x[0]), lane_xor<STRIDE>(x[1])}, at, size, STRIDE);
-    if constexpr (STRIDE > 1) wave_steps<STRIDE / 2>(x, at, size);
+__device__ __forceinline__ void wave_steps(Items& x, uint32_t first, uint32_t size) {
+    if (STRIDE < (int)size) {
+        Items y;
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) {
+            if constexpr (STRIDE < 64) y[k] = lane_xor<STRIDE>(x[k]);
+            else y[k] = x[k ^ (STRIDE / 64)];
+        }
+        keep(x, y, first, size, STRIDE);
+    }
+    if constexpr (STRIDE > 1) wave_steps<STRIDE / 2>(x, first, size);
 }
 
 // edges: the elements before and behind the 16-byte vectors of the table, written here.
@@ -170,35 +181,38 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t
         return;
     }
     __shared__ uint32_t shared[kBlock];
-    // element p of the block: lane p % 64 of wave p / 128, its first or second by p / 64 % 2
-    const uint32_t at[2] = {(tid >> 6) * 128 + (tid & 63), (tid >> 6) * 128 + (tid & 63) + 64};
+    const uint32_t first = (tid >> 6) * (64 * kItems) + (tid & 63);      // the lane's elements: first + 64 k
     const uint32_t base = blockIdx.x * (uint32_t)kBlock;
-    uint32_t x[2];
+    Items x;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        uint32_t v = kNone;
-        if (base + at[k] < rows) {
-            const int32_t id = ids[base + at[k]];
-            if (ignore_id < 0 || id != ignore_id) v = (uint32_t)row_of(id, vocab) << kBlockBits | at[k];
+    for (int k = 0; k < kItems; ++k) {
+        const uint32_t at = first + 64 * k;
+        uint32_t r = kMaxVocab;
+        if (base + at < rows) {
+            const int32_t id = ids[base + at];
+            if (ignore_id < 0 || id != ignore_id) r = (uint32_t)row_of(id, vocab);
         }
-        x[k] = v == kNone ? kMaxVocab << kBlockBits | at[k] : v;
+        x[k] = r << kBlockBits | at;
     }
-    for (uint32_t size = 2; size <= kBlock; size *= 2) {
-        for (uint32_t stride = size / 2; stride >= 128; stride /= 2) {
+    const uint32_t here = rows - base < kBlock ? rows - base : kBlock;   // what lies behind them is in order already
+    for (uint32_t size = 2; size < 2 * here; size *= 2) {
+        for (uint32_t stride = size / 2; stride >= 64 * kItems; stride /= 2) {
             __syncthreads();
-            shared[at[0]] = x[0];
-            shared[at[1]] = x[1];
+#pragma unroll
+            for (int k = 0; k < kItems; ++k) shared[first + 64 * k] = x[k];
             __syncthreads();
-            keep(x, {shared[at[0] ^ stride], shared[at[1] ^ stride]}, at, size, stride);
+            Items y;
+#pragma unroll
+            for (int k = 0; k < kItems; ++k) y[k] = shared[(first + 64 * k) ^ stride];
+            keep(x, y, first, size, stride);
         }
-        if (size >= 128) keep(x, {x[1], x[0]}, at, size, 64);
-        wave_steps<32>(x, at, size);
+        wave_steps<32 * kItems>(x, first, size);
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < kItems; ++k) {
         const uint32_t r = x[k] >> kBlockBits;
-        row[base + at[k]] = r == kMaxVocab ? kNone : r;
-        token[base + at[k]] = base + (x[k] & (kBlock - 1));
+        row[base + first + 64 * k] = r == kMaxVocab ? kNone : r;
+        token[base + first + 64 * k] = base + (x[k] & (kBlock - 1));
     }
 }
 
