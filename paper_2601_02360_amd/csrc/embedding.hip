@@ -287,6 +287,18 @@ struct Columns {
         back = mine ? VEC - n : 0;
     }
 };
+// Which piece or window (their number is a multiple of eight) and which slice of its columns a wave takes.  A workgroup's waves,
+// up to four, are independent; they and the other workgroups of the same rows follow each other on one XCD, so that lines which two
+// slices share meet in one L2.
+struct Unit {
+    uint32_t item, slice;
+    __device__ __forceinline__ Unit(uint32_t group, uint32_t slices) {
+        const uint32_t waves = blockDim.x / 64, groups = (slices + waves - 1) / waves, place = group / 8;
+        item = place / groups * 8 + group % 8;
+        slice = place % groups * waves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    }
+};
+constexpr uint32_t kMostWaves = 4;
 template <int VEC>
 struct Sums {
     float v[VEC];
@@ -308,23 +320,23 @@ __device__ __forceinline__ void add(Sums<VEC>& a, const Sums<VEC>& b) {
     for (int j = 0; j < VEC; ++j) a.v[j] += b.v[j];
 }
 
-constexpr int kWaves = 4;                // independent waves of a workgroup: neighbouring columns of the same rows
 constexpr int kPiece = 16;               // entries of a piece: rows of grad_out in flight
 constexpr int kWindow = 64;              // entries that one partial sum covers: those a wave looks at together
 static_assert(kWindow <= 64 && kBlock % kWindow == 0 && kWindow % kPiece == 0, "a wave walks whole windows");
 
 // Windows of entries that lie inside one run: their sums, so that a frequent token's run is not left to one wave.
 template <int VEC, class G>
-__global__ __launch_bounds__(64) void window_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
+__global__ __launch_bounds__(kMostWaves * 64) void window_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
                                                          const uint32_t* __restrict__ token, int d, int slices,
                                                          float* __restrict__ partial, uint32_t groups, Zeros zeros) {
     if (blockIdx.x >= groups) {
         write_zeros(zeros, blockIdx.x - groups);
         return;
     }
-    const uint32_t window = blockIdx.x / (uint32_t)slices, slice = blockIdx.x % (uint32_t)slices, first = window * kWindow;
-    if (row[first] != row[first + kWindow - 1] || row[first] == kNone) return;
-    const Columns<VEC> at(d, (int)slice, slices, (int)threadIdx.x);
+    const Unit unit(blockIdx.x, (uint32_t)slices);
+    const uint32_t slice = unit.slice, lane = threadIdx.x & 63, first = unit.item * kWindow;
+    if (slice >= (uint32_t)slices || row[first] != row[first + kWindow - 1] || row[first] == kNone) return;
+    const Columns<VEC> at(d, (int)slice, slices, (int)lane);
     Sums<VEC> sum = {};
     for (int e = 0; e < kWindow; e += kPiece) {
         Sums<VEC> x[kPiece];
@@ -333,7 +345,7 @@ __global__ __launch_bounds__(64) void window_sums_kernel(const G* __restrict__ g
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) add(sum, x[k]);
     }
-    float* to = partial + ((uint64_t)blockIdx.x * 64 + threadIdx.x) * VEC;
+    float* to = partial + (((uint64_t)unit.item * slices + slice) * 64 + lane) * VEC;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) to[j] = sum.v[j];
 }
@@ -364,13 +376,13 @@ __device__ __forceinline__ Sums<VEC> load_row(const O* out, const Columns<VEC>& 
 }
 
 template <int VEC, bool ADDED, class G, class O>
-__global__ __launch_bounds__(kWaves * 64) void row_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
+__global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
                                                       const uint32_t* __restrict__ token, const float* __restrict__ partial,
                                                       uint32_t entries, int d, int slices, float scale,
                                                       O* __restrict__ out) {
-    const uint32_t unit = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const uint32_t piece = unit / (uint32_t)slices, slice = unit % (uint32_t)slices;
-    if (piece * kPiece >= entries) return;
+    const Unit unit(blockIdx.x, (uint32_t)slices);
+    const uint32_t piece = unit.item, slice = unit.slice, lane = threadIdx.x & 63;
+    if (slice >= (uint32_t)slices) return;
     // the piece's window, an entry a lane (their number is a multiple of 2048); the piece begins at entry q of it
     uint32_t e = piece * kPiece / kWindow * kWindow;
     const uint32_t q = piece * kPiece % kWindow;
@@ -588,13 +600,14 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
         constexpr int VEC = decltype(vec)::value;
         using G = decltype(gradient);
         using O = decltype(result);
+        const uint32_t each = ((uint32_t)slices + kMostWaves - 1) / kMostWaves, waves = ((uint32_t)slices + each - 1) / each;
+        const uint32_t window_groups = entries / kWindow * each;
         if (many)
-            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(entries / kWindow * (uint32_t)slices + groups_of(shares[2])), dim3(64), 0,
-                               st, static_cast<const G*>(grad_out), row[in], token[in], d, slices, partial,
-                               entries / kWindow * (uint32_t)slices, shares[2]);
+            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(window_groups + groups_of(shares[2])), dim3(waves * 64), 0, st,
+                               static_cast<const G*>(grad_out), row[in], token[in], d, slices, partial, window_groups, shares[2]);
         auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((entries / kPiece * (uint32_t)slices + kWaves - 1) / kWaves), dim3(kWaves * 64), 0, st,
-                               static_cast<const G*>(grad_out), row[in], token[in], many ? partial : nullptr, entries, d, slices, scale, static_cast<O*>(grad_table));
+            hipLaunchKernelGGL(kernel, dim3(entries / kPiece * each), dim3(waves * 64), 0, st, static_cast<const G*>(grad_out), row[in],
+                               token[in], many ? partial : nullptr, entries, d, slices, scale, static_cast<O*>(grad_table));
         };
         if (accumulate) launch(row_sums_kernel<VEC, true, G, O>);
         else launch(row_sums_kernel<VEC, false, G, O>);
