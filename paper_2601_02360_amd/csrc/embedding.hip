@@ -60,6 +60,8 @@ __device__ __forceinline__ int row_of(int32_t id, int vocab) { return id < 0 ? 0
 
 // ---------------------------------------------------------------- lookup
 
+constexpr int64_t kMostFours = 1 << 21;  // (a launch has fewer than 2^32 lanes)
+
 // A wave takes one token in one span of columns.  Workgroups go to the eight XCDs round-robin by number, and spans go with
 // them: with four spans an XCD's L2 is asked for one fourth of every table row and of PosEmbed, and holds four times as many of them.
 template <class T, class O>
@@ -69,31 +71,31 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
                                                      int width) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int span = (int)(blockIdx.x % (unsigned)spans);
-    const int64_t row = (int64_t)(blockIdx.x / (unsigned)spans) * 4 + wave;
-    if (row >= rows) return;
-    const int64_t from = (int64_t)row_of(ids[row], vocab) * d;
-    const T *a = table + from, *b = t_perp ? t_perp + from : nullptr;
-    const T* p = pos ? pos + (int64_t)((uint32_t)row % (uint32_t)seq) * d : nullptr;
     const int end = (span + 1) * width < d ? (span + 1) * width : d;
-    for (int c = span * width + lane * 4; c < end; c += 512) {
-        float4 x[2], y[2], z[2];
+    for (int64_t row = (int64_t)(blockIdx.x / (unsigned)spans) * 4 + wave; row < rows; row += gridDim.x / (unsigned)spans * 4ll) {
+        const int64_t from = (int64_t)row_of(ids[row], vocab) * d;
+        const T *a = table + from, *b = t_perp ? t_perp + from : nullptr;
+        const T* p = pos ? pos + (int64_t)((uint32_t)row % (uint32_t)seq) * d : nullptr;
+        for (int c = span * width + lane * 4; c < end; c += 512) {
+            float4 x[2], y[2], z[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
-            if (at >= end) continue;
-            x[k] = load_some(a + at, n);
-            if (b) y[k] = load_some(b + at, n);
-            if (p) z[k] = load_some(p + at, n);
-        }
+            for (int k = 0; k < 2; ++k) {
+                const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
+                if (at >= end) continue;
+                x[k] = load_some(a + at, n);
+                if (b) y[k] = load_some(b + at, n);
+                if (p) z[k] = load_some(p + at, n);
+            }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
-            if (at >= end) continue;
-            float4 v = x[k];
-            if (b) v = make_float4(v.x + y[k].x, v.y + y[k].y, v.z + y[k].z, v.w + y[k].w);
-            v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
-            if (p) v = make_float4(v.x + z[k].x, v.y + z[k].y, v.z + z[k].z, v.w + z[k].w);
-            store_some(out + row * d + at, n, v);
+            for (int k = 0; k < 2; ++k) {
+                const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
+                if (at >= end) continue;
+                float4 v = x[k];
+                if (b) v = make_float4(v.x + y[k].x, v.y + y[k].y, v.z + y[k].z, v.w + y[k].w);
+                v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
+                if (p) v = make_float4(v.x + z[k].x, v.y + z[k].y, v.z + z[k].z, v.w + z[k].w);
+                store_some(out + row * d + at, n, v);
+            }
         }
     }
 }
@@ -118,11 +120,12 @@ struct Zeros {
     uint64_t vectors;
 };
 constexpr int kZeroSpan = 512;           // vectors a workgroup writes (50304 rows of 768: 26.6 us, 1024: 28.3, 2048: 30.4, 256: 36.7)
+constexpr uint32_t kMostZeroGroups = 1 << 20;
 __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group) {
     typedef uint32_t vuint4 __attribute__((ext_vector_type(4)));
-    const uint64_t from = (uint64_t)group * kZeroSpan;
-    for (uint32_t i = threadIdx.x; i < kZeroSpan; i += blockDim.x)
-        if (from + i < z.vectors) __builtin_nontemporal_store(vuint4{0, 0, 0, 0}, (SPLC_GLOBAL vuint4*)(z.at + from + i));
+    for (uint64_t from = (uint64_t)group * kZeroSpan; from < z.vectors; from += (uint64_t)kMostZeroGroups * kZeroSpan)
+        for (uint32_t i = threadIdx.x; i < kZeroSpan; i += blockDim.x)
+            if (from + i < z.vectors) __builtin_nontemporal_store(vuint4{0, 0, 0, 0}, (SPLC_GLOBAL vuint4*)(z.at + from + i));
 }
 
 // The value that lane (this one ^ STRIDE) has.  Below 16 lanes by the vector ALU's own lane moves; through LDS, whose pipe 16
@@ -485,6 +488,16 @@ __global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __re
 
 int vec_of(int d) { return d < 256 ? 1 : 4; }
 int slices_of(int d) { return ((d + vec_of(d) - 1) / vec_of(d) + 63) / 64; }
+// How the workgroups of the sums take a row's slices: `groups` of them, of `waves` waves.
+struct Slices {
+    uint32_t count, groups, waves, lanes;
+    explicit Slices(int d) {
+        count = (uint32_t)slices_of(d);
+        groups = (count + kMostWaves - 1) / kMostWaves;
+        waves = (count + groups - 1) / groups;
+        lanes = groups * waves * 64;
+    }
+};
 
 // The workspace: entries (rows and tokens) of two stages of the sort in turn, the windows' sums.
 struct GradSpace {
@@ -501,7 +514,8 @@ struct GradSpace {
 };
 
 bool grad_sizes_fit(int64_t rows, int vocab, int d) {
-    return rows >= 0 && rows < ((int64_t)1 << 31) - kBlock && vocab >= 1 && vocab < (int)kMaxVocab && d >= 1 && d < 1 << 24;
+    if (rows < 0 || rows >= (int64_t)1 << 30 || vocab < 1 || vocab >= (int)kMaxVocab || d < 1 || d >= 1 << 24) return false;
+    return ((rows + kBlock - 1) / kBlock * (kBlock / kPiece)) * Slices(d).lanes < (int64_t)1 << 32;      // (of one launch)
 }
 
 }  // namespace
@@ -524,7 +538,7 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
     int spans = 1;                                            // 1, 2 or 4, of whole vectors
     while (spans < 4 && spans * 256 < d) spans *= 2;
     const int width = ((d + spans - 1) / spans + 3) / 4 * 4;
-    const int64_t groups = (rows + 3) / 4 * spans;            // (below 2^31)
+    const int64_t fours = (rows + 3) / 4, groups = (fours < kMostFours ? fours : kMostFours) * spans;
     auto launch = [&](auto element, auto result) {
         using T = decltype(element);
         using O = decltype(result);
@@ -557,7 +571,7 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     const GradSpace space(rows, d);
     if (ws_bytes < space.bytes) return SPLC_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const int slices = slices_of(d);
+    const Slices slices(d);
     const uint32_t entries = (uint32_t)space.entries, blocks = entries / kBlock;
     const bool many = blocks > 1;        // to be merged, and runs worth more than a wave
     uint32_t *row[2], *token[2];
@@ -577,7 +591,10 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     const uint64_t sort_share = many ? vectors / 2 : vectors, merge_share = many ? vectors / 4 : 0;
     const Zeros shares[3] = {{vector, sort_share}, {vector + sort_share, merge_share},
                              {vector + sort_share + merge_share, vectors - sort_share - merge_share}};
-    auto groups_of = [](const Zeros& z) { return (uint32_t)((z.vectors + kZeroSpan - 1) / kZeroSpan); };
+    auto groups_of = [](const Zeros& z) {
+        const uint64_t spans = (z.vectors + kZeroSpan - 1) / kZeroSpan;
+        return (uint32_t)(spans < kMostZeroGroups ? spans : kMostZeroGroups);
+    };
 
     auto sort = [&](auto result) {
         using O = decltype(result);
@@ -600,14 +617,15 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
         constexpr int VEC = decltype(vec)::value;
         using G = decltype(gradient);
         using O = decltype(result);
-        const uint32_t each = ((uint32_t)slices + kMostWaves - 1) / kMostWaves, waves = ((uint32_t)slices + each - 1) / each;
-        const uint32_t window_groups = entries / kWindow * each;
+        const uint32_t window_groups = entries / kWindow * slices.groups;
         if (many)
-            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(window_groups + groups_of(shares[2])), dim3(waves * 64), 0, st,
-                               static_cast<const G*>(grad_out), row[in], token[in], d, slices, partial, window_groups, shares[2]);
+            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(window_groups + groups_of(shares[2])), dim3(slices.waves * 64), 0, st,
+                               static_cast<const G*>(grad_out), row[in], token[in], d, (int)slices.count, partial, window_groups,
+                               shares[2]);
         auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(entries / kPiece * each), dim3(waves * 64), 0, st, static_cast<const G*>(grad_out), row[in],
-                               token[in], many ? partial : nullptr, entries, d, slices, scale, static_cast<O*>(grad_table));
+            hipLaunchKernelGGL(kernel, dim3(entries / kPiece * slices.groups), dim3(slices.waves * 64), 0, st,
+                               static_cast<const G*>(grad_out), row[in], token[in], many ? partial : nullptr, entries, d,
+                               (int)slices.count, scale, static_cast<O*>(grad_table));
         };
         if (accumulate) launch(row_sums_kernel<VEC, true, G, O>);
         else launch(row_sums_kernel<VEC, false, G, O>);

@@ -51,7 +51,10 @@ def test_gradient_arguments():
     for bad in (dict(g=ctypes.c_void_p(4098)), dict(table=ctypes.c_void_p(4097), tt=1), dict(ids=ctypes.c_void_p(4098)),
                 dict(ws=ctypes.c_void_p(4100))):
         assert call(**bad) == B.SPLC_EALIGN, bad
-    assert size(0, 5, 8) >= 0 and size(2 ** 31, 5, 8) == B.SPLC_EINVAL
+    assert size(0, 5, 8) >= 0 and size(2 ** 30, 5, 8) == B.SPLC_EINVAL
+    for rows, d in ((2 ** 30 - 2048, 32), (2 ** 28, 127), (2 ** 20, 32767), (2 ** 11, 2 ** 24 - 1)):
+        assert size(rows, 5, d) > 0                                       # rows d < 2^35
+    assert size(2 ** 30 - 2048, 5, 2 ** 20) == B.SPLC_EINVAL
     for vocab, d in ((5, 8), (50304, 768), (32001, 2050)):                # more rows never need less
         sizes = [size(rows, vocab, d) for rows in (0, 1, 100, 16384, 16385, 10 ** 6)]
         assert sizes == sorted(sizes)
