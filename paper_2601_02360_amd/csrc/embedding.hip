@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
 // ---------------------------------------------------------------- gradient: order of the tokens
 //
 // Entries (table row, token) are sorted by row, equal rows by token.  A workgroup sorts a block of 2048 in registers and LDS
-// (bitonic, on row * 2048 + place in the block); then up to eight sorted runs at a time become one, every entry finding its place
+// (bitonically, by row * 2048 + place in the block); then up to eight sorted runs at a time become one, every entry finding its place
 // by itself: the number of smaller entries in each of the other runs, by binary search.  Tokens that are left out, and what fills the last
 // block, have row kNone and come last.
 //
@@ -128,44 +128,68 @@ __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group) {
             if (from + i < z.vectors) __builtin_nontemporal_store(vuint4{0, 0, 0, 0}, (SPLC_GLOBAL vuint4*)(z.at + from + i));
 }
 
-// The value that lane (this one ^ STRIDE) has.  Below 16 lanes by the vector ALU's own lane moves; through LDS, whose pipe 16
-// waves share, those steps took most of the sort.
-template <int STRIDE>
+// The value that lane (this one ^ MASK) has.  Inside rows of 16 lanes by the vector ALU's own lane moves.
+template <int MASK>
 __device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
     auto move = [](uint32_t v, auto control) {
         return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, 0xF, 0xF, true);
     };
     using std::integral_constant;
-    if constexpr (STRIDE == 1) return move(x, integral_constant<int, 0xB1>{});           // quads: 1 0 3 2
-    else if constexpr (STRIDE == 2) return move(x, integral_constant<int, 0x4E>{});      // quads: 2 3 0 1
-    else if constexpr (STRIDE == 4)                                                      // 7 - lane of eight, quads: 3 2 1 0
-        return move(move(x, integral_constant<int, 0x141>{}), integral_constant<int, 0x1B>{});
-    else if constexpr (STRIDE == 8) return move(x, integral_constant<int, 0x128>{});     // rows of 16 turned by eight
-    else return __shfl_xor(x, STRIDE);
+    if constexpr (MASK == 1) return move(x, integral_constant<int, 0xB1>{});             // quads: 1 0 3 2
+    else if constexpr (MASK == 2) return move(x, integral_constant<int, 0x4E>{});        // quads: 2 3 0 1
+    else if constexpr (MASK == 3) return move(x, integral_constant<int, 0x1B>{});        // quads: 3 2 1 0
+    else if constexpr (MASK == 4) return lane_xor<3>(lane_xor<7>(x));
+    else if constexpr (MASK == 7) return move(x, integral_constant<int, 0x141>{});       // eights turned round
+    else if constexpr (MASK == 8) return move(x, integral_constant<int, 0x128>{});       // rows turned by eight
+    else if constexpr (MASK == 15) return move(x, integral_constant<int, 0x140>{});      // rows turned round
+    else return __shfl_xor(x, MASK);
 }
-// One bitonic step on a lane's elements (numbers first + 64 k), y what the elements `stride` apart hold: the smaller one stays if this
-// is the first of a pair that ascends, or the second of one that descends.
+
+// The sort of a block: sorted runs of SIZE / 2 become runs of SIZE.  Every element meets the one whose number differs in the bits of
+// MASK, first all below SIZE (so that one of the two runs is taken backwards), then one bit at a time, and of the two the one with
+// the lower number keeps the smaller.  A lane's elements have the numbers first + 64 k.
 using Items = uint32_t[kItems];
-__device__ __forceinline__ void keep(Items& x, const Items& y, uint32_t first, uint32_t size, uint32_t stride) {
+struct SortShared {
+    uint32_t x[2][kBlock];
+};
+template <uint32_t MASK>
+__device__ __forceinline__ void meet(Items& x, uint32_t first, uint32_t bit, SortShared& shared, uint32_t& side) {
+    Items y;
+    if constexpr (MASK >= 64 * kItems) {
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        const uint32_t at = first + 64 * k;
-        const bool smaller = ((at & size) == 0) == ((at & stride) == 0);
-        x[k] = smaller == (x[k] < y[k]) ? x[k] : y[k];
-    }
-}
-template <int STRIDE>
-__device__ __forceinline__ void wave_steps(Items& x, uint32_t first, uint32_t size) {
-    if (STRIDE < (int)size) {
-        Items y;
+        for (int k = 0; k < kItems; ++k) shared.x[side][first + 64 * k] = x[k];
+        __syncthreads();                                     // (the other side is written next: nobody reads it any more)
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) y[k] = shared.x[side][(first + 64 * k) ^ MASK];
+        side ^= 1;
+    } else {
 #pragma unroll
         for (int k = 0; k < kItems; ++k) {
-            if constexpr (STRIDE < 64) y[k] = lane_xor<STRIDE>(x[k]);
-            else y[k] = x[k ^ (STRIDE / 64)];
+            const uint32_t other = x[k ^ (int)(MASK / 64)];
+            if constexpr (MASK % 64 == 0) y[k] = other;
+            else y[k] = lane_xor<MASK % 64>(other);
         }
-        keep(x, y, first, size, STRIDE);
     }
-    if constexpr (STRIDE > 1) wave_steps<STRIDE / 2>(x, first, size);
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const uint32_t smaller = x[k] < y[k] ? x[k] : y[k], larger = x[k] < y[k] ? y[k] : x[k];
+        x[k] = ((first + 64 * k) & bit) == 0 ? smaller : larger;
+    }
+}
+template <uint32_t BIT>
+__device__ __forceinline__ void meet_by_bits(Items& x, uint32_t first, SortShared& shared, uint32_t& side) {
+    if constexpr (BIT > 0) {
+        meet<BIT>(x, first, BIT, shared, side);
+        meet_by_bits<BIT / 2>(x, first, shared, side);
+    }
+}
+// Up to the first `count` elements; those behind them are in order already.
+template <uint32_t SIZE>
+__device__ __forceinline__ void merge_up(Items& x, uint32_t first, uint32_t count, SortShared& shared, uint32_t& side) {
+    if (SIZE >= 2 * count) return;
+    meet<SIZE - 1>(x, first, SIZE / 2, shared, side);
+    meet_by_bits<SIZE / 4>(x, first, shared, side);
+    if constexpr (SIZE < kBlock) merge_up<SIZE * 2>(x, first, count, shared, side);
 }
 
 // edges: the elements before and behind the 16-byte vectors of the table, written here.
@@ -183,7 +207,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t
         write_zeros(zeros, blockIdx.x - blocks);
         return;
     }
-    __shared__ uint32_t shared[kBlock];
+    __shared__ SortShared shared;
     const uint32_t first = (tid >> 6) * (64 * kItems) + (tid & 63);      // the lane's elements: first + 64 k
     const uint32_t base = blockIdx.x * (uint32_t)kBlock;
     Items x;
@@ -197,20 +221,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t
         }
         x[k] = r << kBlockBits | at;
     }
-    const uint32_t here = rows - base < kBlock ? rows - base : kBlock;   // what lies behind them is in order already
-    for (uint32_t size = 2; size < 2 * here; size *= 2) {
-        for (uint32_t stride = size / 2; stride >= 64 * kItems; stride /= 2) {
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < kItems; ++k) shared[first + 64 * k] = x[k];
-            __syncthreads();
-            Items y;
-#pragma unroll
-            for (int k = 0; k < kItems; ++k) y[k] = shared[(first + 64 * k) ^ stride];
-            keep(x, y, first, size, stride);
-        }
-        wave_steps<32 * kItems>(x, first, size);
-    }
+    uint32_t side = 0;
+    merge_up<2>(x, first, rows - base < kBlock ? rows - base : kBlock, shared, side);
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
         const uint32_t r = x[k] >> kBlockBits;
@@ -370,7 +382,7 @@ template <int VEC, class O>
 __device__ __forceinline__ Sums<VEC> load_row(const O* out, const Columns<VEC>& at) {
     Sums<VEC> s;
     if constexpr (VEC == 4) {
-        const float4 x = load_some(out + at.col, at.n);
+        const float4 x = at.n == 4 ? widened(stream_load4(out + at.col)) : load_some(out + at.col, at.n);
         s.v[0] = x.x; s.v[1] = x.y; s.v[2] = x.z; s.v[3] = x.w;
     } else {
         s.v[0] = widened(out[at.col]);
