@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
 
 constexpr int kBlock = 2048, kBlockBits = 11, kSortThreads = 1024, kFanIn = 8;
 constexpr int kItems = kBlock / kSortThreads;                // elements of a lane while it sorts
-constexpr uint32_t kNone = 0xFFFFFFFFu, kMaxVocab = (1u << (32 - kBlockBits)) - 1;
+constexpr uint32_t kNone = 0x7FFFFFFFu, kMaxVocab = (1u << (32 - kBlockBits)) - 1;
 
 // A launch's share of the zeros: 16-byte vectors from `at`, workgroup by workgroup.
 struct Zeros {
@@ -231,51 +231,60 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t
     }
 }
 
-// Sorted runs of `length` entries (the last one of all may be shorter), kFanIn of them at a time, to one run.  Of every run 256
-// entries at equal distances lie in LDS for the first steps of the search; from a distance of 32 on the others are in one cache line.
-constexpr uint32_t kSamples = 256;
-__global__ __launch_bounds__(256) void merge_runs_kernel(const uint32_t* __restrict__ row, const uint32_t* __restrict__ token,
-                                                         uint32_t entries, uint32_t length, uint32_t* __restrict__ row_out,
-                                                         uint32_t* __restrict__ token_out, uint32_t groups, Zeros zeros) {
+// Sorted runs of `length` entries (the last one of all may be shorter), kFanIn of them at a time, to one run.  Of every run
+// SAMPLES entries at equal distances lie in LDS for the first steps of the search: all of them while runs are blocks, of longer
+// ones 1024, and from a distance of 32 on the others are in one cache line.
+template <bool BLOCKS, uint32_t SAMPLES, uint32_t THREADS>
+__global__ __launch_bounds__(THREADS) void merge_runs_kernel(const uint32_t* __restrict__ row, const uint32_t* __restrict__ token,
+                                                             uint32_t entries, uint32_t length, uint32_t* __restrict__ row_out,
+                                                             uint32_t* __restrict__ token_out, uint32_t groups, Zeros zeros) {
     if (blockIdx.x >= groups) {
         write_zeros(zeros, blockIdx.x - groups);
         return;
     }
-    __shared__ uint32_t sample[kFanIn * kSamples];           // the last entry of each stretch
-    const uint32_t i = blockIdx.x * 256 + threadIdx.x;       // (the number of entries is a multiple of 2048, as is a run's)
-    const uint32_t run = blockIdx.x * 256 / length, first = run / kFanIn * kFanIn, stretch = length / kSamples;
-    uint32_t some[kFanIn * kSamples / 256];
+    __shared__ uint32_t sample[kFanIn * SAMPLES];            // the last entry of each stretch
+    static_assert(!BLOCKS || SAMPLES == kBlock, "all entries of a block");
+    const uint32_t i = blockIdx.x * THREADS + threadIdx.x;   // (the number of entries is a multiple of 2048, as is a run's)
+    const uint32_t run = blockIdx.x * THREADS / length, first = run / kFanIn * kFanIn, stretch = BLOCKS ? 1 : length / SAMPLES;
+    uint32_t some[kFanIn * SAMPLES / THREADS];
 #pragma unroll
-    for (uint32_t s = 0; s < kFanIn * kSamples / 256; ++s) {
-        const uint64_t at = (uint64_t)first * length + (uint64_t)(s * 256 + threadIdx.x + 1) * stretch - 1;
+    for (uint32_t s = 0; s < kFanIn * SAMPLES / THREADS; ++s) {
+        const uint64_t at = (uint64_t)first * length + (uint64_t)(s * THREADS + threadIdx.x + 1) * stretch - 1;
         some[s] = at < entries ? row[at] : kNone;
     }
     const uint32_t r = row[i], t = token[i];
 #pragma unroll
-    for (uint32_t s = 0; s < kFanIn * kSamples / 256; ++s) sample[s * 256 + threadIdx.x] = some[s];
+    for (uint32_t s = 0; s < kFanIn * SAMPLES / THREADS; ++s) sample[s * THREADS + threadIdx.x] = some[s];
     __syncthreads();
     uint32_t below[kFanIn] = {};                             // entries that go before this one; the searches go side by side
-    auto before = [&](uint32_t seen, uint32_t k) { return seen < r || (seen == r && first + k < run); };     // (of equal rows)
-#pragma unroll 1
-    for (uint32_t step = kSamples / 2; step > 0; step /= 2)
+    uint32_t limit[kFanIn];                                  // those of rows below it; of equal rows earlier runs' entries do
+#pragma unroll
+    for (uint32_t k = 0; k < kFanIn; ++k) limit[k] = first + k < run ? r + 1 : r;
+#pragma unroll
+    for (uint32_t step = SAMPLES / 2; step > 0; step /= 2)
+#pragma unroll
+        for (uint32_t k = 0; k < kFanIn; ++k) below[k] += sample[k * SAMPLES + step - 1 + below[k]] < limit[k] ? step : 0;
+    // (all stretches but the last at most are counted: whether that one goes before is for what follows to find)
+    if constexpr (BLOCKS) {
 #pragma unroll
         for (uint32_t k = 0; k < kFanIn; ++k)
-            if (before(sample[k * kSamples + below[k] + step - 1], k)) below[k] += step;
-    // (255 stretches at most are counted: whether the last one goes before is for the steps below to find)
+            below[k] += sample[k * SAMPLES + below[k]] < limit[k] ? 1 : 0;
+    } else {
 #pragma unroll
-    for (uint32_t k = 0; k < kFanIn; ++k) below[k] *= stretch;
-    for (uint32_t step = stretch; step > 0; step /= 2) {
-        uint32_t seen[kFanIn];
-        bool inside[kFanIn];
+        for (uint32_t k = 0; k < kFanIn; ++k) below[k] *= stretch;
+        for (uint32_t step = stretch; step > 0; step /= 2) {
+            uint32_t seen[kFanIn];
+            bool inside[kFanIn];
 #pragma unroll
-        for (uint32_t k = 0; k < kFanIn; ++k) {
-            const uint64_t at = (uint64_t)(first + k) * length + below[k] + step - 1;
-            inside[k] = below[k] + step <= length && at < entries;
-            seen[k] = inside[k] ? row[at] : kNone;
+            for (uint32_t k = 0; k < kFanIn; ++k) {
+                const uint64_t at = (uint64_t)(first + k) * length + below[k] + step - 1;
+                inside[k] = below[k] + step <= length && at < entries;
+                seen[k] = inside[k] ? row[at] : kNone;
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kFanIn; ++k)
+                below[k] += inside[k] && seen[k] < limit[k] ? step : 0;
         }
-#pragma unroll
-        for (uint32_t k = 0; k < kFanIn; ++k)
-            if (inside[k] && before(seen[k], k)) below[k] += step;
     }
     uint32_t place = first * length + (i - run * length);
 #pragma unroll
@@ -621,9 +630,14 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     if (rows == 0) return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
     int in = 0;
     for (uint64_t length = kBlock; length < entries; length *= kFanIn, in ^= 1) {
-        const Zeros share = length == kBlock ? shares[1] : Zeros{nullptr, 0};
-        hipLaunchKernelGGL(merge_runs_kernel, dim3(entries / 256 + groups_of(share)), dim3(256), 0, st, row[in], token[in], entries,
-                           (uint32_t)length, row[in ^ 1], token[in ^ 1], entries / 256, share);
+        const bool blocks_yet = length == kBlock;
+        const Zeros share = blocks_yet ? shares[1] : Zeros{nullptr, 0};
+        auto merge = [&](auto kernel, uint32_t threads) {
+            hipLaunchKernelGGL(kernel, dim3(entries / threads + groups_of(share)), dim3(threads), 0, st, row[in], token[in], entries,
+                               (uint32_t)length, row[in ^ 1], token[in ^ 1], entries / threads, share);
+        };
+        if (blocks_yet) merge(merge_runs_kernel<true, kBlock, 512>, 512);
+        else merge(merge_runs_kernel<false, 1024, 512>, 512);
     }
     auto sums = [&](auto vec, auto gradient, auto result) {
         constexpr int VEC = decltype(vec)::value;
