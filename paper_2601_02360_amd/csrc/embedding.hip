@@ -105,7 +105,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
 // Entries (table row, token) are sorted by row, equal rows by token.  A workgroup sorts a block of 2048 in registers and LDS
 // (bitonically, by row * 2048 + place in the block); then up to eight sorted runs at a time become one, every entry finding its place
 // by itself: the number of smaller entries in each of the other runs, by binary search.  Tokens that are left out, and what fills the last
-// block, have row kNone and come last.
+// block, have row kNone and token 0 and come last.
 //
 // Where the table is written whole, its zeros are written by further workgroups of these launches, which have little else to
 // do with the memory; rows that have tokens are written again later.
@@ -192,7 +192,7 @@ __device__ __forceinline__ void merge_up(Items& x, uint32_t first, uint32_t coun
     if constexpr (SIZE < kBlock) merge_up<SIZE * 2>(x, first, count, shared, side);
 }
 
-// edges: the elements before and behind the 16-byte vectors of the table, written here.
+// head, tail: how many elements of the table lie before and behind its 16-byte vectors; the first further workgroup writes them.
 template <class O>
 __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t* __restrict__ ids, uint32_t rows, int vocab,
                                                                    int32_t ignore_id, uint32_t blocks, uint32_t* __restrict__ row,
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t
     for (int k = 0; k < kItems; ++k) {
         const uint32_t r = x[k] >> kBlockBits;
         row[base + first + 64 * k] = r == kMaxVocab ? kNone : r;
-        token[base + first + 64 * k] = base + (x[k] & (kBlock - 1));
+        token[base + first + 64 * k] = r == kMaxVocab ? 0 : base + (x[k] & (kBlock - 1));   // (read, and not used)
     }
 }
 

@@ -158,6 +158,24 @@ def test_every_token_ignored_and_rows_with_nan(rows, vocab, d, accumulate):
     assert torch.isnan(table).nonzero().tolist() == [[(rows - 1) % vocab, d - 1]]
 
 
+@pytest.mark.parametrize("rows,entries,stage", [(5, 2048, 0), (2048, 2048, 0), (2049, 4096, 1), (16384 + 7, 18432, 0)])
+def test_no_entry_of_the_order_names_a_token_that_is_not_there(rows, entries, stage):
+    """The workspace holds the order of the tokens ([rows, tokens] of two stages): every entry's token is one of the call's, also
+    of those that only fill a block, whose rows of grad_out are read like the others'."""
+    vocab, d = 50, 8
+    ws = B.embedding_grad_workspace(rows, vocab, d)
+    ws.fill_(255)
+    ids = torch.arange(rows, device="cuda", dtype=torch.int32) % vocab
+    grad, table = torch.ones(rows, d, device="cuda"), torch.empty(vocab, d, device="cuda")
+    B.sparseloco_embedding_grad(grad, ids, table, ws)
+    at = (2 * stage + 1) * entries
+    row, token = (ws[:16 * entries].view(torch.int32)[at + k * entries:at + (k + 1) * entries] for k in (-1, 0))
+    assert token.min().item() >= 0 and token.max().item() < rows
+    assert torch.equal(row[:rows], ids.sort().values) and (row[rows:] >= vocab).all()
+    assert torch.equal(ids[token[:rows].long()], row[:rows])
+    assert torch.equal(table.sum(1), torch.bincount(ids, minlength=vocab).float() * d)
+
+
 def test_gradient_against_differences():
     """The sum of weights times the looked-up rows, by differences in the table, in fp64 from fp32 lookups of powers of two
     that every step of the lookup forms exactly: the quotient of differences is the gradient exactly."""

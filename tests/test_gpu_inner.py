@@ -154,6 +154,43 @@ def test_adamw(numels, grad_dtype, copy, scaled, tiled):
             assert torch.equal(t_copy[i], t_theta[i].to(torch.bfloat16))
 
 
+@pytest.mark.parametrize("grad_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shifts", [(1, 1, 2, 1, 2), (63, 63, 62, 63, 62), (64, 64, 64, 64, 64), (33, 2, 4, 0, 6), (0, 5, 2, 63, 34), (32, 32, 32, 32, 32)])
+def test_adamw_of_arrays_at_any_place(shifts, grad_dtype):
+    """Workgroups begin where theta has a multiple of 256 bytes: theta, m, v, gradients and copy at this many elements past one,
+    together and each by itself, tensors that end inside, at and just behind a chunk's end, and beside each other in memory."""
+    numels = [4096 * 3, 4096 * 2 + 1, 4096 * 2 + 64, 4096, 4095, 4033, 64, 63, 1, 4097, 4096 * 2 - 63]
+    theta, g, m, v = inputs(numels, sum(shifts), grad_dtype)
+    plan = B.Plan(numels, 32)
+    arrays = [theta, m, [np.zeros(n, np.float32) for n in numels], v, g]
+    dtypes = [torch.float32, torch.float32, torch.bfloat16, torch.float32, grad_dtype]
+    shifts = list(shifts[:4]) + [shifts[4] if grad_dtype == torch.bfloat16 else shifts[0]]
+    tens, buffers = [], []
+    for host, dtype, shift in zip(arrays, dtypes, shifts):
+        step = 2 if dtype == torch.bfloat16 else 1           # (a bf16 tensor starts at a dword)
+        shift = shift // step * step
+        buf = torch.full((shift + sum(-(-n // step) * step for n in numels) + 64,), GUARD, dtype=dtype, device="cuda")
+        assert buf.data_ptr() % 256 == 0
+        at, views, mine = shift, [], torch.zeros(buf.numel(), dtype=torch.bool, device="cuda")
+        for h, n in zip(host, numels):
+            views.append(buf[at:at + n].copy_(torch.as_tensor(h)))
+            mine[at:at + n] = True
+            at += -(-n // step) * step
+        tens.append(views)
+        buffers.append((buf, mine))
+    t_theta, t_m, t_copy, t_v, t_g = tens
+    B.sparseloco_adamw_step(plan, plan.bind(t_theta), plan.bind(t_g, dtype=grad_dtype), plan.bind(t_m), plan.bind(t_v),
+                            theta_bf16=plan.bind(t_copy, dtype=torch.bfloat16), **HOW)
+    for buf, mine in buffers:
+        assert (buf[~mine] == GUARD).all(), "written beside a tensor"
+    for i, n in enumerate(numels):
+        want = step_tensor((theta[i], g[i], m[i], np.sqrt(v[i].astype(np.float64))), 1.0, 1.0, HOW)
+        for got, k, what in ((t_theta[i], 0, "theta"), (t_m[i], 1, "m"), (t_v[i], 2, "v")):
+            within(f64(got), want[k], want[k + 3], "%s of tensor %d" % (what, i))
+        assert torch.equal(t_copy[i], t_theta[i].to(torch.bfloat16))
+        assert torch.equal(t_g[i].float().cpu(), torch.as_tensor(g[i])), "gradients were changed"
+
+
 @pytest.mark.parametrize("how", [dict(HOW, step=1), dict(HOW, beta1=0.0, beta2=0.0), dict(HOW, weight_decay=0.0, eps=1e-3),
                                  dict(HOW, step=100000, beta2=0.999), dict(HOW, lr=0.0)])
 def test_adamw_numbers(how):
