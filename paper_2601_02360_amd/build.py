@@ -12,6 +12,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -21,7 +22,7 @@ LIB = os.path.join(HERE, "libsparseloco.so")
 CALLS = os.path.join(HERE, "_calls.so")
 
 HIPCC_FLAGS = [
-    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
+    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
     "-ffp-contract=off",
     # keep the compiler from forming packed fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -39,8 +40,20 @@ def _run(cmd, out: str, verbose: bool) -> None:
 
 
 def build(verbose: bool = False, extra=()) -> str:
+    """Every source to an object, side by side, and the objects to the library."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    _run([hipcc, *HIPCC_FLAGS, *extra, *SOURCES], LIB, verbose)
+    with tempfile.TemporaryDirectory() as at:
+        objects, running = [], []
+        for source in SOURCES:
+            objects.append(os.path.join(at, os.path.basename(source) + ".o"))
+            cmd = [hipcc, *HIPCC_FLAGS, *extra, "-c", source, "-o", objects[-1]]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append((cmd, subprocess.Popen(cmd)))
+        failed = [cmd for cmd, p in running if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        _run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", *objects], LIB, verbose)
     build_calls(verbose)
     return LIB
 

@@ -16,27 +16,8 @@ namespace {
 
 using namespace splc;
 
-typedef __bf16 vbf16x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ float widened(float v) { return v; }
-__device__ __forceinline__ float widened(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ float4 widened(float4 v) { return v; }
-__device__ __forceinline__ float4 widened(uint2 v) {
-    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
-                       __uint_as_float(v.y & 0xFFFF0000u));
-}
-// Rounded to nearest, ties to even.
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-    const vbf16x2 v = {(__bf16)a, (__bf16)b};
-    return __builtin_bit_cast(uint32_t, v);
-}
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(uint16_t* p, float v) { *p = (uint16_t)bf16_pair(v, v); }
-__device__ __forceinline__ void put4(float* p, float4 v) { stream_store4(p, v); }
-__device__ __forceinline__ void put4(uint16_t* p, float4 v) {
-    const vuint2 t = {bf16_pair(v.x, v.y), bf16_pair(v.z, v.w)};
-    __builtin_nontemporal_store(t, (SPLC_GLOBAL vuint2*)p);
-}
 // n (1..4) elements at p.
 template <class T>
 __device__ __forceinline__ float4 load_some(const T* p, int n) {
@@ -49,7 +30,7 @@ __device__ __forceinline__ float4 load_some(const T* p, int n) {
 template <class T>
 __device__ __forceinline__ void store_some(T* p, int n, float4 v) {
     if (n == 4) {
-        put4(p, v);
+        stream_store4(p, v);
         return;
     }
     store1(p, v.x);
@@ -62,8 +43,12 @@ __device__ __forceinline__ int row_of(int32_t id, int vocab) { return id < 0 ? 0
 
 constexpr int64_t kMostFours = 1 << 21;  // (a launch has fewer than 2^32 lanes)
 
-// A wave takes one token in one span of columns.  Workgroups go to the eight XCDs round-robin by number, and spans go with
-// them: with four spans an XCD's L2 is asked for one fourth of every table row and of PosEmbed, and holds four times as many of them.
+// Bound by memory: rows of the table in the order of the tokens, and out.  A wave takes one token in one span of columns, two
+// vectors of every array in flight.  Workgroups go to the eight XCDs round-robin by number, and spans go with them: with four
+// spans an XCD's L2 is asked for one fourth of every table row and of PosEmbed, and holds four times as many of them.  MI355X, 16384
+// tokens of 32000, d 2048, both tables and positions to bf16, 1 / 2 / 4 / 8 spans: 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be
+// done without, 4.1 TB/s; a copy reaches 4.8); one table 22.0 us; two, four or eight tokens a wave 40.7 / 40.8 / 42.0; out without the
+// streaming hint 45.0.
 template <class T, class O>
 __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table, const T* __restrict__ t_perp,
                                                      const int32_t* __restrict__ ids, int vocab, const T* __restrict__ pos,
@@ -109,6 +94,9 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
 //
 // Where the table is written whole, its zeros are written by further workgroups of these launches, which have little else to
 // do with the memory; rows that have tokens are written again later.
+//
+// MI355X: sorting a block takes 7 us (64 tokens 2.7), bound by the vector ALU of its compute unit; merging 5 to 9 us, of which 4 are
+// the launch and a chain of loads.
 
 constexpr int kBlock = 2048, kBlockBits = 11, kSortThreads = 1024, kFanIn = 8;
 constexpr int kItems = kBlock / kSortThreads;                // elements of a lane while it sorts
@@ -295,8 +283,13 @@ __global__ __launch_bounds__(THREADS) void merge_runs_kernel(const uint32_t* __r
 
 // ---------------------------------------------------------------- gradient: sums
 //
-// A wave takes the runs of equal rows that begin in one piece of 16 entries, in one span of columns.  A lane has VEC consecutive
-// columns: four, or one where the table is narrow.
+// A wave takes the runs of equal rows that begin in one piece of 16 entries, in one span of columns, and keeps their sums in
+// registers: grad_out is read once, in rows, and every row of the table is written once, by one wave.  A lane has VEC consecutive
+// columns: four, or one where the table is narrow.  A run that goes on behind its piece is followed by its wave, through the sums of
+// whole windows, which other waves have formed before (a token that makes up 7 % of 65537: 69 windows in 5 batches instead of 4400
+// rows).  Bound by memory: MI355X, 65537 fp32 rows of 2050 into 32001 rows, frequencies 1 / rank, added to what is there: windows 42 us
+// (4.5 TB/s), runs 126 us (4.5 TB/s); 16384 bf16 rows of 2048: runs 21 us.  One token throughout: 98 and 145 us, 18 and 41 us.  grad_out
+// is read without the streaming hint, which loses lines that two slices share (65537 rows of few different tokens: 180 us with it, 128).
 
 // The lane's columns of a slice.  The last vector of a row whose length is no multiple of four holds fewer: it is read as the
 // four elements that end with the row (`back` elements earlier), and its elements are brought to the front.

@@ -65,6 +65,25 @@ __device__ __forceinline__ void stream_store4(float* p, float4 v) {
     __builtin_nontemporal_store(t, (SPLC_GLOBAL vfloat4*)p);
 }
 
+// fp32 and bf16 elements as fp32 (bf16 is the upper half of the word), one and four at a time.
+__device__ __forceinline__ float widened(float v) { return v; }
+__device__ __forceinline__ float widened(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ float4 widened(float4 v) { return v; }
+__device__ __forceinline__ float4 widened(uint2 v) {
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
+                       __uint_as_float(v.y & 0xFFFF0000u));
+}
+// Two as bf16, rounded to nearest, ties to even.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    typedef __bf16 vbf16x2 __attribute__((ext_vector_type(2)));
+    const vbf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ void stream_store4(uint16_t* p, float4 v) {
+    const vuint2 t = {bf16_pair(v.x, v.y), bf16_pair(v.z, v.w)};
+    __builtin_nontemporal_store(t, (SPLC_GLOBAL vuint2*)p);
+}
+
 }  // namespace splc
 
 struct sparseloco_plan {
