@@ -41,7 +41,7 @@ __device__ __forceinline__ int row_of(int32_t id, int vocab) { return id < 0 ? 0
 
 // ---------------------------------------------------------------- lookup
 
-constexpr int64_t kMostFours = 1 << 21;  // (a launch has fewer than 2^32 lanes)
+constexpr int64_t kMostTurns = 1 << 21;  // (a launch has fewer than 2^32 lanes)
 
 // Bound by memory: rows of the table in the order of the tokens, and out.  A wave takes one token in one span of columns, two
 // vectors of every array in flight.  Workgroups go to the eight XCDs round-robin by number, and spans go with them: with four
@@ -49,15 +49,18 @@ constexpr int64_t kMostFours = 1 << 21;  // (a launch has fewer than 2^32 lanes)
 // tokens of 32000, d 2048, both tables and positions to bf16, 1 / 2 / 4 / 8 spans: 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be
 // done without, 4.1 TB/s; a copy reaches 4.8); one table 22.0 us; two, four or eight tokens a wave 40.7 / 40.8 / 42.0; out without the
 // streaming hint 45.0.
-template <class T, class O>
+// NARROW: rows of at most 128 columns, of which a wave takes as many as it has `lanes` lanes for (22817 tokens, d 106: 8.0 -> 5.5 us; 65536, d 64: 18.9 -> 6.4).
+template <bool NARROW, class T, class O>
 __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table, const T* __restrict__ t_perp,
                                                      const int32_t* __restrict__ ids, int vocab, const T* __restrict__ pos,
                                                      int seq, float scale, O* __restrict__ out, int64_t rows, int d, int spans,
-                                                     int width) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+                                                     int width, int lanes) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = NARROW ? threadIdx.x % lanes : threadIdx.x & 63;
+    const int at_once = NARROW ? 256 / lanes : 4;            // rows a workgroup takes at once
     const int span = (int)(blockIdx.x % (unsigned)spans);
     const int end = (span + 1) * width < d ? (span + 1) * width : d;
-    for (int64_t row = (int64_t)(blockIdx.x / (unsigned)spans) * 4 + wave; row < rows; row += gridDim.x / (unsigned)spans * 4ll) {
+    for (int64_t row = (int64_t)(blockIdx.x / (unsigned)spans) * at_once + (NARROW ? (int)threadIdx.x / lanes : wave); row < rows;
+         row += (int64_t)(gridDim.x / (unsigned)spans) * at_once) {
         const int64_t from = (int64_t)row_of(ids[row], vocab) * d;
         const T *a = table + from, *b = t_perp ? t_perp + from : nullptr;
         const T* p = pos ? pos + (int64_t)((uint32_t)row % (uint32_t)seq) * d : nullptr;
@@ -552,13 +555,19 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
     int spans = 1;                                            // 1, 2 or 4, of whole vectors
     while (spans < 4 && spans * 256 < d) spans *= 2;
     const int width = ((d + spans - 1) / spans + 3) / 4 * 4;
-    const int64_t fours = (rows + 3) / 4, groups = (fours < kMostFours ? fours : kMostFours) * spans;
+    int lanes = 64;                                           // for a row; 16, 32 or 64
+    while (lanes > 16 && d <= lanes * 2) lanes /= 2;
+    const int64_t turns = (rows * lanes + 255) / 256, groups = (turns < kMostTurns ? turns : kMostTurns) * spans;
     auto launch = [&](auto element, auto result) {
         using T = decltype(element);
         using O = decltype(result);
-        hipLaunchKernelGGL((lookup_kernel<T, O>), dim3((unsigned)groups), dim3(256), 0, static_cast<hipStream_t>(stream),
-                           static_cast<const T*>(table), static_cast<const T*>(t_perp), token_ids, vocab,
-                           static_cast<const T*>(pos_embed), seq_len, scale, static_cast<O*>(out), rows, d, spans, width);
+        auto with = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, static_cast<hipStream_t>(stream),
+                               static_cast<const T*>(table), static_cast<const T*>(t_perp), token_ids, vocab,
+                               static_cast<const T*>(pos_embed), seq_len, scale, static_cast<O*>(out), rows, d, spans, width, lanes);
+        };
+        if (lanes < 64) with(lookup_kernel<true, T, O>);
+        else with(lookup_kernel<false, T, O>);
     };
     if (table_dtype == SPLC_F32 && out_dtype == SPLC_F32) launch(float{}, float{});
     else if (table_dtype == SPLC_F32) launch(float{}, uint16_t{});
