@@ -319,6 +319,10 @@ struct Unit {
     }
 };
 constexpr uint32_t kMostWaves = 4;
+// Up to so many entries a workgroup's waves take a piece together (below), instead of windows' sums and a wave by itself.  Together /
+// with windows, whole call: 2415 bf16 rows of 1792 of 388: 23.3 / 29.7 us, 4096 of 2048 of 32000: 53.5 / 55.7, 4096 fp32 rows of 256 of
+// 3000: 22.5 / 24.5; 8192 of 2048 of 32000: 60.4 / 59.0, 8192 of 512 of 1000: 34.6 / 28.5, 16000 of 1024 of 500: 57.6 / 33.1.
+constexpr uint32_t kTogetherMost = 4096;
 template <int VEC>
 struct Sums {
     float v[VEC];
@@ -395,14 +399,26 @@ __device__ __forceinline__ Sums<VEC> load_row(const O* out, const Columns<VEC>& 
     return s;
 }
 
-template <int VEC, bool ADDED, class G, class O>
+// TOGETHER: for few tokens, which leave most of the chip idle and make a launch for windows' sums too dear.  A workgroup's four waves
+// take one piece and slice; the first does what a wave does otherwise, and what goes on behind the piece's window is divided among
+// them, window by window, and joined in their order (runs of 2000 tokens of 300, fp32, d 2048: 22 -> 13 us).
+template <int VEC, bool ADDED, bool TOGETHER, class G, class O>
 __global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
                                                       const uint32_t* __restrict__ token, const float* __restrict__ partial,
                                                       uint32_t entries, int d, int slices, float scale,
                                                       O* __restrict__ out) {
-    const Unit unit(blockIdx.x, (uint32_t)slices);
-    const uint32_t piece = unit.item, slice = unit.slice, lane = threadIdx.x & 63;
-    if (slice >= (uint32_t)slices) return;
+    uint32_t piece, slice, wave = 0;
+    if constexpr (TOGETHER) {
+        piece = blockIdx.x / (uint32_t)slices;
+        slice = blockIdx.x % (uint32_t)slices;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    } else {
+        const Unit unit(blockIdx.x, (uint32_t)slices);
+        piece = unit.item;
+        slice = unit.slice;
+        if (slice >= (uint32_t)slices) return;
+    }
+    const uint32_t lane = threadIdx.x & 63;
     // the piece's window, an entry a lane (their number is a multiple of 2048); the piece begins at entry q of it
     uint32_t e = piece * kPiece / kWindow * kWindow;
     const uint32_t q = piece * kPiece % kWindow;
@@ -434,7 +450,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __re
                 if (k + i < end) add(sum, x[i]);
         }
     };
-    {
+    if (!TOGETHER || wave == 0) {
         Sums<VEC> x[kPiece];
         uint32_t r[kPiece];
         load(x, q, q + kPiece);
@@ -468,9 +484,31 @@ __global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __re
     if (last == kNone) return;
     now = last;
     uint32_t end = run_end(q + kPiece);
-    add_run(q + kPiece, end);
-    while (end == kWindow && (e += kWindow) < entries) {     // the run goes on in the next window
-        if (partial) {                                       // and in whole ones, up to 16 at a time
+    if (!TOGETHER || wave == 0) add_run(q + kPiece, end);
+    if constexpr (TOGETHER) {
+        for (uint32_t w = e + (wave + 1) * kWindow; end == kWindow && w < entries; w += kMostWaves * kWindow) {
+            rows = row[w + lane % kWindow];
+            tokens = token[w + lane % kWindow];
+            const uint32_t stop = run_end(0);
+            add_run(0, stop);
+            if (stop < kWindow) break;
+        }
+        if (end == kWindow) {                                // (the same for all four)
+            __shared__ float parts[kMostWaves - 1][VEC][64];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (wave > 0) parts[wave - 1][j][lane] = sum.v[j];
+            __syncthreads();
+            for (uint32_t w = 0; w < kMostWaves - 1; ++w) {
+                Sums<VEC> x;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) x.v[j] = parts[w][j][lane];
+                add(sum, x);
+            }
+        }
+        if (wave > 0) return;
+    } else {
+        while (end == kWindow && (e += kWindow) < entries) { // the run goes on in the next window, and in whole ones, up to 16 at a time
             const uint32_t w = e + lane * kWindow;
             const bool whole = lane < kPiece && w < entries && row[w] == now && row[w + kWindow - 1] == now;
             const uint32_t n = (uint32_t)__builtin_ctzll(~__ballot(whole));
@@ -488,11 +526,11 @@ __global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __re
                 e += (n - 1) * kWindow;
                 continue;
             }
+            rows = row[e + lane % kWindow];
+            tokens = token[e + lane % kWindow];
+            end = run_end(0);
+            add_run(0, end);
         }
-        rows = row[e + lane % kWindow];
-        tokens = token[e + lane % kWindow];
-        end = run_end(0);
-        add_run(0, end);
     }
     if (at.n > 0) {
         Sums<VEC> was;
@@ -596,7 +634,7 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const Slices slices(d);
     const uint32_t entries = (uint32_t)space.entries, blocks = entries / kBlock;
-    const bool many = blocks > 1;        // to be merged, and runs worth more than a wave
+    const bool merged = blocks > 1, many = entries > kTogetherMost;
     uint32_t *row[2], *token[2];
     for (int k = 0; k < 2; ++k) {
         row[k] = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + space.row[k]);
@@ -611,7 +649,7 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     const uint64_t vectors = accumulate ? 0 : (size - head) * element / 16;
     const uint64_t tail = size - head - vectors * 16 / element;
     uint4* vector = reinterpret_cast<uint4*>(static_cast<char*>(grad_table) + head * element);
-    const uint64_t sort_share = many ? vectors / 2 : vectors, merge_share = many ? vectors / 4 : 0;
+    const uint64_t sort_share = merged ? vectors / 2 : vectors, merge_share = many ? vectors / 4 : vectors - sort_share;
     const Zeros shares[3] = {{vector, sort_share}, {vector + sort_share, merge_share},
                              {vector + sort_share + merge_share, vectors - sort_share - merge_share}};
     auto groups_of = [](const Zeros& z) {
@@ -650,13 +688,15 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
             hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(window_groups + groups_of(shares[2])), dim3(slices.waves * 64), 0, st,
                                static_cast<const G*>(grad_out), row[in], token[in], d, (int)slices.count, partial, window_groups,
                                shares[2]);
-        auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(entries / kPiece * slices.groups), dim3(slices.waves * 64), 0, st,
-                               static_cast<const G*>(grad_out), row[in], token[in], many ? partial : nullptr, entries, d,
-                               (int)slices.count, scale, static_cast<O*>(grad_table));
+        auto launch = [&](auto kernel, uint32_t groups, uint32_t waves) {
+            hipLaunchKernelGGL(kernel, dim3(groups), dim3(waves * 64), 0, st, static_cast<const G*>(grad_out), row[in], token[in], partial,
+                               entries, d, (int)slices.count, scale, static_cast<O*>(grad_table));
         };
-        if (accumulate) launch(row_sums_kernel<VEC, true, G, O>);
-        else launch(row_sums_kernel<VEC, false, G, O>);
+        const uint32_t pieces = entries / kPiece;
+        if (many && accumulate) launch(row_sums_kernel<VEC, true, false, G, O>, pieces * slices.groups, slices.waves);
+        else if (many) launch(row_sums_kernel<VEC, false, false, G, O>, pieces * slices.groups, slices.waves);
+        else if (accumulate) launch(row_sums_kernel<VEC, true, true, G, O>, pieces * slices.count, kMostWaves);
+        else launch(row_sums_kernel<VEC, false, true, G, O>, pieces * slices.count, kMostWaves);
     };
     auto by_type = [&](auto vec) {
         if (grad_dtype == SPLC_F32 && table_dtype == SPLC_F32) sums(vec, float{}, float{});
