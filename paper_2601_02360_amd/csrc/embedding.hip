@@ -570,7 +570,9 @@ struct GradSpace {
 
 bool grad_sizes_fit(int64_t rows, int vocab, int d) {
     if (rows < 0 || rows >= (int64_t)1 << 30 || vocab < 1 || vocab >= (int)kMaxVocab || d < 1 || d >= 1 << 24) return false;
-    return ((rows + kBlock - 1) / kBlock * (kBlock / kPiece)) * Slices(d).lanes < (int64_t)1 << 32;      // (of one launch)
+    const int64_t entries = (rows + kBlock - 1) / kBlock * kBlock;
+    const int64_t lanes = entries > kTogetherMost ? Slices(d).lanes : Slices(d).count * kMostWaves * 64;       // for a piece
+    return entries / kPiece * lanes < (int64_t)1 << 32;       // (of one launch)
 }
 
 }  // namespace

@@ -123,7 +123,7 @@ def test_gradient_of_few_tokens(rows, vocab, d):
 
 @pytest.mark.parametrize("rows,vocab,d", [(2048, 4000, 260), (4097, 300, 513), (16384, 32000, 64), (16383, 2000, 300), (16385, 2561, 257),
                                           (40000, 999, 65), (33000, 9000, 270), (50000, 3, 258), (2049, 40, 64),
-                                          (65537, 700, 80), (140000, 5000, 66)])
+                                          (65537, 700, 80), (140000, 5000, 66), (4096, 700, 300)])
 @pytest.mark.parametrize("how", ["text", "same", "spread"])
 def test_gradient_of_many_tokens(rows, vocab, d, how):
     """Long runs of one token, several blocks of the sort, one and two rounds of merging."""

@@ -55,6 +55,7 @@ def test_gradient_arguments():
     for rows, d in ((2 ** 30 - 2048, 32), (2 ** 28, 127), (2 ** 20, 32767), (2 ** 11, 2 ** 24 - 1)):
         assert size(rows, 5, d) > 0                                       # rows d < 2^35
     assert size(2 ** 30 - 2048, 5, 2 ** 20) == B.SPLC_EINVAL
+    assert size(4096, 5, 2 ** 24 - 1) == B.SPLC_EINVAL and size(4096, 5, 2 ** 23 - 1) > 0
     for vocab, d in ((5, 8), (50304, 768), (32001, 2050)):                # more rows never need less
         sizes = [size(rows, vocab, d) for rows in (0, 1, 100, 16384, 16385, 10 ** 6)]
         assert sizes == sorted(sizes)
