@@ -43,46 +43,55 @@ __device__ __forceinline__ int row_of(int32_t id, int vocab) { return id < 0 ? 0
 
 constexpr int64_t kMostTurns = 1 << 21;  // (a launch has fewer than 2^32 lanes)
 
-// Bound by memory: rows of the table in the order of the tokens, and out.  A wave takes one token in one span of columns, two
-// vectors of every array in flight.  Workgroups go to the eight XCDs round-robin by number, and spans go with them: with four
-// spans an XCD's L2 is asked for one fourth of every table row and of PosEmbed, and holds four times as many of them.  MI355X, 16384
-// tokens of 32000, d 2048, both tables and positions to bf16, 1 / 2 / 4 / 8 spans: 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be
-// done without, 4.1 TB/s; a copy reaches 4.8); one table 22.0 us; two, four or eight tokens a wave 40.7 / 40.8 / 42.0; out without the
-// streaming hint 45.0.
-// NARROW: rows of at most 128 columns, of which a wave takes as many as it has `lanes` lanes for (22817 tokens, d 106: 8.0 -> 5.5 us; 65536, d 64: 18.9 -> 6.4).
-template <bool NARROW, class T, class O>
+// Bound by memory: rows of the table in the order of the tokens, and out.  A wave takes ROWS tokens in one span of columns, and two
+// to four vectors of every array are in flight: two of one row, or, of spans of at most 256 columns, one of four (65536 tokens of
+// 50304, d 256, bf16: 15.4 -> 11.7 us; d 150, fp32, two tables: 18.0 -> 14.3).
+// Workgroups go to the eight XCDs round-robin by number, and spans go with them: with four spans an XCD's L2 is asked for one fourth of
+// every table row and of PosEmbed, and holds four times as many of them.  But a span is 1 to 2 KB of a row where there are several,
+// since waves that read less of it at once wait longer than they read.  MI355X, 16384 tokens of 32000, d 2048, both fp32 tables and
+// positions to bf16, 1 / 2 / 4 / 8 spans: 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be done without, 4.1 TB/s; a copy reaches
+// 4.8); 65536 of 50304, d 768, bf16, 1 / 2 / 4 spans: 31.0 / 43.0 / 64.8.  out without the streaming hint: 45.0 instead of 40.1.
+// NARROW: rows of at most 128 columns, of which a wave takes as many at once as it has `lanes` lanes for (22817 tokens, d 106: 8.0 -> 5.5
+// us; 65536, d 64: 18.9 -> 6.4, and 5.0 with four times as many).
+template <bool NARROW, int ROWS, class T, class O>
 __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table, const T* __restrict__ t_perp,
                                                      const int32_t* __restrict__ ids, int vocab, const T* __restrict__ pos,
                                                      int seq, float scale, O* __restrict__ out, int64_t rows, int d, int spans,
                                                      int width, int lanes) {
+    constexpr int COLS = ROWS == 1 ? 2 : 1;                  // vectors of a row at once
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = NARROW ? threadIdx.x % lanes : threadIdx.x & 63;
-    const int at_once = NARROW ? 256 / lanes : 4;            // rows a workgroup takes at once
+    const int at_once = (NARROW ? 256 / lanes : 4) * ROWS;   // rows a workgroup takes at once
     const int span = (int)(blockIdx.x % (unsigned)spans);
     const int end = (span + 1) * width < d ? (span + 1) * width : d;
-    for (int64_t row = (int64_t)(blockIdx.x / (unsigned)spans) * at_once + (NARROW ? (int)threadIdx.x / lanes : wave); row < rows;
+    for (int64_t row = (int64_t)(blockIdx.x / (unsigned)spans) * at_once + (NARROW ? (int)threadIdx.x / lanes : wave) * ROWS; row < rows;
          row += (int64_t)(gridDim.x / (unsigned)spans) * at_once) {
-        const int64_t from = (int64_t)row_of(ids[row], vocab) * d;
-        const T *a = table + from, *b = t_perp ? t_perp + from : nullptr;
-        const T* p = pos ? pos + (int64_t)((uint32_t)row % (uint32_t)seq) * d : nullptr;
-        for (int c = span * width + lane * 4; c < end; c += 512) {
-            float4 x[2], y[2], z[2];
+        int64_t from[ROWS];
+        const T* p[ROWS];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
+        for (int r = 0; r < ROWS; ++r) {
+            const int64_t at = row + r < rows ? row + r : rows - 1;      // (the last row once more, and not written)
+            from[r] = (int64_t)row_of(ids[at], vocab) * d;
+            p[r] = pos ? pos + (int64_t)((uint32_t)at % (uint32_t)seq) * d : nullptr;
+        }
+        for (int c = span * width + lane * 4; c < end; c += 256 * COLS) {
+            float4 x[ROWS * COLS], y[ROWS * COLS], z[ROWS * COLS];
+#pragma unroll
+            for (int k = 0; k < ROWS * COLS; ++k) {
+                const int at = c + 256 * (k % COLS), n = d - at < 4 ? d - at : 4, r = k / COLS;
                 if (at >= end) continue;
-                x[k] = load_some(a + at, n);
-                if (b) y[k] = load_some(b + at, n);
-                if (p) z[k] = load_some(p + at, n);
+                x[k] = load_some(table + from[r] + at, n);
+                if (t_perp) y[k] = load_some(t_perp + from[r] + at, n);
+                if (pos) z[k] = load_some(p[r] + at, n);
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int at = c + 256 * k, n = d - at < 4 ? d - at : 4;
-                if (at >= end) continue;
+            for (int k = 0; k < ROWS * COLS; ++k) {
+                const int at = c + 256 * (k % COLS), n = d - at < 4 ? d - at : 4, r = k / COLS;
+                if (at >= end || row + r >= rows) continue;
                 float4 v = x[k];
-                if (b) v = make_float4(v.x + y[k].x, v.y + y[k].y, v.z + y[k].z, v.w + y[k].w);
+                if (t_perp) v = make_float4(v.x + y[k].x, v.y + y[k].y, v.z + y[k].z, v.w + y[k].w);
                 v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
-                if (p) v = make_float4(v.x + z[k].x, v.y + z[k].y, v.z + z[k].z, v.w + z[k].w);
-                store_some(out + row * d + at, n, v);
+                if (pos) v = make_float4(v.x + z[k].x, v.y + z[k].y, v.z + z[k].z, v.w + z[k].w);
+                store_some(out + (row + r) * d + at, n, v);
             }
         }
     }
@@ -593,11 +602,12 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
         return SPLC_EALIGN;
     if (rows == 0) return SPLC_OK;
     int spans = 1;                                            // 1, 2 or 4, of whole vectors
-    while (spans < 4 && spans * 256 < d) spans *= 2;
+    while (spans < 4 && spans * (2048 / (int)in) < d) spans *= 2;
     const int width = ((d + spans - 1) / spans + 3) / 4 * 4;
     int lanes = 64;                                           // for a row; 16, 32 or 64
     while (lanes > 16 && d <= lanes * 2) lanes /= 2;
-    const int64_t turns = (rows * lanes + 255) / 256, groups = (turns < kMostTurns ? turns : kMostTurns) * spans;
+    const int each = width <= 256 ? 4 : 1;                    // rows of a wave at once
+    const int64_t turns = ((rows + each - 1) / each * lanes + 255) / 256, groups = (turns < kMostTurns ? turns : kMostTurns) * spans;
     auto launch = [&](auto element, auto result) {
         using T = decltype(element);
         using O = decltype(result);
@@ -606,8 +616,9 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
                                static_cast<const T*>(table), static_cast<const T*>(t_perp), token_ids, vocab,
                                static_cast<const T*>(pos_embed), seq_len, scale, static_cast<O*>(out), rows, d, spans, width, lanes);
         };
-        if (lanes < 64) with(lookup_kernel<true, T, O>);
-        else with(lookup_kernel<false, T, O>);
+        if (lanes < 64) with(lookup_kernel<true, 4, T, O>);
+        else if (each == 4) with(lookup_kernel<false, 4, T, O>);
+        else with(lookup_kernel<false, 1, T, O>);
     };
     if (table_dtype == SPLC_F32 && out_dtype == SPLC_F32) launch(float{}, float{});
     else if (table_dtype == SPLC_F32) launch(float{}, uint16_t{});
