@@ -438,7 +438,7 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
  * Without accumulate every row is written (zero where no token has it), with it only the rows that tokens have.
  *   token_ids: as above; those equal to ignore_id (a padding token; negative: none) are left out.
  *   ws: sparseloco_embedding_grad_ws_bytes(rows, vocab, d) bytes of device memory, 8-byte aligned, need not be cleared; a
- *   workspace for more rows serves fewer.  rows <= 2^30 - 2048, rows * d < 2^35, vocab < 2^21 - 1, d < 2^24.
+ *   workspace for more rows serves fewer.  d < 2^24, rows * max(d, 64) < 2^34.
  * The tokens of a row are added in an order that depends on token_ids alone: the same call gives the same bits.
  */
 int64_t sparseloco_embedding_grad_ws_bytes(int64_t rows, int vocab, int d);

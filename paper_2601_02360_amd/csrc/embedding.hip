@@ -99,27 +99,31 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
 
 // ---------------------------------------------------------------- gradient: order of the tokens
 //
-// Entries (table row, token) are sorted by row, equal rows by token.  A workgroup sorts a block of 2048 in registers and LDS
-// (bitonically, by row * 2048 + place in the block); then up to eight sorted runs at a time become one, every entry finding its place
-// by itself: the number of smaller entries in each of the other runs, by binary search.  Tokens that are left out, and what fills the last
-// block, have row kNone and token 0 and come last.
+// Entries (table row, token) are sorted by row, equal rows by token.  A workgroup has 64 or 128 entries of a run and finds their
+// places in it by looking at all others of the run; runs are kDirect long where that is all, else kRun, and up to eight at a
+// time become one, every entry finding its place by itself: the number of smaller entries in each of the other runs, by binary
+// search.  Tokens that are left out, and what fills the last windows, have row kNone and token 0 and come last.
 //
 // Where the table is written whole, its zeros are written by further workgroups of these launches, which have little else to
 // do with the memory; rows that have tokens are written again later.
 //
-// MI355X: sorting a block takes 7 us (64 tokens 2.7), bound by the vector ALU of its compute unit; merging 5 to 9 us, of which 4 are
-// the launch and a chain of loads.
+// MI355X: 64 tokens 3.1 us, 4096 at once 4.8, 16384 9.4; 65537 in runs 8.6, merged in 5.9 and 8.7, of which 4 are the launch and a chain
+// of loads.  Bound by the vector ALU and LDS, which take every token through 7 (8) steps of search for every 64 (128) others of its run.
 
-constexpr int kBlock = 2048, kBlockBits = 11, kSortThreads = 1024, kFanIn = 8;
-constexpr int kItems = kBlock / kSortThreads;                // elements of a lane while it sorts
-constexpr uint32_t kNone = 0x7FFFFFFFu, kMaxVocab = (1u << (32 - kBlockBits)) - 1;
+constexpr uint32_t kNone = 0x7FFFFFFFu;
+constexpr int kBlock = 512;              // the number of entries is a multiple of this
+// Above 64 MB of zeros the launches that write them take longer than the order, and one more has room for it: at once / in runs,
+// whole call, 16384 bf16 rows of 2048 of 50304: 88.5 / 84.1 us, of 32000: 65.2 / 61.9, of 16000: 44.9 / 42.9, of 8000: 34.2 / 34.4; added
+// to what is there, 43.1 / 46.
+constexpr uint64_t kFewZeros = 1 << 22;  // vectors
+constexpr uint32_t kRun = 2048, kDirect = 16384, kOrderThreads = 1024, kMergeThreads = 512, kFanIn = 8;
 
 // A launch's share of the zeros: 16-byte vectors from `at`, workgroup by workgroup.
 struct Zeros {
     uint4* at;
     uint64_t vectors;
 };
-constexpr int kZeroSpan = 512;           // vectors a workgroup writes (50304 rows of 768: 26.6 us, 1024: 28.3, 2048: 30.4, 256: 36.7)
+constexpr uint32_t kZeroSpan = 512;      // vectors a workgroup writes (50304 rows of 768: 26.6 us, 1024: 28.3, 2048: 30.4, 256: 36.7)
 constexpr uint32_t kMostZeroGroups = 1 << 20;
 __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group) {
     typedef uint32_t vuint4 __attribute__((ext_vector_type(4)));
@@ -128,133 +132,130 @@ __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group) {
             if (from + i < z.vectors) __builtin_nontemporal_store(vuint4{0, 0, 0, 0}, (SPLC_GLOBAL vuint4*)(z.at + from + i));
 }
 
-// The value that lane (this one ^ MASK) has.  Inside rows of 16 lanes by the vector ALU's own lane moves.
-template <int MASK>
-__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
-    auto move = [](uint32_t v, auto control) {
-        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, 0xF, 0xF, true);
-    };
-    using std::integral_constant;
-    if constexpr (MASK == 1) return move(x, integral_constant<int, 0xB1>{});             // quads: 1 0 3 2
-    else if constexpr (MASK == 2) return move(x, integral_constant<int, 0x4E>{});        // quads: 2 3 0 1
-    else if constexpr (MASK == 3) return move(x, integral_constant<int, 0x1B>{});        // quads: 3 2 1 0
-    else if constexpr (MASK == 4) return lane_xor<3>(lane_xor<7>(x));
-    else if constexpr (MASK == 7) return move(x, integral_constant<int, 0x141>{});       // eights turned round
-    else if constexpr (MASK == 8) return move(x, integral_constant<int, 0x128>{});       // rows turned by eight
-    else if constexpr (MASK == 15) return move(x, integral_constant<int, 0x140>{});      // rows turned round
-    else return __shfl_xor(x, MASK);
-}
-
-// The sort of a block: sorted runs of SIZE / 2 become runs of SIZE.  Every element meets the one whose number differs in the bits of
-// MASK, first all below SIZE (so that one of the two runs is taken backwards), then one bit at a time, and of the two the one with
-// the lower number keeps the smaller.  A lane's elements have the numbers first + 64 k.
-using Items = uint32_t[kItems];
-struct SortShared {
-    uint32_t x[2][kBlock];
-};
-template <uint32_t MASK>
-__device__ __forceinline__ void meet(Items& x, uint32_t first, uint32_t bit, SortShared& shared, uint32_t& side) {
-    Items y;
-    if constexpr (MASK >= 64 * kItems) {
-#pragma unroll
-        for (int k = 0; k < kItems; ++k) shared.x[side][first + 64 * k] = x[k];
-        __syncthreads();                                     // (the other side is written next: nobody reads it any more)
-#pragma unroll
-        for (int k = 0; k < kItems; ++k) y[k] = shared.x[side][(first + 64 * k) ^ MASK];
-        side ^= 1;
-    } else {
-#pragma unroll
-        for (int k = 0; k < kItems; ++k) {
-            const uint32_t other = x[k ^ (int)(MASK / 64)];
-            if constexpr (MASK % 64 == 0) y[k] = other;
-            else y[k] = lane_xor<MASK % 64>(other);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        const uint32_t smaller = x[k] < y[k] ? x[k] : y[k], larger = x[k] < y[k] ? y[k] : x[k];
-        x[k] = ((first + 64 * k) & bit) == 0 ? smaller : larger;
-    }
-}
-template <uint32_t BIT>
-__device__ __forceinline__ void meet_by_bits(Items& x, uint32_t first, SortShared& shared, uint32_t& side) {
-    if constexpr (BIT > 0) {
-        meet<BIT>(x, first, BIT, shared, side);
-        meet_by_bits<BIT / 2>(x, first, shared, side);
-    }
-}
-// Up to the first `count` elements; those behind them are in order already.
-template <uint32_t SIZE>
-__device__ __forceinline__ void merge_up(Items& x, uint32_t first, uint32_t count, SortShared& shared, uint32_t& side) {
-    if (SIZE >= 2 * count) return;
-    meet<SIZE - 1>(x, first, SIZE / 2, shared, side);
-    meet_by_bits<SIZE / 4>(x, first, shared, side);
-    if constexpr (SIZE < kBlock) merge_up<SIZE * 2>(x, first, count, shared, side);
-}
-
-// head, tail: how many elements of the table lie before and behind its 16-byte vectors; the first further workgroup writes them.
-template <class O>
-__global__ __launch_bounds__(kSortThreads) void sort_tokens_kernel(const int32_t* __restrict__ ids, uint32_t rows, int vocab,
-                                                                   int32_t ignore_id, uint32_t blocks, uint32_t* __restrict__ row,
-                                                                   uint32_t* __restrict__ token, Zeros zeros, O* table,
-                                                                   uint64_t table_size, uint32_t head, uint32_t tail) {
-    const uint32_t tid = threadIdx.x;
-    if (blockIdx.x >= blocks) {
-        if (blockIdx.x == blocks) {
+// The order of every run of `run` entries.  A workgroup has KEYS of a run's entries, puts these in order by comparing each with each, and
+// finds for every other of the run before which of them it goes, by binary search; the numbers of those add up to places.
+// 64 where that gives few workgroups, 128 in runs of kRun (65537 tokens: 10.8 and 8.6 us, 256: 13.1).
+constexpr uint32_t kAtOnce = 4;                              // searches of a lane side by side
+template <uint32_t KEYS, class O>
+__global__ __launch_bounds__(kOrderThreads) void order_tokens_kernel(const int32_t* __restrict__ ids, uint32_t rows, int vocab,
+                                                                     int32_t ignore_id, uint32_t run, uint32_t groups,
+                                                                     uint32_t* __restrict__ row, uint32_t* __restrict__ token,
+                                                                     Zeros zeros, O* table,
+                                                                     uint64_t table_size, uint32_t head, uint32_t tail) {
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (blockIdx.x >= groups) {
+        if (blockIdx.x == groups) {
             if (tid < head) table[tid] = O(0);
             if (tid < tail) table[table_size - 1 - tid] = O(0);
         }
-        write_zeros(zeros, blockIdx.x - blocks);
+        write_zeros(zeros, blockIdx.x - groups);
         return;
     }
-    __shared__ SortShared shared;
-    const uint32_t first = (tid >> 6) * (64 * kItems) + (tid & 63);      // the lane's elements: first + 64 k
-    const uint32_t base = blockIdx.x * (uint32_t)kBlock;
-    Items x;
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        const uint32_t at = first + 64 * k;
-        uint32_t r = kMaxVocab;
-        if (base + at < rows) {
-            const int32_t id = ids[base + at];
-            if (ignore_id < 0 || id != ignore_id) r = (uint32_t)row_of(id, vocab);
+    const uint32_t base = blockIdx.x * KEYS, run_from = base / run * run, run_to = rows < run_from + run ? rows : run_from + run;
+    if (base >= rows) {                                      // (these only fill the last windows)
+        if (tid < KEYS) {
+            row[base + tid] = kNone;
+            token[base + tid] = 0;
         }
-        x[k] = r << kBlockBits | at;
+        return;
     }
-    uint32_t side = 0;
-    merge_up<2>(x, first, rows - base < kBlock ? rows - base : kBlock, shared, side);
+    auto row_named = [&](int32_t id) { return ignore_id < 0 || id != ignore_id ? (uint32_t)row_of(id, vocab) : kNone; };
+    auto key = [&](uint32_t i) { return base + i < rows ? row_named(ids[base + i]) : kNone; };
+    // the KEYS by 64; a wave compares 64 of them with kEach of 64
+    constexpr uint32_t kSets = KEYS / 64, kWaves = kOrderThreads / 64 / kSets, kEach = KEYS / kWaves;
+    static_assert(kEach <= 64 && 64 % kEach == 0 && KEYS <= kOrderThreads, "a set's waves share the comparisons");
+    __shared__ uint32_t smaller[kWaves][KEYS], sorted[KEYS], from[KEYS], before[KEYS];
+    const uint32_t set = wave % kSets, part = wave / kSets;
+    const uint32_t mine = key(set * 64 + lane), others = key(part * kEach / 64 * 64 + lane);
+    uint32_t j = run_from + tid;
+    int32_t id[kAtOnce];
+    auto load = [&]() {
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        const uint32_t r = x[k] >> kBlockBits;
-        row[base + first + 64 * k] = r == kMaxVocab ? kNone : r;
-        token[base + first + 64 * k] = r == kMaxVocab ? 0 : base + (x[k] & (kBlock - 1));   // (read, and not used)
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            const uint32_t at = j + k * kOrderThreads;
+            id[k] = ids[at < run_to ? at : run_to - 1];
+        }
+    };
+    load();
+    uint32_t count = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k) {
+        const uint32_t other = __builtin_amdgcn_readlane(others, part * kEach % 64 + k);
+        count += other < mine || (other == mine && part * kEach + k < set * 64 + lane) ? 1 : 0;
+    }
+    smaller[part][set * 64 + lane] = count;
+    __syncthreads();
+    if (part == 0) {
+        uint32_t place = 0;
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) place += smaller[w][set * 64 + lane];
+        sorted[place] = mine;                                // the KEYS in order,
+        from[place] = set * 64 + lane;                       // which they were,
+        before[set * 64 + lane] = 0;                         // and how many others come just before each
+    }
+    __syncthreads();
+    while (j < run_to) {
+        uint32_t limit[kAtOnce], below[kAtOnce] = {};        // how many of the KEYS go before it: rows below `limit`
+        bool counts[kAtOnce];
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            const uint32_t at = j + k * kOrderThreads;
+            counts[k] = at < run_to && at / KEYS != blockIdx.x;
+            limit[k] = row_named(id[k]) + (at < base ? 0 : 1);
+        }
+        j += kAtOnce * kOrderThreads;
+        if (j - tid < run_to) load();
+#pragma unroll
+        for (uint32_t step = KEYS / 2; step > 0; step /= 2)
+#pragma unroll
+            for (uint32_t k = 0; k < kAtOnce; ++k) below[k] |= sorted[below[k] + step - 1] < limit[k] ? step : 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k)
+            if (counts[k] && sorted[below[k]] >= limit[k]) atomicAdd(&before[below[k]], 1u);
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    uint32_t sums[kSets], sum = 0;                           // a lane has kSets that follow each other
+#pragma unroll
+    for (uint32_t k = 0; k < kSets; ++k) sums[k] = sum += before[lane * kSets + k];
+    uint32_t upto = sum;
+    for (uint32_t step = 1; step < 64; step *= 2) {
+        const uint32_t lower = __shfl_up(upto, step);
+        if (lane >= step) upto += lower;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kSets; ++k) {
+        const uint32_t i = lane * kSets + k, r = sorted[i], at = base + from[i];
+        const uint32_t place = at < rows ? run_from + i + (upto - sum) + sums[k] : at;
+        row[place] = r;
+        token[place] = r == kNone ? 0 : at;
     }
 }
 
 // Sorted runs of `length` entries (the last one of all may be shorter), kFanIn of them at a time, to one run.  Of every run
-// SAMPLES entries at equal distances lie in LDS for the first steps of the search: all of them while runs are blocks, of longer
-// ones 1024, and from a distance of 32 on the others are in one cache line.
-template <bool BLOCKS, uint32_t SAMPLES, uint32_t THREADS>
-__global__ __launch_bounds__(THREADS) void merge_runs_kernel(const uint32_t* __restrict__ row, const uint32_t* __restrict__ token,
-                                                             uint32_t entries, uint32_t length, uint32_t* __restrict__ row_out,
-                                                             uint32_t* __restrict__ token_out, uint32_t groups, Zeros zeros) {
+// kSamples entries at equal distances lie in LDS for the first steps of the search; from a distance of 32 on the others are in one
+// cache line.
+template <uint32_t SAMPLES>
+__global__ __launch_bounds__(kMergeThreads) void merge_runs_kernel(const uint32_t* __restrict__ row, const uint32_t* __restrict__ token,
+                                                                   uint32_t entries, uint32_t length, uint32_t* __restrict__ row_out,
+                                                                   uint32_t* __restrict__ token_out, uint32_t groups, Zeros zeros) {
     if (blockIdx.x >= groups) {
         write_zeros(zeros, blockIdx.x - groups);
         return;
     }
-    __shared__ uint32_t sample[kFanIn * SAMPLES];            // the last entry of each stretch
-    static_assert(!BLOCKS || SAMPLES == kBlock, "all entries of a block");
-    const uint32_t i = blockIdx.x * THREADS + threadIdx.x;   // (the number of entries is a multiple of 2048, as is a run's)
-    const uint32_t run = blockIdx.x * THREADS / length, first = run / kFanIn * kFanIn, stretch = BLOCKS ? 1 : length / SAMPLES;
-    uint32_t some[kFanIn * SAMPLES / THREADS];
+    __shared__ uint32_t sample[kFanIn * SAMPLES];           // the last entry of each stretch
+    static_assert(kBlock % kMergeThreads == 0 && kRun % kMergeThreads == 0, "whole workgroups");
+    const uint32_t i = blockIdx.x * kMergeThreads + threadIdx.x;
+    const uint32_t run = blockIdx.x * kMergeThreads / length, first = run / kFanIn * kFanIn, stretch = length / SAMPLES;
+    uint32_t some[kFanIn * SAMPLES / kMergeThreads];
 #pragma unroll
-    for (uint32_t s = 0; s < kFanIn * SAMPLES / THREADS; ++s) {
-        const uint64_t at = (uint64_t)first * length + (uint64_t)(s * THREADS + threadIdx.x + 1) * stretch - 1;
+    for (uint32_t s = 0; s < kFanIn * SAMPLES / kMergeThreads; ++s) {
+        const uint64_t at = (uint64_t)first * length + (uint64_t)(s * kMergeThreads + threadIdx.x + 1) * stretch - 1;
         some[s] = at < entries ? row[at] : kNone;
     }
     const uint32_t r = row[i], t = token[i];
 #pragma unroll
-    for (uint32_t s = 0; s < kFanIn * SAMPLES / THREADS; ++s) sample[s * THREADS + threadIdx.x] = some[s];
+    for (uint32_t s = 0; s < kFanIn * SAMPLES / kMergeThreads; ++s) sample[s * kMergeThreads + threadIdx.x] = some[s];
     __syncthreads();
     uint32_t below[kFanIn] = {};                             // entries that go before this one; the searches go side by side
     uint32_t limit[kFanIn];                                  // those of rows below it; of equal rows earlier runs' entries do
@@ -265,10 +266,9 @@ __global__ __launch_bounds__(THREADS) void merge_runs_kernel(const uint32_t* __r
 #pragma unroll
         for (uint32_t k = 0; k < kFanIn; ++k) below[k] += sample[k * SAMPLES + step - 1 + below[k]] < limit[k] ? step : 0;
     // (all stretches but the last at most are counted: whether that one goes before is for what follows to find)
-    if constexpr (BLOCKS) {
+    if (stretch == 1) {
 #pragma unroll
-        for (uint32_t k = 0; k < kFanIn; ++k)
-            below[k] += sample[k * SAMPLES + below[k]] < limit[k] ? 1 : 0;
+        for (uint32_t k = 0; k < kFanIn; ++k) below[k] += sample[k * SAMPLES + below[k]] < limit[k] ? 1 : 0;
     } else {
 #pragma unroll
         for (uint32_t k = 0; k < kFanIn; ++k) below[k] *= stretch;
@@ -295,13 +295,13 @@ __global__ __launch_bounds__(THREADS) void merge_runs_kernel(const uint32_t* __r
 
 // ---------------------------------------------------------------- gradient: sums
 //
-// A wave takes the runs of equal rows that begin in one piece of 16 entries, in one span of columns, and keeps their sums in
-// registers: grad_out is read once, in rows, and every row of the table is written once, by one wave.  A lane has VEC consecutive
-// columns: four, or one where the table is narrow.  A run that goes on behind its piece is followed by its wave, through the sums of
-// whole windows, which other waves have formed before (a token that makes up 7 % of 65537: 69 windows in 5 batches instead of 4400
-// rows).  Bound by memory: MI355X, 65537 fp32 rows of 2050 into 32001 rows, frequencies 1 / rank, added to what is there: windows 42 us
-// (4.5 TB/s), runs 126 us (4.5 TB/s); 16384 bf16 rows of 2048: runs 21 us.  One token throughout: 98 and 145 us, 18 and 41 us.  grad_out
-// is read without the streaming hint, which loses lines that two slices share (65537 rows of few different tokens: 180 us with it, 128).
+// Sums are kept in registers: grad_out is read once, in rows, and every row of the table is written once, by one wave.  A lane has
+// VEC consecutive columns: four, or one where the table is narrow.  Windows that lie inside one run are summed first, where there
+// are many tokens, so that a frequent token's run is not left to few waves (one that makes up 7 % of 65537: 69 windows instead of 4400
+// rows).  Bound by memory: MI355X, 65537 fp32 rows of 2050 into 32001 rows, frequencies 1 / rank, added to what is there: windows 37 us
+// (4.6 TB/s), runs 117 to 126 us (5.1 to 4.7 TB/s); 16384 bf16 rows of 2048: runs 18 us.  One token throughout: 92 and 33 us, 20 (with
+// zeros) and 10 us.  Small calls wait: 4096 bf16 rows of 1792 of 388, 11 us.  grad_out is read without the streaming hint, which loses
+// lines that two slices share (65537 rows of few different tokens: 180 us with it, 128).
 
 // The lane's columns of a slice.  The last vector of a row whose length is no multiple of four holds fewer: it is read as the
 // four elements that end with the row (`back` elements earlier), and its elements are brought to the front.
@@ -316,22 +316,21 @@ struct Columns {
         back = mine ? VEC - n : 0;
     }
 };
-// Which piece or window (their number is a multiple of eight) and which slice of its columns a wave takes.  A workgroup's waves,
-// up to four, are independent; they and the other workgroups of the same rows follow each other on one XCD, so that lines which two
-// slices share meet in one L2.
+// Which window (their number is a multiple of eight) and which slice of its columns a workgroup takes: those of the same rows
+// follow each other on one XCD, so that lines which two slices share meet in one L2.
 struct Unit {
-    uint32_t item, slice;
+    uint32_t window, slice;
     __device__ __forceinline__ Unit(uint32_t group, uint32_t slices) {
-        const uint32_t waves = blockDim.x / 64, groups = (slices + waves - 1) / waves, place = group / 8;
-        item = place / groups * 8 + group % 8;
-        slice = place % groups * waves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t place = group / 8;
+        window = place / slices * 8 + group % 8;
+        slice = place % slices;
     }
 };
-constexpr uint32_t kMostWaves = 4;
-// Up to so many entries a workgroup's waves take a piece together (below), instead of windows' sums and a wave by itself.  Together /
-// with windows, whole call: 2415 bf16 rows of 1792 of 388: 23.3 / 29.7 us, 4096 of 2048 of 32000: 53.5 / 55.7, 4096 fp32 rows of 256 of
-// 3000: 22.5 / 24.5; 8192 of 2048 of 32000: 60.4 / 59.0, 8192 of 512 of 1000: 34.6 / 28.5, 16000 of 1024 of 500: 57.6 / 33.1.
-constexpr uint32_t kTogetherMost = 4096;
+// Up to so many entries a long run is left to the waves of a workgroup, without windows' sums.  Without / with them, whole call: 2415
+// bf16 rows of 1792 of 388: 12.6 / 13.7 us, 4096 of 2048 of 32000: 47.4 / 49.1, 4096 fp32 rows of 2048 of 700: 16.8 / 19.3 (one token
+// throughout: 59.5 / 19.6); 5135 fp32 rows of 448 of 258: 18.5 / 15.4, 8192 of 512 of 1000: 21.6 / 16.2, 8192 bf16 rows of 2048 of 32000:
+// 55.1 / 52.9.
+constexpr uint32_t kFewEntries = 4096;
 template <int VEC>
 struct Sums {
     float v[VEC];
@@ -353,34 +352,43 @@ __device__ __forceinline__ void add(Sums<VEC>& a, const Sums<VEC>& b) {
     for (int j = 0; j < VEC; ++j) a.v[j] += b.v[j];
 }
 
-constexpr int kPiece = 16;               // entries of a piece: rows of grad_out in flight
-constexpr int kWindow = 64;              // entries that one partial sum covers: those a wave looks at together
-static_assert(kWindow <= 64 && kBlock % kWindow == 0 && kWindow % kPiece == 0, "a wave walks whole windows");
+constexpr int kWindow = 64;              // entries of a workgroup, one a lane; and those that one partial sum covers
+constexpr int kPiece = 8;                // of which a wave has so many: rows in flight (16: 2415 bf16 rows of 1792, 21.2 for 19.5 us)
+constexpr int kSumWaves = kWindow / kPiece;
+constexpr int kFlight = 16;              // rows in flight where a wave has little else to hold
+static_assert(kWindow == 64 && kBlock % (8 * kWindow) == 0, "windows in eights");
 
 // Windows of entries that lie inside one run: their sums, so that a frequent token's run is not left to one wave.
 template <int VEC, class G>
-__global__ __launch_bounds__(kMostWaves * 64) void window_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
+__global__ __launch_bounds__(kWindow / kFlight * 64) void window_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
                                                          const uint32_t* __restrict__ token, int d, int slices,
                                                          float* __restrict__ partial, uint32_t groups, Zeros zeros) {
     if (blockIdx.x >= groups) {
         write_zeros(zeros, blockIdx.x - groups);
         return;
     }
+    constexpr uint32_t kWaves = kWindow / kFlight;
+    __shared__ float parts[kWaves - 1][VEC][64];
     const Unit unit(blockIdx.x, (uint32_t)slices);
-    const uint32_t slice = unit.slice, lane = threadIdx.x & 63, first = unit.item * kWindow;
-    if (slice >= (uint32_t)slices || row[first] != row[first + kWindow - 1] || row[first] == kNone) return;
-    const Columns<VEC> at(d, (int)slice, slices, (int)lane);
-    Sums<VEC> sum = {};
-    for (int e = 0; e < kWindow; e += kPiece) {
-        Sums<VEC> x[kPiece];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = unit.window * kWindow;
+    if (row[first] != row[first + kWindow - 1] || row[first] == kNone) return;
+    const Columns<VEC> at(d, (int)unit.slice, slices, (int)lane);
+    Sums<VEC> x[kFlight];
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) x[k] = load_grad<VEC>(grad, token[first + e + k], d, at);
+    for (int k = 0; k < kFlight; ++k) x[k] = load_grad<VEC>(grad, token[first + wave * kFlight + k], d, at);
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) add(sum, x[k]);
+    for (int k = 1; k < kFlight; ++k) add(x[0], x[k]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+        if (wave > 0) parts[wave - 1][j][lane] = x[0].v[j];
+    __syncthreads();
+    if (wave > 0) return;
+    float* to = partial + (((uint64_t)unit.window * slices + unit.slice) * 64 + lane) * VEC;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        for (uint32_t w = 0; w < kWaves - 1; ++w) x[0].v[j] += parts[w][j][lane];
+        to[j] = x[0].v[j];
     }
-    float* to = partial + (((uint64_t)unit.item * slices + slice) * 64 + lane) * VEC;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) to[j] = sum.v[j];
 }
 
 // Writes a row's columns: scale * sum, added to what is there if asked to.
@@ -408,64 +416,39 @@ __device__ __forceinline__ Sums<VEC> load_row(const O* out, const Columns<VEC>& 
     return s;
 }
 
-// TOGETHER: for few tokens, which leave most of the chip idle and make a launch for windows' sums too dear.  A workgroup's four waves
-// take one piece and slice; the first does what a wave does otherwise, and what goes on behind the piece's window is divided among
-// them, window by window, and joined in their order (runs of 2000 tokens of 300, fp32, d 2048: 22 -> 13 us).
-template <int VEC, bool ADDED, bool TOGETHER, class G, class O>
-__global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
-                                                      const uint32_t* __restrict__ token, const float* __restrict__ partial,
-                                                      uint32_t entries, int d, int slices, float scale,
-                                                      O* __restrict__ out) {
-    uint32_t piece, slice, wave = 0;
-    if constexpr (TOGETHER) {
-        piece = blockIdx.x / (uint32_t)slices;
-        slice = blockIdx.x % (uint32_t)slices;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    } else {
-        const Unit unit(blockIdx.x, (uint32_t)slices);
-        piece = unit.item;
-        slice = unit.slice;
-        if (slice >= (uint32_t)slices) return;
-    }
-    const uint32_t lane = threadIdx.x & 63;
-    // the piece's window, an entry a lane (their number is a multiple of 2048); the piece begins at entry q of it
-    uint32_t e = piece * kPiece / kWindow * kWindow;
-    const uint32_t q = piece * kPiece % kWindow;
-    uint32_t rows = row[e + lane % kWindow], tokens = token[e + lane % kWindow];
-    auto row_at = [&](uint32_t k) { return __builtin_amdgcn_readlane(rows, k); };
-    uint32_t now = q > 0 ? row_at(q - 1) : (e > 0 ? row[e - 1] : kNone);         // the run that `sum` belongs to
-    const uint32_t last = row_at(q + kPiece - 1);
-    if (row_at(q) == kNone || (piece > 0 && last == now)) return;                // nothing begins here
+// A workgroup takes one window in one span of columns, each of its waves a piece, of which every entry's row of grad_out is read once.
+// Runs that begin and end inside a piece are written at once.  A piece's wave has, besides, the sum of its last run so far and that of
+// the entries at its front which belong to a run from an earlier piece: the latter go through LDS to the wave in whose piece
+// that run begins.  The one run that may leave the window is followed by all waves in turn: MANY: by whole windows' sums, else, and
+// in its last window, in pieces; their parts go the same way.
+template <int VEC, bool ADDED, bool MANY, class G, class O>
+__global__ __launch_bounds__(kSumWaves * 64) void row_sums_kernel(const G* __restrict__ grad, const uint32_t* __restrict__ row,
+                                                     const uint32_t* __restrict__ token, const float* __restrict__ partial,
+                                                     uint32_t entries, int d, int slices, float scale, O* __restrict__ out) {
+    __shared__ float parts[2][kSumWaves][VEC][64];
+    const Unit unit(blockIdx.x, (uint32_t)slices);
+    const uint32_t slice = unit.slice;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t e = unit.window * kWindow, q = wave * kPiece;  // the window's first entry, and the piece's in it
+    const uint32_t rows = row[e + lane], tokens = token[e + lane];               // an entry a lane
+    const uint32_t previous = e > 0 ? row[e - 1] : kNone, next = e + kWindow < entries ? row[e + kWindow] : kNone;
+    const uint32_t leaving = __builtin_amdgcn_readlane(rows, kWindow - 1);
+    if (__builtin_amdgcn_readlane(rows, 0) == kNone || (e > 0 && leaving == previous)) return;     // nothing begins here
     const Columns<VEC> at(d, (int)slice, slices, (int)lane);
-    Sums<VEC> sum = {};
     auto out_row = [&](uint32_t r) { return out + (uint64_t)r * (uint64_t)d; };
-    // Rows of grad_out of entries k .. k + 15 of the window at hand; those from `end` on are read as the last one before it.
-    auto load = [&](Sums<VEC> (&x)[kPiece], uint32_t k, uint32_t end) {
+
+    uint32_t r[kPiece];
 #pragma unroll
-        for (uint32_t i = 0; i < kPiece; ++i)
-            x[i] = load_grad<VEC>(grad, __builtin_amdgcn_readlane(tokens, k + i < end ? k + i : end - 1), d, at);
-    };
-    // How far the entries from k on belong to `now`.
-    auto run_end = [&](uint32_t k) {
-        const uint64_t others = k < kWindow ? __ballot(rows != now && lane < kWindow) >> k << k : 0;
-        return others == 0 ? kWindow : (uint32_t)__builtin_ctzll(others);
-    };
-    auto add_run = [&](uint32_t k, uint32_t end) {
-        for (; k < end; k += kPiece) {
-            Sums<VEC> x[kPiece];
-            load(x, k, end);
-#pragma unroll
-            for (uint32_t i = 0; i < kPiece; ++i)
-                if (k + i < end) add(sum, x[i]);
-        }
-    };
-    if (!TOGETHER || wave == 0) {
+    for (uint32_t i = 0; i < kPiece; ++i) r[i] = __builtin_amdgcn_readlane(rows, q + i);
+    const uint32_t before = q > 0 ? __builtin_amdgcn_readlane(rows, q - 1) : previous, last = r[kPiece - 1];
+    const bool from_before = q + e > 0;
+    const bool mine = last != kNone && !(from_before && last == before);         // the last run begins in this piece
+    Sums<VEC> sum = {}, head = {};
+    if (r[0] != kNone && !(e > 0 && last == previous)) {
         Sums<VEC> x[kPiece];
-        uint32_t r[kPiece];
-        load(x, q, q + kPiece);
 #pragma unroll
-        for (uint32_t i = 0; i < kPiece; ++i) r[i] = row_at(q + i);
-        // x becomes the sums of the runs up to here: those that end inside the piece are written, unless they began before it
+        for (uint32_t i = 0; i < kPiece; ++i) x[i] = load_grad<VEC>(grad, __builtin_amdgcn_readlane(tokens, q + i), d, at);
+        // x becomes the sums of the runs up to here
 #pragma unroll
         for (uint32_t i = 1; i < kPiece; ++i)
             if (r[i] == r[i - 1]) {
@@ -473,96 +456,94 @@ __global__ __launch_bounds__(kMostWaves * 64) void row_sums_kernel(const G* __re
                 add(upto, x[i]);
                 x[i] = upto;
             }
-        auto written = [&](uint32_t i) { return r[i] != now && r[i] != kNone && r[i] != last; };
 #pragma unroll
-        for (uint32_t half = 0; half < kPiece; half += kPiece / 2) {
-            Sums<VEC> was[kPiece / 2];
-            if (ADDED && at.n > 0)
+        for (uint32_t i = 0; i < kPiece; ++i)
+            if (r[i] == before) head = x[i];
+        auto written = [&](uint32_t i) { return r[i] != r[i + 1] && r[i] != kNone && !(from_before && r[i] == before); };
+        if (at.n > 0)
 #pragma unroll
-                for (uint32_t i = 0; i < kPiece / 2; ++i)
-                    if (i + half + 1 < kPiece && r[half + i] != r[half + i + 1] && written(half + i))
-                        was[i] = load_row<VEC>(out_row(r[half + i]), at);
-            if (at.n > 0)
+            for (uint32_t half = 0; half < kPiece; half += kPiece / 2) {
+                Sums<VEC> was[kPiece / 2];
 #pragma unroll
                 for (uint32_t i = 0; i < kPiece / 2; ++i)
-                    if (i + half + 1 < kPiece && r[half + i] != r[half + i + 1] && written(half + i))
+                    if (ADDED && half + i + 1 < kPiece && written(half + i)) was[i] = load_row<VEC>(out_row(r[half + i]), at);
+#pragma unroll
+                for (uint32_t i = 0; i < kPiece / 2; ++i)
+                    if (half + i + 1 < kPiece && written(half + i))
                         store_row<VEC>(out_row(r[half + i]), at, x[half + i], scale, ADDED ? &was[i] : nullptr);
-        }
+            }
         sum = x[kPiece - 1];
     }
-    if (last == kNone) return;
-    now = last;
-    uint32_t end = run_end(q + kPiece);
-    if (!TOGETHER || wave == 0) add_run(q + kPiece, end);
-    if constexpr (TOGETHER) {
-        for (uint32_t w = e + (wave + 1) * kWindow; end == kWindow && w < entries; w += kMostWaves * kWindow) {
-            rows = row[w + lane % kWindow];
-            tokens = token[w + lane % kWindow];
-            const uint32_t stop = run_end(0);
-            add_run(0, stop);
-            if (stop < kWindow) break;
-        }
-        if (end == kWindow) {                                // (the same for all four)
-            __shared__ float parts[kMostWaves - 1][VEC][64];
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (wave > 0) parts[wave - 1][j][lane] = sum.v[j];
-            __syncthreads();
-            for (uint32_t w = 0; w < kMostWaves - 1; ++w) {
-                Sums<VEC> x;
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) x.v[j] = parts[w][j][lane];
-                add(sum, x);
-            }
-        }
-        if (wave > 0) return;
-    } else {
-        while (end == kWindow && (e += kWindow) < entries) { // the run goes on in the next window, and in whole ones, up to 16 at a time
-            const uint32_t w = e + lane * kWindow;
-            const bool whole = lane < kPiece && w < entries && row[w] == now && row[w + kWindow - 1] == now;
-            const uint32_t n = (uint32_t)__builtin_ctzll(~__ballot(whole));
-            if (n > 0) {
+    const bool shared = leaving != kNone && next == leaving; // (its run begins in this window)
+    Sums<VEC> part = {};
+    if (shared) {
+        uint32_t from = e + kWindow, stop = from, n;
+        do {                                                 // windows that begin with it
+            const uint32_t w = stop + lane * kWindow;
+            const uint64_t others = __ballot(w >= entries || row[w] != leaving);
+            n = others == 0 ? 64 : (uint32_t)__builtin_ctzll(others);
+            stop += n * kWindow;
+        } while (n == 64);
+        const uint64_t others = __ballot(row[stop - kWindow + lane] != leaving);
+        if (others != 0) stop -= kWindow - (uint32_t)__builtin_ctzll(others);
+        if constexpr (MANY) {
+            const uint32_t whole = (stop - from) / kWindow;
+            for (uint32_t b = wave; b < whole; b += kPiece * kSumWaves) {
                 Sums<VEC> x[kPiece];
 #pragma unroll
                 for (uint32_t i = 0; i < kPiece; ++i) {
-                    const float* from = partial + ((((uint64_t)(e / kWindow) + (i < n ? i : n - 1)) * slices + slice) * 64 + lane) * VEC;
+                    const uint32_t w = b + i * kSumWaves < whole ? b + i * kSumWaves : whole - 1;
+                    const float* of = partial + (((uint64_t)(from / kWindow + w) * slices + slice) * 64 + lane) * VEC;
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) x[i].v[j] = from[j];
+                    for (int j = 0; j < VEC; ++j) x[i].v[j] = of[j];
                 }
 #pragma unroll
                 for (uint32_t i = 0; i < kPiece; ++i)
-                    if (i < n) add(sum, x[i]);
-                e += (n - 1) * kWindow;
-                continue;
+                    if (b + i * kSumWaves < whole) add(part, x[i]);
             }
-            rows = row[e + lane % kWindow];
-            tokens = token[e + lane % kWindow];
-            end = run_end(0);
-            add_run(0, end);
+            from += whole * kWindow;
+        }
+        // a wave takes every so manieth piece of kRows entries, and has the tokens of some at a time in its lanes
+        constexpr uint32_t kRows = MANY ? kPiece : kFlight, kRound = kRows * kSumWaves;
+        for (uint32_t b = from + wave * kRows; b < stop; b += 64 / kRows * kRound) {
+            const uint32_t entry = b + lane / kRows * kRound + lane % kRows;
+            const uint32_t its = token[entry < stop ? entry : stop - 1];
+#pragma unroll 1
+            for (uint32_t k = 0; k < 64 / kRows && b + k * kRound < stop; ++k) {
+                Sums<VEC> x[kRows];
+#pragma unroll
+                for (uint32_t i = 0; i < kRows; ++i) x[i] = load_grad<VEC>(grad, __builtin_amdgcn_readlane(its, k * kRows + i), d, at);
+#pragma unroll
+                for (uint32_t i = 0; i < kRows; ++i)
+                    if (b + k * kRound + i < stop) add(part, x[i]);
+            }
         }
     }
-    if (at.n > 0) {
-        Sums<VEC> was;
-        if (ADDED) was = load_row<VEC>(out_row(now), at);
-        store_row<VEC>(out_row(now), at, sum, scale, ADDED ? &was : nullptr);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        parts[0][wave][j][lane] = head.v[j];
+        if (shared) parts[1][wave][j][lane] = part.v[j];
     }
+    __syncthreads();
+    if (!mine || at.n == 0) return;
+    auto add_part = [&](uint32_t which, uint32_t w) {
+        Sums<VEC> x;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x.v[j] = parts[which][w][j][lane];
+        add(sum, x);
+    };
+    Sums<VEC> was;
+    if (ADDED) was = load_row<VEC>(out_row(last), at);
+    for (uint32_t w = wave + 1; w < kSumWaves && __builtin_amdgcn_readlane(rows, w * kPiece) == last; ++w) add_part(0, w);
+    if (shared && last == leaving)
+        for (uint32_t w = 0; w < kSumWaves; ++w) add_part(1, w);
+    store_row<VEC>(out_row(last), at, sum, scale, ADDED ? &was : nullptr);
 }
 
 // ---------------------------------------------------------------- host side
 
 int vec_of(int d) { return d < 256 ? 1 : 4; }
 int slices_of(int d) { return ((d + vec_of(d) - 1) / vec_of(d) + 63) / 64; }
-// How the workgroups of the sums take a row's slices: `groups` of them, of `waves` waves.
-struct Slices {
-    uint32_t count, groups, waves, lanes;
-    explicit Slices(int d) {
-        count = (uint32_t)slices_of(d);
-        groups = (count + kMostWaves - 1) / kMostWaves;
-        waves = (count + groups - 1) / groups;
-        lanes = groups * waves * 64;
-    }
-};
-
 // The workspace: entries (rows and tokens) of two stages of the sort in turn, the windows' sums.
 struct GradSpace {
     int64_t entries, row[2], token[2], partial, bytes;
@@ -578,10 +559,8 @@ struct GradSpace {
 };
 
 bool grad_sizes_fit(int64_t rows, int vocab, int d) {
-    if (rows < 0 || rows >= (int64_t)1 << 30 || vocab < 1 || vocab >= (int)kMaxVocab || d < 1 || d >= 1 << 24) return false;
-    const int64_t entries = (rows + kBlock - 1) / kBlock * kBlock;
-    const int64_t lanes = entries > kTogetherMost ? Slices(d).lanes : Slices(d).count * kMostWaves * 64;       // for a piece
-    return entries / kPiece * lanes < (int64_t)1 << 32;       // (of one launch)
+    if (rows < 0 || rows >= (int64_t)1 << 30 || vocab < 1 || d < 1 || d >= 1 << 24) return false;
+    return rows * (d < 64 ? 64 : d) < (int64_t)1 << 34;       // (a launch has fewer than 2^32 lanes)
 }
 
 }  // namespace
@@ -645,9 +624,8 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     const GradSpace space(rows, d);
     if (ws_bytes < space.bytes) return SPLC_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const Slices slices(d);
-    const uint32_t entries = (uint32_t)space.entries, blocks = entries / kBlock;
-    const bool merged = blocks > 1, many = entries > kTogetherMost;
+    const uint32_t slices = (uint32_t)slices_of(d);
+    const uint32_t entries = (uint32_t)space.entries, windows = entries / kWindow;
     uint32_t *row[2], *token[2];
     for (int k = 0; k < 2; ++k) {
         row[k] = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + space.row[k]);
@@ -662,7 +640,9 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     const uint64_t vectors = accumulate ? 0 : (size - head) * element / 16;
     const uint64_t tail = size - head - vectors * 16 / element;
     uint4* vector = reinterpret_cast<uint4*>(static_cast<char*>(grad_table) + head * element);
-    const uint64_t sort_share = merged ? vectors / 2 : vectors, merge_share = many ? vectors / 4 : vectors - sort_share;
+    const bool many = entries > kFewEntries, merged = many && (entries > kDirect || vectors > kFewZeros);
+    const uint32_t run = merged ? kRun : kDirect;
+    const uint64_t sort_share = many ? vectors / 2 : vectors, merge_share = merged ? vectors / 4 : 0;
     const Zeros shares[3] = {{vector, sort_share}, {vector + sort_share, merge_share},
                              {vector + sort_share + merge_share, vectors - sort_share - merge_share}};
     auto groups_of = [](const Zeros& z) {
@@ -673,43 +653,47 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
     auto sort = [&](auto result) {
         using O = decltype(result);
         const uint32_t more = accumulate ? 0 : groups_of(shares[0]) + (shares[0].vectors == 0 ? 1 : 0);
-        if (blocks + more > 0)
-            hipLaunchKernelGGL(sort_tokens_kernel<O>, dim3(blocks + more), dim3(kSortThreads), 0, st, token_ids, (uint32_t)rows, vocab,
-                               ignore_id, blocks, row[0], token[0], shares[0], static_cast<O*>(grad_table), size, (uint32_t)head,
-                               (uint32_t)tail);
+        auto order = [&](auto kernel, uint32_t keys) {
+            if (entries / keys + more > 0)
+                hipLaunchKernelGGL(kernel, dim3(entries / keys + more), dim3(kOrderThreads), 0, st, token_ids, (uint32_t)rows, vocab,
+                                   ignore_id, run, entries / keys, row[0], token[0], shares[0], static_cast<O*>(grad_table), size,
+                                   (uint32_t)head, (uint32_t)tail);
+        };
+        if (merged) order(order_tokens_kernel<128, O>, 128);
+        else order(order_tokens_kernel<64, O>, 64);
     };
     if (table_dtype == SPLC_F32) sort(float{});
     else sort(uint16_t{});
     if (rows == 0) return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
     int in = 0;
-    for (uint64_t length = kBlock; length < entries; length *= kFanIn, in ^= 1) {
-        const bool blocks_yet = length == kBlock;
-        const Zeros share = blocks_yet ? shares[1] : Zeros{nullptr, 0};
-        auto merge = [&](auto kernel, uint32_t threads) {
-            hipLaunchKernelGGL(kernel, dim3(entries / threads + groups_of(share)), dim3(threads), 0, st, row[in], token[in], entries,
-                               (uint32_t)length, row[in ^ 1], token[in ^ 1], entries / threads, share);
+    for (uint64_t length = run; length < entries; length *= kFanIn, in ^= 1) {
+        const Zeros share = length == run ? shares[1] : Zeros{nullptr, 0};
+        const uint32_t groups = entries / kMergeThreads;
+        auto merge = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(groups + groups_of(share)), dim3(kMergeThreads), 0, st, row[in], token[in], entries,
+                               (uint32_t)length, row[in ^ 1], token[in ^ 1], groups, share);
         };
-        if (blocks_yet) merge(merge_runs_kernel<true, kBlock, 512>, 512);
-        else merge(merge_runs_kernel<false, 1024, 512>, 512);
+        if (length == kRun) merge(merge_runs_kernel<2048>);
+        else merge(merge_runs_kernel<1024>);
     }
     auto sums = [&](auto vec, auto gradient, auto result) {
         constexpr int VEC = decltype(vec)::value;
         using G = decltype(gradient);
         using O = decltype(result);
-        const uint32_t window_groups = entries / kWindow * slices.groups;
+        const uint32_t groups = windows * slices;
         if (many)
-            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(window_groups + groups_of(shares[2])), dim3(slices.waves * 64), 0, st,
-                               static_cast<const G*>(grad_out), row[in], token[in], d, (int)slices.count, partial, window_groups,
+            hipLaunchKernelGGL((window_sums_kernel<VEC, G>), dim3(groups + groups_of(shares[2])), dim3(kWindow / kFlight * 64), 0, st,
+                               static_cast<const G*>(grad_out), row[in], token[in], d, (int)slices, partial, groups,
                                shares[2]);
-        auto launch = [&](auto kernel, uint32_t groups, uint32_t waves) {
-            hipLaunchKernelGGL(kernel, dim3(groups), dim3(waves * 64), 0, st, static_cast<const G*>(grad_out), row[in], token[in], partial,
-                               entries, d, (int)slices.count, scale, static_cast<O*>(grad_table));
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(groups), dim3(kSumWaves * 64), 0, st,
+                               static_cast<const G*>(grad_out), row[in], token[in], partial, entries, d, (int)slices, scale,
+                               static_cast<O*>(grad_table));
         };
-        const uint32_t pieces = entries / kPiece;
-        if (many && accumulate) launch(row_sums_kernel<VEC, true, false, G, O>, pieces * slices.groups, slices.waves);
-        else if (many) launch(row_sums_kernel<VEC, false, false, G, O>, pieces * slices.groups, slices.waves);
-        else if (accumulate) launch(row_sums_kernel<VEC, true, true, G, O>, pieces * slices.count, kMostWaves);
-        else launch(row_sums_kernel<VEC, false, true, G, O>, pieces * slices.count, kMostWaves);
+        if (many && accumulate) launch(row_sums_kernel<VEC, true, true, G, O>);
+        else if (many) launch(row_sums_kernel<VEC, false, true, G, O>);
+        else if (accumulate) launch(row_sums_kernel<VEC, true, false, G, O>);
+        else launch(row_sums_kernel<VEC, false, false, G, O>);
     };
     auto by_type = [&](auto vec) {
         if (grad_dtype == SPLC_F32 && table_dtype == SPLC_F32) sums(vec, float{}, float{});

@@ -124,7 +124,7 @@ def test_gradient_of_few_tokens(rows, vocab, d):
 
 @pytest.mark.parametrize("rows,vocab,d", [(2048, 4000, 260), (4097, 300, 513), (16384, 32000, 64), (16383, 2000, 300), (16385, 2561, 257),
                                           (40000, 999, 65), (33000, 9000, 270), (50000, 3, 258), (2049, 40, 64),
-                                          (65537, 700, 80), (140000, 5000, 66), (4096, 700, 300)])
+                                          (65537, 700, 80), (140000, 5000, 66), (4096, 700, 300), (4097, 33000, 514), (16384, 66000, 260)])
 @pytest.mark.parametrize("how", ["text", "same", "spread"])
 def test_gradient_of_many_tokens(rows, vocab, d, how):
     """Long runs of one token, several blocks of the sort, one and two rounds of merging."""
@@ -160,7 +160,7 @@ def test_every_token_ignored_and_rows_with_nan(rows, vocab, d, accumulate):
     assert torch.isnan(table).nonzero().tolist() == [[(rows - 1) % vocab, d - 1]]
 
 
-@pytest.mark.parametrize("rows,entries,stage", [(5, 2048, 0), (2048, 2048, 0), (2049, 4096, 1), (16384 + 7, 18432, 0)])
+@pytest.mark.parametrize("rows,entries,stage", [(5, 512, 0), (2048, 2048, 0), (2049, 2560, 0), (16384, 16384, 0), (16384 + 7, 16896, 0)])
 def test_no_entry_of_the_order_names_a_token_that_is_not_there(rows, entries, stage):
     """The workspace holds the order of the tokens ([rows, tokens] of two stages): every entry's token is one of the call's, also
     of those that only fill a block, whose rows of grad_out are read like the others'."""
@@ -244,7 +244,7 @@ def test_refusals():
     for call in (lambda: B.sparseloco_embedding_lookup(table, ids, x, scale=float("nan")),
                  lambda: B.sparseloco_embedding_grad(x, ids, table, ws, scale=float("inf")),
                  lambda: B.sparseloco_embedding_grad(x, ids, table, ws[:8]),
-                 lambda: B.embedding_grad_workspace(8, 2 ** 21 - 1, 16), lambda: B.embedding_grad_workspace(8, 0, 16),
+                 lambda: B.embedding_grad_workspace(2 ** 28, 5, 16), lambda: B.embedding_grad_workspace(8, 0, 16),
                  lambda: B.embedding_grad_workspace(-1, 5, 16)):
         with pytest.raises(B.SparseLoCoError) as e:
             call()
