@@ -18,25 +18,18 @@ using namespace splc;
 
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(uint16_t* p, float v) { *p = (uint16_t)bf16_pair(v, v); }
-// n (1..4) elements at p.
+// The last n of v's elements at p.
 template <class T>
-__device__ __forceinline__ float4 load_some(const T* p, int n) {
-    if (n == 4) return widened(cached_load4(p));
-    float4 v = make_float4(widened(p[0]), 0.f, 0.f, 0.f);
-    if (n > 1) v.y = widened(p[1]);
-    if (n > 2) v.z = widened(p[2]);
-    return v;
-}
-template <class T>
-__device__ __forceinline__ void store_some(T* p, int n, float4 v) {
+__device__ __forceinline__ void store_last(T* p, int n, float4 v) {
     if (n == 4) {
         stream_store4(p, v);
         return;
     }
-    store1(p, v.x);
-    if (n > 1) store1(p + 1, v.y);
-    if (n > 2) store1(p + 2, v.z);
+    if (n == 3) store1(p + n - 3, v.y);
+    if (n > 1) store1(p + n - 2, v.z);
+    store1(p + n - 1, v.w);
 }
+__device__ __forceinline__ float4 plus(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 __device__ __forceinline__ int row_of(int32_t id, int vocab) { return id < 0 ? 0 : (id < vocab ? id : vocab - 1); }
 
 // ---------------------------------------------------------------- lookup
@@ -50,9 +43,10 @@ constexpr int64_t kMostTurns = 1 << 21;  // (a launch has fewer than 2^32 lanes)
 // every table row and of PosEmbed, and holds four times as many of them.  But a span is 1 to 2 KB of a row where there are several,
 // since waves that read less of it at once wait longer than they read.  MI355X, 16384 tokens of 32000, d 2048, both fp32 tables and
 // positions to bf16, 1 / 2 / 4 / 8 spans: 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be done without, 4.1 TB/s; a copy reaches
-// 4.8); 65536 of 50304, d 768, bf16, 1 / 2 / 4 spans: 31.0 / 43.0 / 64.8.  out without the streaming hint: 45.0 instead of 40.1.
+// 4.8); 65536 of 50304, d 768, bf16: 23.9 (in 1 / 2 / 4 spans, when bf16 vectors were still widened as they came in, which made every
+// load wait for the one before: 31.0 / 43.0 / 64.8).  out without the streaming hint: 45.0 instead of 40.1.
 // NARROW: rows of at most 128 columns, of which a wave takes as many at once as it has `lanes` lanes for (22817 tokens, d 106: 8.0 -> 5.5
-// us; 65536, d 64: 18.9 -> 6.4, and 5.0 with four times as many).
+// us; 65536, d 64: 18.9 -> 6.4, and 4.7 with four times as many).
 template <bool NARROW, int ROWS, class T, class O>
 __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table, const T* __restrict__ t_perp,
                                                      const int32_t* __restrict__ ids, int vocab, const T* __restrict__ pos,
@@ -74,26 +68,41 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T* __restrict__ table
             p[r] = pos ? pos + (int64_t)((uint32_t)at % (uint32_t)seq) * d : nullptr;
         }
         for (int c = span * width + lane * 4; c < end; c += 256 * COLS) {
-            float4 x[ROWS * COLS], y[ROWS * COLS], z[ROWS * COLS];
+            decltype(cached_load4(table)) x[ROWS * COLS], y[ROWS * COLS], z[ROWS * COLS];        // as they lie in memory
 #pragma unroll
             for (int k = 0; k < ROWS * COLS; ++k) {
-                const int at = c + 256 * (k % COLS), n = d - at < 4 ? d - at : 4, r = k / COLS;
+                const int at = c + 256 * (k % COLS), r = k / COLS, four = at + 4 <= d ? at : d - 4;     // (the row's last four)
                 if (at >= end) continue;
-                x[k] = load_some(table + from[r] + at, n);
-                if (t_perp) y[k] = load_some(t_perp + from[r] + at, n);
-                if (pos) z[k] = load_some(p[r] + at, n);
+                x[k] = cached_load4(table + from[r] + four);
+                if (t_perp) y[k] = cached_load4(t_perp + from[r] + four);
+                if (pos) z[k] = cached_load4(p[r] + four);
             }
 #pragma unroll
             for (int k = 0; k < ROWS * COLS; ++k) {
                 const int at = c + 256 * (k % COLS), n = d - at < 4 ? d - at : 4, r = k / COLS;
                 if (at >= end || row + r >= rows) continue;
-                float4 v = x[k];
-                if (t_perp) v = make_float4(v.x + y[k].x, v.y + y[k].y, v.z + y[k].z, v.w + y[k].w);
+                float4 v = widened(x[k]);
+                if (t_perp) v = plus(v, widened(y[k]));
                 v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
-                if (pos) v = make_float4(v.x + z[k].x, v.y + z[k].y, v.z + z[k].z, v.w + z[k].w);
-                store_some(out + (row + r) * d + at, n, v);
+                if (pos) v = plus(v, widened(z[k]));
+                store_last(out + (row + r) * d + at, n, v);
             }
         }
+    }
+}
+
+// Rows of fewer than four columns: an element a lane.
+template <class T, class O>
+__global__ __launch_bounds__(256) void lookup_short_kernel(const T* __restrict__ table, const T* __restrict__ t_perp,
+                                                           const int32_t* __restrict__ ids, int vocab, const T* __restrict__ pos,
+                                                           int seq, float scale, O* __restrict__ out, int64_t rows, int d) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * d; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / d, c = i % d, at = (int64_t)row_of(ids[row], vocab) * d + c;
+        float v = widened(table[at]);
+        if (t_perp) v += widened(t_perp[at]);
+        v *= scale;
+        if (pos) v += widened(pos[(int64_t)((uint32_t)row % (uint32_t)seq) * d + c]);
+        store1(out + i, v);
     }
 }
 
@@ -304,7 +313,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_runs_kernel(const uint32_
 // lines that two slices share (65537 rows of few different tokens: 180 us with it, 128).
 
 // The lane's columns of a slice.  The last vector of a row whose length is no multiple of four holds fewer: it is read as the
-// four elements that end with the row (`back` elements earlier), and its elements are brought to the front.
+// four elements that end with the row (`back` elements earlier), of which the last ones are the lane's.
 template <int VEC>
 struct Columns {
     int col, n, back;
@@ -395,11 +404,9 @@ __global__ __launch_bounds__(kWindow / kFlight * 64) void window_sums_kernel(con
 template <int VEC, class O>
 __device__ __forceinline__ void store_row(O* out, const Columns<VEC>& at, Sums<VEC> s, float scale, const Sums<VEC>* was) {
     if constexpr (VEC == 4) {
-        if (at.back & 1) { s.v[0] = s.v[1]; s.v[1] = s.v[2]; s.v[2] = s.v[3]; }
-        if (at.back & 2) { s.v[0] = s.v[2]; s.v[1] = s.v[3]; }
         float4 x = make_float4(s.v[0] * scale, s.v[1] * scale, s.v[2] * scale, s.v[3] * scale);
-        if (was) x = make_float4(was->v[0] + x.x, was->v[1] + x.y, was->v[2] + x.z, was->v[3] + x.w);
-        store_some(out + at.col, at.n, x);
+        if (was) x = plus(make_float4(was->v[0], was->v[1], was->v[2], was->v[3]), x);
+        store_last(out + at.col, at.n, x);
     } else {
         store1(out + at.col, was ? was->v[0] + s.v[0] * scale : s.v[0] * scale);
     }
@@ -408,7 +415,7 @@ template <int VEC, class O>
 __device__ __forceinline__ Sums<VEC> load_row(const O* out, const Columns<VEC>& at) {
     Sums<VEC> s;
     if constexpr (VEC == 4) {
-        const float4 x = at.n == 4 ? widened(stream_load4(out + at.col)) : load_some(out + at.col, at.n);
+        const float4 x = widened(stream_load4(out + at.col - at.back));
         s.v[0] = x.x; s.v[1] = x.y; s.v[2] = x.z; s.v[3] = x.w;
     } else {
         s.v[0] = widened(out[at.col]);
@@ -590,14 +597,15 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
     auto launch = [&](auto element, auto result) {
         using T = decltype(element);
         using O = decltype(result);
-        auto with = [&](auto kernel) {
+        auto with = [&](auto kernel, auto... layout) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, static_cast<hipStream_t>(stream),
                                static_cast<const T*>(table), static_cast<const T*>(t_perp), token_ids, vocab,
-                               static_cast<const T*>(pos_embed), seq_len, scale, static_cast<O*>(out), rows, d, spans, width, lanes);
+                               static_cast<const T*>(pos_embed), seq_len, scale, static_cast<O*>(out), rows, d, layout...);
         };
-        if (lanes < 64) with(lookup_kernel<true, 4, T, O>);
-        else if (each == 4) with(lookup_kernel<false, 4, T, O>);
-        else with(lookup_kernel<false, 1, T, O>);
+        if (d < 4) with(lookup_short_kernel<T, O>);
+        else if (lanes < 64) with(lookup_kernel<true, 4, T, O>, spans, width, lanes);
+        else if (each == 4) with(lookup_kernel<false, 4, T, O>, spans, width, lanes);
+        else with(lookup_kernel<false, 1, T, O>, spans, width, lanes);
     };
     if (table_dtype == SPLC_F32 && out_dtype == SPLC_F32) launch(float{}, float{});
     else if (table_dtype == SPLC_F32) launch(float{}, uint16_t{});

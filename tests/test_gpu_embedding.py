@@ -201,8 +201,9 @@ def test_gradient_against_differences():
         assert (loss(up) - loss(down)) / 4.0 == grad[v, c].item()
 
 
-def test_a_larger_workspace_a_stream_and_a_graph():
-    rows, vocab, d = 5000, 700, 257
+@pytest.mark.parametrize("rows", [5000, 20000])
+def test_a_larger_workspace_a_stream_and_a_graph(rows):
+    vocab, d = 700, 257
     rng = np.random.default_rng(4)
     ws = B.embedding_grad_workspace(4 * rows, vocab, d)
     grad, ids = torch.empty(rows, d, device="cuda"), torch.empty(rows, dtype=torch.int32, device="cuda")
