@@ -30,7 +30,7 @@ __device__ __forceinline__ void store_last(T* p, int n, float4 v) {
     store1(p + n - 1, v.w);
 }
 __device__ __forceinline__ float4 plus(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
-__device__ __forceinline__ int row_of(int32_t id, int vocab) { return id < 0 ? 0 : (id < vocab ? id : vocab - 1); }
+__device__ __forceinline__ int row_of(int32_t id, int vocab) { return max(0, min(id, vocab - 1)); }
 
 // ---------------------------------------------------------------- lookup
 
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256) void lookup_short_kernel(const T* __restrict__
 // Where the table is written whole, its zeros are written by further workgroups of these launches, which have little else to
 // do with the memory; rows that have tokens are written again later.
 //
-// MI355X: 64 tokens 3.1 us, 4096 at once 4.8, 16384 9.4; 65537 in runs 8.6, merged in 5.9 and 8.7, of which 4 are the launch and a chain
+// MI355X: 64 tokens 3.1 us, 4096 at once 4.5, 16384 8.5; 65537 in runs 8.7, merged in 5.9 and 8.7, of which 4 are the launch and a chain
 // of loads.  Bound by the vector ALU and LDS, which take every token through 7 (8) steps of search for every 64 (128) others of its run.
 
 constexpr uint32_t kNone = 0x7FFFFFFFu;
@@ -145,6 +145,8 @@ __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group) {
 // finds for every other of the run before which of them it goes, by binary search; the numbers of those add up to places.
 // 64 where that gives few workgroups, 128 in runs of kRun (65537 tokens: 10.8 and 8.6 us, 256: 13.1).
 constexpr uint32_t kAtOnce = 4;                              // searches of a lane side by side
+constexpr uint32_t kCopies = 8;                              // of a count, by lanes: those that add to the same one wait for each other
+                                                             // (one token 16384 times: 19.4 -> 7.5 us, frequencies 1 / rank 9.2 -> 8.5)
 template <uint32_t KEYS, class O>
 __global__ __launch_bounds__(kOrderThreads) void order_tokens_kernel(const int32_t* __restrict__ ids, uint32_t rows, int vocab,
                                                                      int32_t ignore_id, uint32_t run, uint32_t groups,
@@ -172,8 +174,8 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens_kernel(const int32
     auto key = [&](uint32_t i) { return base + i < rows ? row_named(ids[base + i]) : kNone; };
     // the KEYS by 64; a wave compares 64 of them with kEach of 64
     constexpr uint32_t kSets = KEYS / 64, kWaves = kOrderThreads / 64 / kSets, kEach = KEYS / kWaves;
-    static_assert(kEach <= 64 && 64 % kEach == 0 && KEYS <= kOrderThreads, "a set's waves share the comparisons");
-    __shared__ uint32_t smaller[kWaves][KEYS], sorted[KEYS], from[KEYS], before[KEYS];
+    static_assert(kEach <= 64 && 64 % kEach == 0 && KEYS * kCopies <= kOrderThreads, "a set's waves share the comparisons");
+    __shared__ uint32_t smaller[kWaves][KEYS], sorted[KEYS], from[KEYS], before[KEYS * kCopies];
     const uint32_t set = wave % kSets, part = wave / kSets;
     const uint32_t mine = key(set * 64 + lane), others = key(part * kEach / 64 * 64 + lane);
     uint32_t j = run_from + tid;
@@ -193,40 +195,47 @@ __global__ __launch_bounds__(kOrderThreads) void order_tokens_kernel(const int32
         count += other < mine || (other == mine && part * kEach + k < set * 64 + lane) ? 1 : 0;
     }
     smaller[part][set * 64 + lane] = count;
+    if (tid < KEYS * kCopies) before[tid] = 0;               // how many others come just before each key
     __syncthreads();
     if (part == 0) {
         uint32_t place = 0;
 #pragma unroll
         for (uint32_t w = 0; w < kWaves; ++w) place += smaller[w][set * 64 + lane];
         sorted[place] = mine;                                // the KEYS in order,
-        from[place] = set * 64 + lane;                       // which they were,
-        before[set * 64 + lane] = 0;                         // and how many others come just before each
+        from[place] = set * 64 + lane;                       // and which they were
     }
     __syncthreads();
     while (j < run_to) {
-        uint32_t limit[kAtOnce], below[kAtOnce] = {};        // how many of the KEYS go before it: rows below `limit`
-        bool counts[kAtOnce];
+        // how many of the KEYS go before it, those of rows below `limit`: four bytes for each
+        uint32_t limit[kAtOnce], below[kAtOnce] = {};
 #pragma unroll
         for (uint32_t k = 0; k < kAtOnce; ++k) {
             const uint32_t at = j + k * kOrderThreads;
-            counts[k] = at < run_to && at / KEYS != blockIdx.x;
-            limit[k] = row_named(id[k]) + (at < base ? 0 : 1);
+            limit[k] = at < run_to && at / KEYS != blockIdx.x ? row_named(id[k]) + (at < base ? 0 : 1) : ~0u;      // (~0: all)
         }
         j += kAtOnce * kOrderThreads;
         if (j - tid < run_to) load();
+        auto key_at = [&](uint32_t bytes) { return *reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(sorted) + bytes); };
 #pragma unroll
         for (uint32_t step = KEYS / 2; step > 0; step /= 2)
 #pragma unroll
-            for (uint32_t k = 0; k < kAtOnce; ++k) below[k] |= sorted[below[k] + step - 1] < limit[k] ? step : 0;
+            for (uint32_t k = 0; k < kAtOnce; ++k) below[k] |= key_at(below[k] + (step - 1) * 4) < limit[k] ? step * 4 : 0;
+        bool before_one[kAtOnce];
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) before_one[k] = key_at(below[k]) >= limit[k];
 #pragma unroll
         for (uint32_t k = 0; k < kAtOnce; ++k)
-            if (counts[k] && sorted[below[k]] >= limit[k]) atomicAdd(&before[below[k]], 1u);
+            if (before_one[k]) atomicAdd(&before[below[k] / 4 * kCopies + lane % kCopies], 1u);
     }
     __syncthreads();
     if (wave > 0) return;
     uint32_t sums[kSets], sum = 0;                           // a lane has kSets that follow each other
 #pragma unroll
-    for (uint32_t k = 0; k < kSets; ++k) sums[k] = sum += before[lane * kSets + k];
+    for (uint32_t k = 0; k < kSets; ++k) {
+#pragma unroll
+        for (uint32_t c = 0; c < kCopies; ++c) sum += before[(lane * kSets + k) * kCopies + c];
+        sums[k] = sum;
+    }
     uint32_t upto = sum;
     for (uint32_t step = 1; step < 64; step *= 2) {
         const uint32_t lower = __shfl_up(upto, step);
