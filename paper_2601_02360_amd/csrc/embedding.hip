@@ -34,13 +34,13 @@ __device__ __forceinline__ int row_of(int32_t id, int vocab) { return max(0, min
 
 // ---------------------------------------------------------------- lookup
 
-constexpr int64_t kMostTurns = 1 << 21;  // (a launch has fewer than 2^32 lanes)
+constexpr int64_t kMostTurns = 1 << 20;  // (a launch has fewer than 2^32 lanes)
 
 // Bound by memory: rows of the table in the order of the tokens, and out.  A wave takes ROWS tokens in one span of columns, and two
 // to four vectors of every array are in flight: two of one row, or, of spans of at most 256 columns, one of four (65536 tokens of
 // 50304, d 256, bf16: 15.4 -> 11.7 us; d 150, fp32, two tables: 18.0 -> 14.3).
 // Workgroups go to the eight XCDs round-robin by number, and spans go with them: with four spans an XCD's L2 is asked for one fourth of
-// every table row and of PosEmbed, and holds four times as many of them.  But a span is 1 to 2 KB of a row where there are several,
+// every table row and of PosEmbed, and holds four times as many of them (d 4096, both fp32 tables, 4 / 8: 99 / 91 us).  But a span is 1 to 2 KB of a row where there are several,
 // since waves that read less of it at once wait longer than they read.  MI355X, 16384 tokens of 32000, d 2048, both fp32 tables and
 // positions to bf16, 1 / 2 / 4 / 8 spans: 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be done without, 4.1 TB/s; a copy reaches
 // 4.8); 65536 of 50304, d 768, bf16: 23.9 (in 1 / 2 / 4 spans, when bf16 vectors were still widened as they came in, which made every
@@ -596,8 +596,8 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
         !aligned(out, out_dtype == SPLC_BF16 ? 2 : 4))
         return SPLC_EALIGN;
     if (rows == 0) return SPLC_OK;
-    int spans = 1;                                            // 1, 2 or 4, of whole vectors
-    while (spans < 4 && spans * (2048 / (int)in) < d) spans *= 2;
+    int spans = 1;                                            // 1, 2, 4 or 8, of whole vectors
+    while (spans < 8 && spans * (2048 / (int)in) < d) spans *= 2;
     const int width = ((d + spans - 1) / spans + 3) / 4 * 4;
     int lanes = 64;                                           // for a row; 16, 32 or 64
     while (lanes > 16 && d <= lanes * 2) lanes /= 2;
