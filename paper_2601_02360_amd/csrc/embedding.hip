@@ -40,11 +40,11 @@ constexpr int64_t kMostTurns = 1 << 20;  // (a launch has fewer than 2^32 lanes)
 // to four vectors of every array are in flight: two of one row, or, of spans of at most 256 columns, one of four (65536 tokens of
 // 50304, d 256, bf16: 15.4 -> 11.7 us; d 150, fp32, two tables: 18.0 -> 14.3).
 // Workgroups go to the eight XCDs round-robin by number, and spans go with them: with four spans an XCD's L2 is asked for one fourth of
-// every table row and of PosEmbed, and holds four times as many of them (d 4096, both fp32 tables, 4 / 8: 99 / 91 us).  But a span is 1 to 2 KB of a row where there are several,
-// since waves that read less of it at once wait longer than they read.  MI355X, 16384 tokens of 32000, d 2048, both fp32 tables and
-// positions to bf16, 1 / 2 / 4 / 8 spans: 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be done without, 4.1 TB/s; a copy reaches
-// 4.8); 65536 of 50304, d 768, bf16: 23.9 (in 1 / 2 / 4 spans, when bf16 vectors were still widened as they came in, which made every
-// load wait for the one before: 31.0 / 43.0 / 64.8).  out without the streaming hint: 45.0 instead of 40.1.
+// every table row and of PosEmbed, and holds four times as many of them.  But a span is 1.25 to 2.5 KB of a row where there are several,
+// since waves that read less of it at once wait longer than they read.  MI355X, 16384 tokens of 32000, tables that no cache holds, both
+// fp32 tables and positions to bf16: d 2048 in 1 / 2 / 4 / 8 spans 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be done without, 4.1
+// TB/s; a copy reaches 4.8), d 4096 in 4 / 8 96 / 91; 60000 of d 672, bf16, in 1 / 4 22.9 / 38.4; spans of 1 to 2 KB: d 2050, bf16, 23.9
+// for 20.3.  out without the streaming hint: 45.0 instead of 40.1.
 // NARROW: rows of at most 128 columns, of which a wave takes as many at once as it has `lanes` lanes for (22817 tokens, d 106: 8.0 -> 5.5
 // us; 65536, d 64: 18.9 -> 6.4, and 4.7 with four times as many).
 template <bool NARROW, int ROWS, class T, class O>
@@ -597,7 +597,7 @@ int sparseloco_embedding_lookup(const void* table, const void* t_perp, int table
         return SPLC_EALIGN;
     if (rows == 0) return SPLC_OK;
     int spans = 1;                                            // 1, 2, 4 or 8, of whole vectors
-    while (spans < 8 && spans * (2048 / (int)in) < d) spans *= 2;
+    while (spans < 8 && spans * (2560 / (int)in) <= d) spans *= 2;
     const int width = ((d + spans - 1) / spans + 3) / 4 * 4;
     int lanes = 64;                                           // for a row; 16, 32 or 64
     while (lanes > 16 && d <= lanes * 2) lanes /= 2;

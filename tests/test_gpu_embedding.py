@@ -48,7 +48,7 @@ def normal(rng, *shape):
 @pytest.mark.parametrize("rows,vocab,d", [(1, 1, 1), (1, 5, 2), (3, 7, 3), (37, 300, 768), (5, 50, 1023), (64, 50, 1024), (65, 50, 1025),
                                           (9, 20, 2050), (130, 1000, 257), (4099, 611, 30), (2, 3, 4096 + 6),
                                           (70, 40, 64), (1001, 33, 33), (129, 40, 127), (255, 40, 128), (257, 40, 129),
-                                          (18, 40, 200), (1031, 99, 256), (7, 30, 512), (6, 30, 513), (5, 9, 1500), (3, 9, 2049), (21, 9, 5003), (9, 9, 8200)])
+                                          (18, 40, 200), (1031, 99, 256), (7, 30, 512), (6, 30, 513), (5, 9, 1500), (3, 9, 2049), (21, 9, 5003), (9, 9, 8200), (8193, 99, 1024), (8195, 60, 1790)])
 @pytest.mark.parametrize("table_type,out_type,perp,seq", [(F32, F32, False, 0), (F32, BF16, True, 5), (BF16, F32, True, 64), (BF16, BF16, False, 3)])
 def test_lookup(rows, vocab, d, table_type, out_type, perp, seq):
     rng = np.random.default_rng(rows + d)
