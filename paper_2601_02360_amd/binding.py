@@ -220,10 +220,15 @@ def _check_tensor(t, numel: int, dtype, what: str, device: bool = True):
         raise ValueError("%s: not on a GPU" % what)
 
 
+_FLOATS = {torch.float32: SPLC_F32, torch.bfloat16: SPLC_BF16}
+
+
 class Tensors:
     """A bound list (or R lists) of the plan's tensors: sparseloco_tensors_bind / _release."""
 
     def __init__(self, plan: "Plan", sets, dtype=torch.float32, stream=None):
+        if dtype not in _FLOATS:                 # (bound as one of these, another type's elements would be read past their end)
+            raise ValueError("dtype %s: tensors are bound as float32 or bfloat16" % dtype)
         if len(sets) and isinstance(sets[0], torch.Tensor) or (len(sets) and sets[0] is None):
             sets = [sets]
         nt = len(plan.numels)
@@ -244,7 +249,7 @@ class Tensors:
         self.dtype = dtype
         self._keep = [list(t) for t in sets]        # the tensors stay alive as long as the binding
         rc = lib().sparseloco_tensors_bind(ctypes.byref(self._h), plan.handle, len(sets), arr,
-                                           SPLC_BF16 if dtype == torch.bfloat16 else SPLC_F32, _stream(stream))
+                                           _FLOATS[dtype], _stream(stream))
         if rc != SPLC_OK:
             self._h = ctypes.c_void_p()
             raise SparseLoCoError(rc, "sparseloco_tensors_bind")
@@ -764,9 +769,6 @@ def sparseloco_adamw_step_8bit(plan: Plan, theta, grads, m: torch.Tensor, m_scal
                                           _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_adamw_step_8bit")
-
-
-_FLOATS = {torch.float32: SPLC_F32, torch.bfloat16: SPLC_BF16}
 
 
 def _check_embedding(matrix, table, token_ids, what):
