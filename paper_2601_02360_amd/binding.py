@@ -428,7 +428,12 @@ class Plan:
 
 
 def _h(x):
-    return None if x is None else x.handle
+    """The handle of a binding.  One that is closed has none, and is not to pass for an optional one that was left out."""
+    if x is None:
+        return None
+    if not x.handle.value:
+        raise SparseLoCoError(SPLC_EINVAL, "a closed binding")
+    return x.handle
 
 
 def _opt(t):
@@ -728,7 +733,7 @@ def sparseloco_adamw_step(plan: Plan, theta, grads, m, v, *, lr: float, step: in
     bf16.  grad_scale: one fp32 element on the GPU, the factor on the gradients (norm_out[1:] of sparseloco_grad_norm); if it
     is not finite nothing changes.  decay: per tensor a factor on weight_decay.  theta_bf16: receives a bf16 copy."""
     if (type(theta) is Tensors and type(grads) is Tensors and type(m) is Tensors and type(v) is Tensors
-            and (theta_bf16 is None or type(theta_bf16) is Tensors)):
+            and (theta_bf16 is None or (type(theta_bf16) is Tensors and theta_bf16._h.value))):
         rc = _native().adamw_step(plan._h.value, theta._h.value, grads._h.value, m._h.value, v._h.value, replica, lr, beta1,
                                   beta2, eps, weight_decay, step, grad_scale, len(plan.numels), decay,
                                   None if theta_bf16 is None else theta_bf16._h.value, _given(stream))
@@ -750,7 +755,8 @@ def sparseloco_adamw_step_8bit(plan: Plan, theta, grads, m: torch.Tensor, m_scal
                                decay: Optional[torch.Tensor] = None, theta_bf16=None, replica: int = 0, stream=None) -> None:
     """sparseloco_adamw_step with the moments in 8 bits: m, m_scale, v, v_scale as plan.adamw_8bit_buffers() makes them
     (float8_e4m3fn and one fp32 scale per 256 elements, m = scale * value, sqrt(v) = scale * value), in place."""
-    if type(theta) is Tensors and type(grads) is Tensors and (theta_bf16 is None or type(theta_bf16) is Tensors):
+    if (type(theta) is Tensors and type(grads) is Tensors
+            and (theta_bf16 is None or (type(theta_bf16) is Tensors and theta_bf16._h.value))):
         rc = _native().adamw_step_8bit(plan._h.value, theta._h.value, grads._h.value, replica, plan._num_flat_chunks, m, m_scale,
                                        v, v_scale, lr, beta1, beta2, eps, weight_decay, step, grad_scale, len(plan.numels), decay,
                                        None if theta_bf16 is None else theta_bf16._h.value, _given(stream))
