@@ -23,12 +23,12 @@
  *     The operations (compress, compress_batch, outer_step_batch, aggregate,
  *     aggregate_update, outer_update and the matrix entry points) ONLY ENQUEUE
  *     KERNELS on it: no allocation, no copy, no event, no host wait.  They can
- *     be recorded into a HIP graph.  plan_create and the bind calls allocate and enqueue one small
+ *     be recorded into a HIP graph.  plan_create and the bind calls allocate (rebind does not) and enqueue one small
  *     host-to-device copy on their stream; work on ANOTHER stream that uses the
  *     plan or the handle must be ordered after that copy by the caller.
- *   - The plan and the handles are immutable once created (the exceptions,
- *     sparseloco_plan_set_select and sparseloco_plan_set_radix_counter, are test
- *     and diagnostic switches) and belong to the device that was current when
+ *   - The plan and the handles are immutable once created (the exceptions:
+ *     sparseloco_plan_set_select and sparseloco_plan_set_radix_counter, test and
+ *     diagnostic switches, and the rebind calls) and belong to the device that was current when
  *     they were created; every operation takes them as
  *     pointers to const and may be called from several host threads at once.
  *     Release a handle or destroy a plan only after the work that uses it has
@@ -170,6 +170,14 @@ int64_t sparseloco_chunk_table(int n_tensors, const int64_t* rows, const int64_t
 int sparseloco_tensors_bind(sparseloco_tensors** out, const sparseloco_plan* plan, int n_sets,
                             const void* const* ptrs, int dtype, void* stream);
 void sparseloco_tensors_release(sparseloco_tensors* tensors);
+/*
+ * Point a handle at other tensors: what release and bind do, without allocating, freeing or waiting for the device.  The
+ * plan is one of the handle's device; n_sets * n_tensors may be at most what it was when the handle was bound
+ * (SPLC_ETOOBIG).  Only after the work that uses the handle has completed, and by one thread.  A refused call leaves the
+ * handle as it is; after SPLC_EHIP it can only be released.
+ */
+int sparseloco_tensors_rebind(sparseloco_tensors* tensors, const sparseloco_plan* plan, int n_sets,
+                              const void* const* ptrs, int dtype, void* stream);
 
 /*
  * Bind the message buffers of n_replicas replicas (1..SPLC_MAX_REPLICAS): pairs[r] uint16[n_chunks * kappa],
@@ -178,6 +186,9 @@ void sparseloco_tensors_release(sparseloco_tensors* tensors);
 int sparseloco_messages_bind(sparseloco_messages** out, const sparseloco_plan* plan, int n_replicas,
                              uint16_t* const* pairs, float* const* aux, void* stream);
 void sparseloco_messages_release(sparseloco_messages* messages);
+/* Point a handle at other message buffers, as above; of at most as many replicas as it was bound for. */
+int sparseloco_messages_rebind(sparseloco_messages* messages, const sparseloco_plan* plan, int n_replicas,
+                               uint16_t* const* pairs, float* const* aux, void* stream);
 
 /*
  * Lines 1-4 of the update equations for ONE replica, all tensors, one launch.

@@ -9,8 +9,10 @@ HIP stream.  There is no fallback: if the library has not been built
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -43,6 +45,7 @@ EXPORTS = [
     "sparseloco_subspace_reconstruct", "sparseloco_subspace_kernel_choice", "sparseloco_strerror",
     "sparseloco_plan_num_flat_chunks", "sparseloco_grad_norm", "sparseloco_adamw_step", "sparseloco_adamw_step_8bit",
     "sparseloco_embedding_lookup", "sparseloco_embedding_grad_ws_bytes", "sparseloco_embedding_grad",
+    "sparseloco_tensors_rebind", "sparseloco_messages_rebind",
 ]
 
 SPLC_OP_PROJECT, SPLC_OP_RECONSTRUCT, SPLC_OP_REPROJECT_PASS1, SPLC_OP_REPROJECT_PASS2 = 0, 1, 2, 3
@@ -93,8 +96,10 @@ def lib():
             "sparseloco_chunk_table": (i64, [i32, p64, p64, i32, vp, i64]),
             "sparseloco_tensors_bind": (i32, [pp, vp, i32, pp, i32, vp]),
             "sparseloco_tensors_release": (None, [vp]),
+            "sparseloco_tensors_rebind": (i32, [vp, vp, i32, pp, i32, vp]),
             "sparseloco_messages_bind": (i32, [pp, vp, i32, pp, pp, vp]),
             "sparseloco_messages_release": (None, [vp]),
+            "sparseloco_messages_rebind": (i32, [vp, vp, i32, pp, pp, vp]),
             "sparseloco_compress": (i32, [vp, i32, vp, vp, vp, i32, f32, vp, vp, vp]),
             "sparseloco_compress_batch": (i32, [vp, i32, vp, vp, vp, f32, vp, vp]),
             "sparseloco_outer_step_batch": (i32, [vp, i32, vp, vp, vp, f32, f32, vp, vp, i32, vp]),
@@ -165,6 +170,24 @@ def _stream(stream) -> Optional[int]:
     return h or None
 
 
+def _torch_stream(stream):
+    """The stream argument of a call as one of torch's."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    if stream is None:
+        return torch.cuda.current_stream()
+    h = _stream(stream)
+    return torch.cuda.ExternalStream(h) if h else torch.cuda.default_stream()
+
+
+def _capturing(stream) -> bool:
+    """Whether this stream or the current one is being captured into a graph."""
+    if torch.cuda.is_current_stream_capturing():
+        return True
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def rows_cols(shape):
     """(rows, cols) of a tensor for the tiled layout: leading dimensions fold into rows; 1-D -> (1, n)."""
     if isinstance(shape, int):
@@ -223,10 +246,76 @@ def _check_tensor(t, numel: int, dtype, what: str, device: bool = True):
 _FLOATS = {torch.float32: SPLC_F32, torch.bfloat16: SPLC_BF16}
 
 
-class Tensors:
+class _Binding:
+    """A handle of the library's and the tensors that it stands for."""
+
+    def _bind(self, kind: str, room: int, spares: "Optional[_Spares]", *args) -> None:
+        """A handle of its own, or a spare one that has room for as many tensors."""
+        self._kind, self._room, self._h = kind, room, ctypes.c_void_p()
+        spare = spares.take(kind, room) if spares is not None else None
+        if spare is not None:
+            self._room, self._h = spare
+            rc = getattr(lib(), kind + "_rebind")(self._h, *args)
+        else:
+            rc = getattr(lib(), kind + "_bind")(ctypes.byref(self._h), *args)
+        if rc != SPLC_OK:
+            self.close()
+            raise SparseLoCoError(rc, kind + "_bind")
+
+    @property
+    def handle(self):
+        return self._h
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            getattr(lib(), self._kind + "_release")(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class _Spares:
+    """Handles of bindings whose work is done, for the next ones: making one allocates, and releasing one waits for the device."""
+    MOST = 32
+
+    def __init__(self):
+        self.handles = []                        # (kind, room, handle), oldest first
+        self.lock = threading.Lock()
+
+    def take(self, kind: str, room: int):
+        with self.lock:
+            for i, (k, r, h) in enumerate(self.handles):
+                if k == kind and r >= room:
+                    del self.handles[i]
+                    return r, h
+        return None
+
+    def put(self, bound: _Binding) -> None:
+        with self.lock:
+            self.handles.append((bound._kind, bound._room, bound._h))
+            gone = self.handles[:-self.MOST]
+            del self.handles[:-self.MOST]
+        bound._h, bound._keep = ctypes.c_void_p(), ()
+        self._release(gone)
+
+    def close(self) -> None:
+        gone, self.handles = self.handles, []
+        self._release(gone)
+
+    @staticmethod
+    def _release(handles) -> None:
+        for kind, _, h in handles:
+            getattr(lib(), kind + "_release")(h)
+
+
+class Tensors(_Binding):
     """A bound list (or R lists) of the plan's tensors: sparseloco_tensors_bind / _release."""
 
-    def __init__(self, plan: "Plan", sets, dtype=torch.float32, stream=None):
+    def __init__(self, plan: "Plan", sets, dtype=torch.float32, stream=None, spares: "Optional[_Spares]" = None):
         if dtype not in _FLOATS:                 # (bound as one of these, another type's elements would be read past their end)
             raise ValueError("dtype %s: tensors are bound as float32 or bfloat16" % dtype)
         if len(sets) and isinstance(sets[0], torch.Tensor) or (len(sets) and sets[0] is None):
@@ -244,36 +333,16 @@ class Tensors:
         for s, tensors in enumerate(sets):
             for i, t in enumerate(tensors):
                 arr[s * nt + i] = None if t is None or t.numel() == 0 else t.data_ptr()
-        self._h = ctypes.c_void_p()
         self.n_sets = len(sets)
         self.dtype = dtype
         self._keep = [list(t) for t in sets]        # the tensors stay alive as long as the binding
-        rc = lib().sparseloco_tensors_bind(ctypes.byref(self._h), plan.handle, len(sets), arr,
-                                           _FLOATS[dtype], _stream(stream))
-        if rc != SPLC_OK:
-            self._h = ctypes.c_void_p()
-            raise SparseLoCoError(rc, "sparseloco_tensors_bind")
-
-    @property
-    def handle(self):
-        return self._h
-
-    def close(self):
-        if getattr(self, "_h", None) is not None and self._h.value:
-            lib().sparseloco_tensors_release(self._h)
-            self._h = ctypes.c_void_p()
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
+        self._bind("sparseloco_tensors", nt * len(sets), spares, plan.handle, len(sets), arr, _FLOATS[dtype], _stream(stream))
 
 
-class Messages:
+class Messages(_Binding):
     """Bound message buffers of R replicas: sparseloco_messages_bind / _release."""
 
-    def __init__(self, plan: "Plan", pairs, aux, stream=None):
+    def __init__(self, plan: "Plan", pairs, aux, stream=None, spares: "Optional[_Spares]" = None):
         if len(pairs) != len(aux):
             raise ValueError("%d pair buffers, %d level/value buffers" % (len(pairs), len(aux)))
         nch = plan.num_chunks
@@ -285,28 +354,9 @@ class Messages:
         n = len(pairs)
         pa = (ctypes.c_void_p * max(n, 1))(*[p.data_ptr() for p in pairs])
         aa = (ctypes.c_void_p * max(n, 1))(*[a.data_ptr() for a in aux])
-        self._h = ctypes.c_void_p()
         self.n_replicas = n
         self._keep = (list(pairs), list(aux))
-        rc = lib().sparseloco_messages_bind(ctypes.byref(self._h), plan.handle, n, pa, aa, _stream(stream))
-        if rc != SPLC_OK:
-            self._h = ctypes.c_void_p()
-            raise SparseLoCoError(rc, "sparseloco_messages_bind")
-
-    @property
-    def handle(self):
-        return self._h
-
-    def close(self):
-        if getattr(self, "_h", None) is not None and self._h.value:
-            lib().sparseloco_messages_release(self._h)
-            self._h = ctypes.c_void_p()
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
+        self._bind("sparseloco_messages", n, spares, plan.handle, n, pa, aa, _stream(stream))
 
 
 class Plan:
@@ -339,12 +389,17 @@ class Plan:
         self.quant = bool(quant)
         self._num_chunks = int(lib().sparseloco_plan_num_chunks(self._h))
         self._num_flat_chunks = int(lib().sparseloco_plan_num_flat_chunks(self._h))
-        self._temps = []           # bindings made on the fly by the convenience wrappers below
+        # bindings that calls made of plain lists (_Lists): those in graphs; the calls' events and bindings, oldest first; and
+        # the handles of those whose calls are done
+        self._recorded, self._in_flight, self._spares = [], collections.deque(), _Spares()
+        self._lock = threading.Lock()
 
     def close(self):
-        for t in getattr(self, "_temps", []):
-            t.close()
-        self._temps = []
+        if getattr(self, "_in_flight", None) is not None:
+            for t in [*self._recorded, *(t for _, made in self._in_flight for t in made)]:
+                t.close()
+            self._recorded, self._in_flight = [], collections.deque()
+            self._spares.close()
         if getattr(self, "_h", None) is not None and self._h.value:
             lib().sparseloco_plan_destroy(self._h)
             self._h = ctypes.c_void_p()
@@ -411,20 +466,54 @@ class Plan:
     def bind_messages(self, pairs, aux, stream=None) -> Messages:
         return Messages(self, pairs, aux, stream)
 
-    # Convenience for callers that pass plain lists: bound on the fly, released with the plan.
-    def _tensors(self, x, dtype=torch.float32, stream=None) -> Optional[Tensors]:
+    CALLS_IN_FLIGHT = 4
+
+    def _hold(self, made, stream) -> None:
+        """Takes the bindings that a call made of plain lists once it has enqueued its work, and lets go of those whose calls are
+        done.  The tensors of at most CALLS_IN_FLIGHT calls stay alive; who is further ahead waits for the oldest."""
+        stream = _torch_stream(stream)
+        if _capturing(stream):                   # the graph may run as long as the plan lives
+            self._recorded += made
+            return
+        event = torch.cuda.Event()
+        event.record(stream)
+        self._in_flight.append((event, made))
+        while True:
+            with self._lock:
+                calls = self._in_flight
+                if not calls or not (len(calls) > self.CALLS_IN_FLIGHT or calls[0][0].query()):
+                    return
+                event, done = calls.popleft()
+            event.synchronize()
+            for t in done:
+                self._spares.put(t)
+
+
+class _Lists:
+    """A call's bindings of plain lists: made on the fly, held by the plan until the call's work is done.  Every
+    such call copies tables: what a loop passes again and again is better bound once."""
+
+    def __init__(self, plan: Plan, stream):
+        self.plan, self.stream, self.made = plan, stream, []
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *_):
+        if self.made:
+            self.plan._hold(self.made, self.stream)
+
+    def tensors(self, x, dtype=torch.float32) -> Optional[Tensors]:
         if x is None or isinstance(x, Tensors):
             return x
-        t = Tensors(self, x, dtype, stream)
-        self._temps.append(t)
-        return t
+        self.made.append(Tensors(self.plan, x, dtype, self.stream, self.plan._spares))
+        return self.made[-1]
 
-    def _messages(self, pairs, aux, stream=None) -> Messages:
+    def messages(self, pairs, aux) -> Messages:
         if isinstance(pairs, Messages):
             return pairs
-        m = Messages(self, pairs, aux, stream)
-        self._temps.append(m)
-        return m
+        self.made.append(Messages(self.plan, pairs, aux, self.stream, self.plan._spares))
+        return self.made[-1]
 
 
 def _h(x):
@@ -457,14 +546,15 @@ def sparseloco_compress(plan: Plan, ef, pairs_out: torch.Tensor, aux_out: torch.
     nch = plan.num_chunks
     _check_tensor(pairs_out, nch * plan.kappa, torch.int16, "pairs_out")
     _check_tensor(aux_out, nch * (2 if plan.quant else plan.kappa), torch.float32, "aux_out")
-    if delta is not None:
-        dt = delta.dtype if isinstance(delta, Tensors) else next((t.dtype for t in delta if t is not None), torch.float32)
-        mode, a, b = SPLC_DELTA_DIRECT, plan._tensors(delta, dt, stream), None
-    else:
-        mode, a, b = SPLC_DELTA_FROM_PARAMS, plan._tensors(theta_outer, stream=stream), plan._tensors(theta_local, stream=stream)
-    e = plan._tensors(ef, stream=stream)
-    rc = lib().sparseloco_compress(plan.handle, mode, _h(a), _h(b), _h(e), int(replica), float(beta),
-                                   pairs_out.data_ptr(), aux_out.data_ptr(), _stream(stream))
+    with _Lists(plan, stream) as lists:
+        if delta is not None:
+            dt = delta.dtype if isinstance(delta, Tensors) else next((t.dtype for t in delta if t is not None), torch.float32)
+            mode, a, b = SPLC_DELTA_DIRECT, lists.tensors(delta, dt), None
+        else:
+            mode, a, b = SPLC_DELTA_FROM_PARAMS, lists.tensors(theta_outer), lists.tensors(theta_local)
+        e = lists.tensors(ef)
+        rc = lib().sparseloco_compress(plan.handle, mode, _h(a), _h(b), _h(e), int(replica), float(beta),
+                                       pairs_out.data_ptr(), aux_out.data_ptr(), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_compress")
 
@@ -476,9 +566,10 @@ def sparseloco_aggregate(plan: Plan, messages, delta_bar_out, *, aux=None, strea
         rc = _native().aggregate(plan._h.value, messages._h.value, delta_bar_out._h.value, _given(stream))
         if _done(rc, "sparseloco_aggregate"):
             return
-    m = plan._messages(messages, aux, stream)
-    rc = lib().sparseloco_aggregate(plan.handle, m.handle, _h(plan._tensors(delta_bar_out, stream=stream)),
-                                    _stream(stream))
+    with _Lists(plan, stream) as lists:
+        m = lists.messages(messages, aux)
+        rc = lib().sparseloco_aggregate(plan.handle, m.handle, _h(lists.tensors(delta_bar_out)),
+                                        _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_aggregate")
 
@@ -489,8 +580,9 @@ def sparseloco_outer_update(plan: Plan, theta_outer, delta_bar, outer_lr: float,
         rc = _native().outer_update(plan._h.value, theta_outer._h.value, delta_bar._h.value, outer_lr, _given(stream))
         if _done(rc, "sparseloco_outer_update"):
             return
-    rc = lib().sparseloco_outer_update(plan.handle, _h(plan._tensors(theta_outer, stream=stream)),
-                                       _h(plan._tensors(delta_bar, stream=stream)), float(outer_lr), _stream(stream))
+    with _Lists(plan, stream) as lists:
+        rc = lib().sparseloco_outer_update(plan.handle, _h(lists.tensors(theta_outer)),
+                                           _h(lists.tensors(delta_bar)), float(outer_lr), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_outer_update")
 
@@ -504,10 +596,11 @@ def sparseloco_aggregate_update(plan: Plan, messages, theta_outer, outer_lr: flo
                                         _given(stream))
         if _done(rc, "sparseloco_aggregate_update"):
             return
-    m = plan._messages(messages, aux, stream)
-    rc = lib().sparseloco_aggregate_update(plan.handle, m.handle, _h(plan._tensors(theta_outer, stream=stream)),
-                                           float(outer_lr), _h(plan._tensors(delta_bar_out, stream=stream)),
-                                           _h(plan._tensors(reset, stream=stream)), _stream(stream))
+    with _Lists(plan, stream) as lists:
+        m = lists.messages(messages, aux)
+        rc = lib().sparseloco_aggregate_update(plan.handle, m.handle, _h(lists.tensors(theta_outer)),
+                                               float(outer_lr), _h(lists.tensors(delta_bar_out)),
+                                               _h(lists.tensors(reset)), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_aggregate_update")
 
@@ -516,11 +609,12 @@ def sparseloco_compress_batch(plan: Plan, theta_outer, theta_local, ef, messages
                               n_replicas: Optional[int] = None, stream=None) -> None:
     """Lines 1-4 for R replicas sharing theta_outer, one launch.  theta_local / ef: multi-set bindings or per
     replica a list of tensors; messages_out: a Messages binding, or the pair buffers with aux_out= the others."""
-    tl, e = plan._tensors(theta_local, stream=stream), plan._tensors(ef, stream=stream)
-    m = plan._messages(messages_out, aux_out, stream)
-    n = tl.n_sets if n_replicas is None else int(n_replicas)
-    rc = lib().sparseloco_compress_batch(plan.handle, n, _h(plan._tensors(theta_outer, stream=stream)), tl.handle,
-                                         e.handle, float(beta), m.handle, _stream(stream))
+    with _Lists(plan, stream) as lists:
+        tl, e = lists.tensors(theta_local), lists.tensors(ef)
+        m = lists.messages(messages_out, aux_out)
+        n = tl.n_sets if n_replicas is None else int(n_replicas)
+        rc = lib().sparseloco_compress_batch(plan.handle, n, _h(lists.tensors(theta_outer)), tl.handle,
+                                             e.handle, float(beta), m.handle, _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_compress_batch")
 
@@ -538,13 +632,14 @@ def sparseloco_outer_step_batch(plan: Plan, theta_outer, theta_local, ef, messag
                                         messages_out._h.value, None, 1 if reset else 0, _given(stream))
         if _done(rc, "sparseloco_outer_step_batch"):
             return
-    tl, e = plan._tensors(theta_local, stream=stream), plan._tensors(ef, stream=stream)
-    m = plan._messages(messages_out, aux_out, stream)
-    n = tl.n_sets if n_replicas is None else int(n_replicas)
-    rc = lib().sparseloco_outer_step_batch(plan.handle, n, _h(plan._tensors(theta_outer, stream=stream)), tl.handle,
-                                           e.handle, float(beta), float(outer_lr), m.handle,
-                                           _h(plan._tensors(delta_bar_out, stream=stream)), 1 if reset else 0,
-                                           _stream(stream))
+    with _Lists(plan, stream) as lists:
+        tl, e = lists.tensors(theta_local), lists.tensors(ef)
+        m = lists.messages(messages_out, aux_out)
+        n = tl.n_sets if n_replicas is None else int(n_replicas)
+        rc = lib().sparseloco_outer_step_batch(plan.handle, n, _h(lists.tensors(theta_outer)), tl.handle,
+                                               e.handle, float(beta), float(outer_lr), m.handle,
+                                               _h(lists.tensors(delta_bar_out)), 1 if reset else 0,
+                                               _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_outer_step_batch")
 
@@ -711,8 +806,9 @@ def sparseloco_grad_norm(plan: Plan, grads, norm_out: torch.Tensor, ws: torch.Te
         if _done(rc, "sparseloco_grad_norm"):
             return
     _check_flat([(norm_out, 2, torch.float32, "norm_out"), (ws, SPLC_NORM_WS_BYTES, torch.uint8, "ws")])
-    rc = lib().sparseloco_grad_norm(plan.handle, _h(plan._tensors(grads, _dtype_of(grads), stream)), int(replica),
-                                    float(max_norm), norm_out.data_ptr(), ws.data_ptr(), _stream(stream))
+    with _Lists(plan, stream) as lists:
+        rc = lib().sparseloco_grad_norm(plan.handle, _h(lists.tensors(grads, _dtype_of(grads))), int(replica),
+                                        float(max_norm), norm_out.data_ptr(), ws.data_ptr(), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_grad_norm")
 
@@ -741,10 +837,11 @@ def sparseloco_adamw_step(plan: Plan, theta, grads, m, v, *, lr: float, step: in
             return
     _check_flat(_check_step(plan, grad_scale, decay))
     how = _AdamW(lr, beta1, beta2, eps, weight_decay, step)
-    rc = lib().sparseloco_adamw_step(plan.handle, _h(plan._tensors(theta, stream=stream)),
-                                     _h(plan._tensors(grads, _dtype_of(grads), stream)), _h(plan._tensors(m, stream=stream)),
-                                     _h(plan._tensors(v, stream=stream)), int(replica), ctypes.byref(how), _opt(grad_scale),
-                                     _opt(decay), _h(plan._tensors(theta_bf16, torch.bfloat16, stream)), _stream(stream))
+    with _Lists(plan, stream) as lists:
+        rc = lib().sparseloco_adamw_step(plan.handle, _h(lists.tensors(theta)),
+                                         _h(lists.tensors(grads, _dtype_of(grads))), _h(lists.tensors(m)),
+                                         _h(lists.tensors(v)), int(replica), ctypes.byref(how), _opt(grad_scale),
+                                         _opt(decay), _h(lists.tensors(theta_bf16, torch.bfloat16)), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_adamw_step")
 
@@ -768,11 +865,12 @@ def sparseloco_adamw_step_8bit(plan: Plan, theta, grads, m: torch.Tensor, m_scal
                  (v, codes, torch.float8_e4m3fn, "v"), (v_scale, scales, torch.float32, "v_scale")]
                 + _check_step(plan, grad_scale, decay))
     how = _AdamW(lr, beta1, beta2, eps, weight_decay, step)
-    rc = lib().sparseloco_adamw_step_8bit(plan.handle, _h(plan._tensors(theta, stream=stream)),
-                                          _h(plan._tensors(grads, _dtype_of(grads), stream)), int(replica), m.data_ptr(),
-                                          m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), ctypes.byref(how),
-                                          _opt(grad_scale), _opt(decay), _h(plan._tensors(theta_bf16, torch.bfloat16, stream)),
-                                          _stream(stream))
+    with _Lists(plan, stream) as lists:
+        rc = lib().sparseloco_adamw_step_8bit(plan.handle, _h(lists.tensors(theta)),
+                                              _h(lists.tensors(grads, _dtype_of(grads))), int(replica), m.data_ptr(),
+                                              m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), ctypes.byref(how),
+                                              _opt(grad_scale), _opt(decay), _h(lists.tensors(theta_bf16, torch.bfloat16)),
+                                              _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_adamw_step_8bit")
 

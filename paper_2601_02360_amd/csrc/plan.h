@@ -123,6 +123,7 @@ struct sparseloco_tensors {
     int n_sets = 0;
     int dtype = SPLC_F32;
     bool disjoint = false;               // no tensor shares memory with another (looked at where it matters: small plans)
+    size_t room = 0;                     // pointers that the tables hold
     void** d_table = nullptr;
     void** h_table = nullptr;            // pinned source of the upload
 };

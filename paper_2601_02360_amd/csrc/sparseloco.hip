@@ -1458,6 +1458,7 @@ struct sparseloco_messages {
     int kappa = 0;
     int64_t n_chunks = 0;
     bool disjoint = false;               // no buffer shares memory with another (as above)
+    size_t room = 0;                     // pointers that the tables hold
     void** d_table = nullptr;
     void** h_table = nullptr;
 };
@@ -1494,6 +1495,67 @@ bool on_small_plan_disjoint(const sparseloco_plan* plan, Collect collect) {
     } catch (const std::bad_alloc&) {
         return false;
     }
+}
+
+// A list of tensors that is to be bound: refused before anything is allocated or written.
+int check_tensor_list(const sparseloco_plan* plan, int n_sets, const void* const* ptrs, int dtype) {
+    if (!plan || !ptrs || n_sets < 1 || n_sets > SPLC_MAX_REPLICAS) return SPLC_EINVAL;
+    if (dtype != SPLC_F32 && dtype != SPLC_BF16) return SPLC_EINVAL;
+    const size_t nt = (size_t)plan->n_tensors, n = nt * (size_t)n_sets;
+    for (size_t i = 0; i < n; ++i) {
+        if (plan->numel[i % nt] == 0) continue;
+        if (!ptrs[i]) return SPLC_EINVAL;
+        if (!aligned(ptrs[i], 4)) return SPLC_EALIGN;             // for bf16 it keeps vector rows dword aligned
+    }
+    return current_device_is(plan->device);
+}
+// Points a binding whose table has room for them at the tensors.
+int point_at(sparseloco_tensors* t, const sparseloco_plan* plan, int n_sets, const void* const* ptrs, int dtype, void* stream) {
+    const size_t nt = (size_t)plan->n_tensors, n = nt * (size_t)n_sets;
+    t->device = plan->device;
+    t->n_tensors = plan->n_tensors;
+    t->n_sets = n_sets;
+    t->dtype = dtype;
+    t->disjoint = n_sets == 1 || on_small_plan_disjoint(plan, [&](auto& ranges) {
+        const uint64_t size = dtype == SPLC_BF16 ? 2 : 4;
+        for (size_t i = 0; i < n; ++i)
+            ranges.push_back(range_of(ptrs[i], (uint64_t)plan->numel[i % nt] * size));
+    });
+    for (size_t i = 0; i < n; ++i) t->h_table[i] = plan->numel[i % nt] == 0 ? nullptr : const_cast<void*>(ptrs[i]);
+    return hipMemcpyAsync(t->d_table, t->h_table, n * sizeof(void*), hipMemcpyHostToDevice, static_cast<hipStream_t>(stream)) ==
+                   hipSuccess ? SPLC_OK : SPLC_EHIP;
+}
+// The same of message buffers.
+int check_message_list(const sparseloco_plan* plan, int n_replicas, uint16_t* const* pairs, float* const* aux) {
+    if (!plan || !pairs || !aux || n_replicas < 1 || n_replicas > SPLC_MAX_REPLICAS) return SPLC_EINVAL;
+    for (int r = 0; r < n_replicas; ++r) {
+        if (plan->n_chunks == 0) continue;
+        if (!pairs[r] || !aux[r]) return SPLC_EINVAL;
+        if (!aligned(pairs[r], 2) || !aligned(aux[r], 4)) return SPLC_EALIGN;
+    }
+    return current_device_is(plan->device);
+}
+int point_at(sparseloco_messages* m, const sparseloco_plan* plan, int n_replicas, uint16_t* const* pairs, float* const* aux,
+             void* stream) {
+    m->device = plan->device;
+    m->n_replicas = n_replicas;
+    m->quant = plan->quant;
+    m->kappa = plan->kappa;
+    m->n_chunks = plan->n_chunks;
+    const size_t nr = (size_t)n_replicas;
+    m->disjoint = n_replicas == 1 || on_small_plan_disjoint(plan, [&](auto& ranges) {
+        const uint64_t slots = (uint64_t)plan->n_chunks * (uint64_t)plan->kappa;
+        for (size_t r = 0; r < nr; ++r) {
+            ranges.push_back(range_of(pairs[r], 2 * slots));
+            ranges.push_back(range_of(aux[r], 4 * (plan->quant == SPLC_QUANT_2BIT ? 2 * (uint64_t)plan->n_chunks : slots)));
+        }
+    });
+    for (size_t r = 0; r < nr; ++r) {
+        m->h_table[r] = pairs[r];
+        m->h_table[nr + r] = aux[r];
+    }
+    return hipMemcpyAsync(m->d_table, m->h_table, 2 * nr * sizeof(void*), hipMemcpyHostToDevice, static_cast<hipStream_t>(stream)) ==
+                   hipSuccess ? SPLC_OK : SPLC_EHIP;
 }
 
 unsigned reserve_lds_compress(const sparseloco_plan* plan, int64_t entries, bool from_params, size_t used) {
@@ -1925,39 +1987,28 @@ int sparseloco_tensors_bind(sparseloco_tensors** out, const sparseloco_plan* pla
                             const void* const* ptrs, int dtype, void* stream) {
     if (!out) return SPLC_EINVAL;
     *out = nullptr;
-    if (!plan || !ptrs || n_sets < 1 || n_sets > SPLC_MAX_REPLICAS) return SPLC_EINVAL;
-    if (dtype != SPLC_F32 && dtype != SPLC_BF16) return SPLC_EINVAL;
-    const size_t nt = (size_t)plan->n_tensors, n = nt * (size_t)n_sets;
-    for (size_t i = 0; i < n; ++i) {
-        if (plan->numel[i % nt] == 0) continue;
-        if (!ptrs[i]) return SPLC_EINVAL;
-        if (!aligned(ptrs[i], 4)) return SPLC_EALIGN;             // for bf16 it keeps vector rows dword aligned
-    }
-    int rc = current_device_is(plan->device);
+    int rc = check_tensor_list(plan, n_sets, ptrs, dtype);
     if (rc != SPLC_OK) return rc;
     sparseloco_tensors* t = new (std::nothrow) sparseloco_tensors();
     if (!t) return SPLC_ENOMEM;
-    t->device = plan->device;
-    t->n_tensors = plan->n_tensors;
-    t->n_sets = n_sets;
-    t->dtype = dtype;
-    t->disjoint = n_sets == 1 || on_small_plan_disjoint(plan, [&](auto& ranges) {
-        const uint64_t size = dtype == SPLC_BF16 ? 2 : 4;
-        for (size_t i = 0; i < n; ++i)
-            ranges.push_back(range_of(ptrs[i], (uint64_t)plan->numel[i % nt] * size));
-    });
-    if ((rc = upload_table(n, &t->h_table, &t->d_table)) == SPLC_OK) {
-        for (size_t i = 0; i < n; ++i) t->h_table[i] = plan->numel[i % nt] == 0 ? nullptr : const_cast<void*>(ptrs[i]);
-        if (hipMemcpyAsync(t->d_table, t->h_table, n * sizeof(void*), hipMemcpyHostToDevice,
-                           static_cast<hipStream_t>(stream)) != hipSuccess)
-            rc = SPLC_EHIP;
-    }
+    t->room = (size_t)plan->n_tensors * (size_t)n_sets;
+    if ((rc = upload_table(t->room, &t->h_table, &t->d_table)) == SPLC_OK) rc = point_at(t, plan, n_sets, ptrs, dtype, stream);
     if (rc != SPLC_OK) {
         sparseloco_tensors_release(t);
         return rc;
     }
     *out = t;
     return SPLC_OK;
+}
+
+int sparseloco_tensors_rebind(sparseloco_tensors* tensors, const sparseloco_plan* plan, int n_sets,
+                              const void* const* ptrs, int dtype, void* stream) {
+    if (!tensors) return SPLC_EINVAL;
+    int rc = check_tensor_list(plan, n_sets, ptrs, dtype);
+    if (rc != SPLC_OK) return rc;
+    if (tensors->device != plan->device) return SPLC_EPLAN;
+    if ((size_t)plan->n_tensors * (size_t)n_sets > tensors->room) return SPLC_ETOOBIG;
+    return point_at(tensors, plan, n_sets, ptrs, dtype, stream);
 }
 
 void sparseloco_tensors_release(sparseloco_tensors* t) {
@@ -1971,44 +2022,28 @@ int sparseloco_messages_bind(sparseloco_messages** out, const sparseloco_plan* p
                              uint16_t* const* pairs, float* const* aux, void* stream) {
     if (!out) return SPLC_EINVAL;
     *out = nullptr;
-    if (!plan || !pairs || !aux || n_replicas < 1 || n_replicas > SPLC_MAX_REPLICAS) return SPLC_EINVAL;
-    for (int r = 0; r < n_replicas; ++r) {
-        if (plan->n_chunks == 0) continue;
-        if (!pairs[r] || !aux[r]) return SPLC_EINVAL;
-        if (!aligned(pairs[r], 2) || !aligned(aux[r], 4)) return SPLC_EALIGN;
-    }
-    int rc = current_device_is(plan->device);
+    int rc = check_message_list(plan, n_replicas, pairs, aux);
     if (rc != SPLC_OK) return rc;
     sparseloco_messages* m = new (std::nothrow) sparseloco_messages();
     if (!m) return SPLC_ENOMEM;
-    m->device = plan->device;
-    m->n_replicas = n_replicas;
-    m->quant = plan->quant;
-    m->kappa = plan->kappa;
-    m->n_chunks = plan->n_chunks;
-    const size_t nr = (size_t)n_replicas;
-    m->disjoint = n_replicas == 1 || on_small_plan_disjoint(plan, [&](auto& ranges) {
-        const uint64_t slots = (uint64_t)plan->n_chunks * (uint64_t)plan->kappa;
-        for (size_t r = 0; r < nr; ++r) {
-            ranges.push_back(range_of(pairs[r], 2 * slots));
-            ranges.push_back(range_of(aux[r], 4 * (plan->quant == SPLC_QUANT_2BIT ? 2 * (uint64_t)plan->n_chunks : slots)));
-        }
-    });
-    if ((rc = upload_table(2 * nr, &m->h_table, &m->d_table)) == SPLC_OK) {
-        for (size_t r = 0; r < nr; ++r) {
-            m->h_table[r] = pairs[r];
-            m->h_table[nr + r] = aux[r];
-        }
-        if (hipMemcpyAsync(m->d_table, m->h_table, 2 * nr * sizeof(void*), hipMemcpyHostToDevice,
-                           static_cast<hipStream_t>(stream)) != hipSuccess)
-            rc = SPLC_EHIP;
-    }
+    m->room = 2 * (size_t)n_replicas;
+    if ((rc = upload_table(m->room, &m->h_table, &m->d_table)) == SPLC_OK) rc = point_at(m, plan, n_replicas, pairs, aux, stream);
     if (rc != SPLC_OK) {
         sparseloco_messages_release(m);
         return rc;
     }
     *out = m;
     return SPLC_OK;
+}
+
+int sparseloco_messages_rebind(sparseloco_messages* messages, const sparseloco_plan* plan, int n_replicas,
+                               uint16_t* const* pairs, float* const* aux, void* stream) {
+    if (!messages) return SPLC_EINVAL;
+    int rc = check_message_list(plan, n_replicas, pairs, aux);
+    if (rc != SPLC_OK) return rc;
+    if (messages->device != plan->device) return SPLC_EPLAN;
+    if (2 * (size_t)n_replicas > messages->room) return SPLC_ETOOBIG;
+    return point_at(messages, plan, n_replicas, pairs, aux, stream);
 }
 
 void sparseloco_messages_release(sparseloco_messages* m) {
