@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import operator
 import os
 import threading
 from typing import Optional, Sequence
@@ -777,6 +778,14 @@ def sparseloco_subspace_reconstruct(x_tilde: torch.Tensor, u: torch.Tensor, out:
         raise SparseLoCoError(rc, "sparseloco_subspace_reconstruct")
 
 
+def _integer(v, bits: int, where: str) -> int:
+    """An integer argument that the library takes in so many bits: ctypes would keep its lower ones."""
+    v = int(v)
+    if not -(1 << bits - 1) <= v < 1 << bits - 1:
+        raise SparseLoCoError(SPLC_EINVAL, where)
+    return v
+
+
 def _dtype_of(tensors):
     """The element type of a binding or of a list of tensors (fp32 where there is none)."""
     if isinstance(tensors, Tensors):
@@ -806,8 +815,9 @@ def sparseloco_grad_norm(plan: Plan, grads, norm_out: torch.Tensor, ws: torch.Te
         if _done(rc, "sparseloco_grad_norm"):
             return
     _check_flat([(norm_out, 2, torch.float32, "norm_out"), (ws, SPLC_NORM_WS_BYTES, torch.uint8, "ws")])
+    replica = _integer(replica, 32, "sparseloco_grad_norm")
     with _Lists(plan, stream) as lists:
-        rc = lib().sparseloco_grad_norm(plan.handle, _h(lists.tensors(grads, _dtype_of(grads))), int(replica),
+        rc = lib().sparseloco_grad_norm(plan.handle, _h(lists.tensors(grads, _dtype_of(grads))), replica,
                                         float(max_norm), norm_out.data_ptr(), ws.data_ptr(), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_grad_norm")
@@ -836,11 +846,12 @@ def sparseloco_adamw_step(plan: Plan, theta, grads, m, v, *, lr: float, step: in
         if _done(rc, "sparseloco_adamw_step"):
             return
     _check_flat(_check_step(plan, grad_scale, decay))
+    replica, step = _integer(replica, 32, "sparseloco_adamw_step"), _integer(operator.index(step), 64, "sparseloco_adamw_step")
     how = _AdamW(lr, beta1, beta2, eps, weight_decay, step)
     with _Lists(plan, stream) as lists:
         rc = lib().sparseloco_adamw_step(plan.handle, _h(lists.tensors(theta)),
                                          _h(lists.tensors(grads, _dtype_of(grads))), _h(lists.tensors(m)),
-                                         _h(lists.tensors(v)), int(replica), ctypes.byref(how), _opt(grad_scale),
+                                         _h(lists.tensors(v)), replica, ctypes.byref(how), _opt(grad_scale),
                                          _opt(decay), _h(lists.tensors(theta_bf16, torch.bfloat16)), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_adamw_step")
@@ -864,10 +875,11 @@ def sparseloco_adamw_step_8bit(plan: Plan, theta, grads, m: torch.Tensor, m_scal
     _check_flat([(m, codes, torch.float8_e4m3fn, "m"), (m_scale, scales, torch.float32, "m_scale"),
                  (v, codes, torch.float8_e4m3fn, "v"), (v_scale, scales, torch.float32, "v_scale")]
                 + _check_step(plan, grad_scale, decay))
+    replica, step = _integer(replica, 32, "sparseloco_adamw_step_8bit"), _integer(operator.index(step), 64, "sparseloco_adamw_step_8bit")
     how = _AdamW(lr, beta1, beta2, eps, weight_decay, step)
     with _Lists(plan, stream) as lists:
         rc = lib().sparseloco_adamw_step_8bit(plan.handle, _h(lists.tensors(theta)),
-                                              _h(lists.tensors(grads, _dtype_of(grads))), int(replica), m.data_ptr(),
+                                              _h(lists.tensors(grads, _dtype_of(grads))), replica, m.data_ptr(),
                                               m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), ctypes.byref(how),
                                               _opt(grad_scale), _opt(decay), _h(lists.tensors(theta_bf16, torch.bfloat16)),
                                               _stream(stream))
@@ -902,18 +914,19 @@ def sparseloco_embedding_lookup(table: torch.Tensor, token_ids: torch.Tensor, ou
             raise ValueError("pos_embed must be a matrix of one row or more")
         specs.append((pos_embed, (pos_embed.shape[0], d), "pos_embed", table.dtype))
     _check_matrices(specs)
-    rc = lib().sparseloco_embedding_lookup(table.data_ptr(), _opt(t_perp), table_type, token_ids.data_ptr(), int(vocab),
-                                           _opt(pos_embed), 0 if pos_embed is None else int(pos_embed.shape[0]), float(scale),
-                                           out.data_ptr(), out_type, int(rows), int(d), _stream(stream))
+    seq, vocab, d = (_integer(n, 32, "sparseloco_embedding_lookup") for n in (0 if pos_embed is None else pos_embed.shape[0], vocab, d))
+    rc = lib().sparseloco_embedding_lookup(table.data_ptr(), _opt(t_perp), table_type, token_ids.data_ptr(), vocab, _opt(pos_embed), seq,
+                                           float(scale), out.data_ptr(), out_type, int(rows), d, _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_embedding_lookup")
 
 
 def embedding_grad_workspace(rows: int, vocab: int, d: int, device="cuda") -> torch.Tensor:
     """A workspace of sparseloco_embedding_grad for up to `rows` tokens."""
-    n = int(lib().sparseloco_embedding_grad_ws_bytes(int(rows), int(vocab), int(d)))
+    where = "sparseloco_embedding_grad_ws_bytes"
+    n = int(lib().sparseloco_embedding_grad_ws_bytes(_integer(rows, 64, where), _integer(vocab, 32, where), _integer(d, 32, where)))
     if n < 0:
-        raise SparseLoCoError(n, "sparseloco_embedding_grad_ws_bytes")
+        raise SparseLoCoError(n, where)
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
@@ -928,8 +941,9 @@ def sparseloco_embedding_grad(grad_out: torch.Tensor, token_ids: torch.Tensor, g
     if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.dim() != 1:
         raise ValueError("ws: must be a contiguous uint8 tensor")
     _check_matrices([(ws, ws.shape, "ws", torch.uint8)])
-    rc = lib().sparseloco_embedding_grad(grad_out.data_ptr(), grad_type, token_ids.data_ptr(), int(rows), int(vocab), int(d),
-                                         float(scale), int(ignore_id), grad_table.data_ptr(), table_type, 1 if accumulate else 0,
+    vocab, d, ignore_id = (_integer(n, 32, "sparseloco_embedding_grad") for n in (vocab, d, ignore_id))
+    rc = lib().sparseloco_embedding_grad(grad_out.data_ptr(), grad_type, token_ids.data_ptr(), int(rows), vocab, d,
+                                         float(scale), ignore_id, grad_table.data_ptr(), table_type, 1 if accumulate else 0,
                                          ws.data_ptr(), int(ws.numel()), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_embedding_grad")
