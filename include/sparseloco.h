@@ -401,8 +401,9 @@ int sparseloco_grad_norm(const sparseloco_plan* plan, const sparseloco_tensors* 
  *   everything as it is: a batch whose gradients overflowed is skipped without the host having to look.
  *   decay: n_tensors floats of device memory or NULL (all 1): how much of the weight decay each tensor takes.
  *   theta_bf16: NULL, or a bf16 binding that receives the new theta rounded to nearest even.
- * A call recorded into a graph keeps its numbers.  Gradients must be finite where grad_scale is.  With eps = 0 an element whose v
- * is 0 becomes NaN.  No buffer may overlap another.
+ * A call recorded into a graph keeps its numbers.  Gradients must be finite where grad_scale is, and small enough for v: the
+ * step works in fp32, and the square of grad_scale * grad is infinite from 1.8e19 on (in 8 bits: and the element's whole block NaN
+ * after the next step).  With eps = 0 an element whose v is 0 becomes NaN.  No buffer may overlap another.
  */
 typedef struct {
     double lr, beta1, beta2, eps, weight_decay;

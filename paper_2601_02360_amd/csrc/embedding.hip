@@ -40,8 +40,8 @@ constexpr int64_t kMostTurns = 1 << 20;  // (a launch has fewer than 2^32 lanes)
 // to four vectors of every array are in flight: two of one row, or, of spans of at most 256 columns, one of four (65536 tokens of
 // 50304, d 256, bf16: 15.4 -> 11.7 us; d 150, fp32, two tables: 18.0 -> 14.3).
 // Workgroups go to the eight XCDs round-robin by number, and spans go with them: with four spans an XCD's L2 is asked for one fourth of
-// every table row and of PosEmbed, and holds four times as many of them.  But a span is 1.25 to 2.5 KB of a row where there are several,
-// since waves that read less of it at once wait longer than they read.  MI355X, 16384 tokens of 32000, tables that no cache holds, both
+// every table row and of PosEmbed, and holds four times as many of them.  But a span is 1.25 to 2.5 KB of a row where there are several
+// (more in rows above 20 KB: there are eight at most), since waves that read less of it at once wait longer than they read.  MI355X, 16384 tokens of 32000, tables that no cache holds, both
 // fp32 tables and positions to bf16: d 2048 in 1 / 2 / 4 / 8 spans 44.2 / 41.6 / 40.1 / 41.4 us (165 MB that cannot be done without, 4.1
 // TB/s; a copy reaches 4.8), d 4096 in 4 / 8 96 / 91; 60000 of d 672, bf16, in 1 / 4 22.9 / 38.4; spans of 1 to 2 KB: d 2050, bf16, 23.9
 // for 20.3.  out without the streaming hint: 45.0 instead of 40.1.
@@ -316,8 +316,8 @@ __global__ __launch_bounds__(kMergeThreads) void merge_runs_kernel(const uint32_
 // Sums are kept in registers: grad_out is read once, in rows, and every row of the table is written once, by one wave.  A lane has
 // VEC consecutive columns: four, or one where the table is narrow.  Windows that lie inside one run are summed first, where there
 // are many tokens, so that a frequent token's run is not left to few waves (one that makes up 7 % of 65537: 69 windows instead of 4400
-// rows).  Bound by memory: MI355X, 65537 fp32 rows of 2050 into 32001 rows, frequencies 1 / rank, added to what is there: windows 37 us
-// (4.6 TB/s), runs 117 to 126 us (5.1 to 4.7 TB/s); 16384 bf16 rows of 2048: runs 18 us.  One token throughout: 92 and 33 us, 20 (with
+// rows).  Bound by memory: MI355X, 65537 fp32 rows of 2050 into 32001 rows, frequencies 1 / rank, added to what is there: windows 34 us
+// (4.9 TB/s), runs 120 us (4.7 TB/s); 16384 bf16 rows of 2048: runs 24 us (18 where caches hold part).  One token throughout: 92 and 33 us, 20 (with
 // zeros) and 10 us.  Small calls wait: 4096 bf16 rows of 1792 of 388, 11 us.  grad_out is read without the streaming hint, which loses
 // lines that two slices share (65537 rows of few different tokens: 180 us with it, 128).
 

@@ -3,11 +3,12 @@
 //
 // All three are element-wise over the tensors, whatever the plan's layout: they walk its flat chunks (4096 consecutive
 // elements, one workgroup at a time), lane `tid` holding, for slot s = 0..3 and j = 0..3, element s*1024 + tid*4 + j, as in
-// the outer update.  They are bound by memory traffic; what they move is what has to be moved (rocprofv3: fetched and written
-// within 0.3 % of it).  MI355X, packed tensors of the 0.9B model (888 M parameters):
-//   norm           2 bytes a parameter (bf16)                     0.257 ms   6.9 TB/s
+// the outer update.  They are bound by memory traffic, and move little that does not have to be moved (rocprofv3, fetched and
+// written: both AdamW steps within 0.5 % of it, the bf16 norm 3.7 % more).  MI355X, the 0.9B model (888 M parameters):
+//   norm           2 bytes a parameter (bf16, packed tensors)     0.257 ms   6.9 TB/s
 //   AdamW          28 (bf16 gradients, fp32 moments, bf16 copy)   4.43 ms    5.6 TB/s
 //   AdamW, 8 bits  16.1 (the same; aligned tensors)               2.43 ms    5.9 TB/s
+//                  16.1 (the same; packed tensors)                2.70 ms    5.3 TB/s
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -85,7 +86,7 @@ __device__ __forceinline__ double group_sum(double x, double* shared) {
 
 // Sum of squares, formed and added in 64 bits: no fp32 value's square overflows or vanishes there, and no order of adding
 // 10^9 of them loses anything that fp32 shows; at a multiply-add per element the vector ALU has time for it.  A workgroup takes
-// every so manieth chunk, and one more workgroup adds the partial sums: 2048 x 2048, which caches hold, 3.9 us and 2.1 us.
+// every so manieth chunk, and one more workgroup adds the partial sums: 2048 x 2048, which caches hold, 3.4 to 5.4 us and 1.9 us.
 template <class T>
 __global__ __launch_bounds__(kThreads) void norm_partial_kernel(const ChunkDesc* __restrict__ chunks, uint32_t n_chunks,
                                                                 const T* const* __restrict__ grad_tab,
