@@ -103,14 +103,20 @@ struct Args {
     }
 };
 
-// The call itself without the interpreter's lock, as ctypes does it: a launch may wait for room in the queue.
+// The call itself without the interpreter's lock, as ctypes does it: a launch may wait for room in the queue.  What it takes
+// from tensors is taken before, under the lock, and the lock is there again for whatever leaves it.
+struct Unlocked {
+    PyThreadState* state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
 template <class Call>
 PyObject* finish(const Args& a, Call call) {
     if (!a.ok || a.left != 0) Py_RETURN_NONE;
     int rc;
-    Py_BEGIN_ALLOW_THREADS
-    rc = call();
-    Py_END_ALLOW_THREADS
+    {
+        Unlocked unlocked;
+        rc = call();
+    }
     return PyLong_FromLong(rc);
 }
 
@@ -327,7 +333,9 @@ PyObject* embedding_lookup(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const void* table = a.float_matrix(vocab, d, in);
         const auto* ids = a.tensor(at::kInt);
         void* out = a.float_matrix(rows, d, result);
+        const int32_t* id = nullptr;
         if (!ids || ids->dim() != 1 || ids->size(0) != rows) a.ok = false;
+        else id = static_cast<const int32_t*>(ids->data_ptr());
         const void *t_perp = nullptr, *pos = nullptr;
         if (!a.none()) {
             t_perp = a.float_matrix(vocab, d, other);
@@ -341,8 +349,8 @@ PyObject* embedding_lookup(PyObject*, PyObject* const* args, Py_ssize_t n) {
         void* stream = a.stream();
         if (vocab > INT_MAX || d > INT_MAX || seq > INT_MAX) a.ok = false;
         return finish(a, [&] {
-            return sparseloco_embedding_lookup(table, t_perp, in, static_cast<const int32_t*>(ids->data_ptr()), (int)vocab, pos,
-                                               (int)(pos ? seq : 0), scale, out, result, rows, (int)d, stream);
+            return sparseloco_embedding_lookup(table, t_perp, in, id, (int)vocab, pos, (int)(pos ? seq : 0), scale, out, result, rows,
+                                               (int)d, stream);
         });
     });
 }
@@ -355,14 +363,23 @@ PyObject* embedding_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const auto* ids = a.tensor(at::kInt);
         void* table = a.float_matrix(vocab, d, result);
         const auto* ws = a.tensor(at::kByte);
-        if (!ids || ids->dim() != 1 || ids->size(0) != rows || !ws || ws->dim() != 1) a.ok = false;
+        const int32_t* id = nullptr;
+        void* space = nullptr;
+        int64_t space_bytes = 0;
+        if (!ids || ids->dim() != 1 || ids->size(0) != rows || !ws || ws->dim() != 1) {
+            a.ok = false;
+        } else {
+            id = static_cast<const int32_t*>(ids->data_ptr());
+            space = ws->data_ptr();
+            space_bytes = ws->numel();
+        }
         const float scale = a.number();
         const int ignore = (int)a.integer(INT_MIN, INT_MAX), accumulate = a.integer();
         void* stream = a.stream();
         if (vocab > INT_MAX || d > INT_MAX) a.ok = false;
         return finish(a, [&] {
-            return sparseloco_embedding_grad(grad, gradient, static_cast<const int32_t*>(ids->data_ptr()), rows, (int)vocab, (int)d,
-                                             scale, ignore, table, result, accumulate, ws->data_ptr(), ws->numel(), stream);
+            return sparseloco_embedding_grad(grad, gradient, id, rows, (int)vocab, (int)d, scale, ignore, table, result, accumulate, space,
+                                             space_bytes, stream);
         });
     });
 }
