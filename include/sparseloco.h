@@ -459,6 +459,54 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
                               int64_t ws_bytes, void* stream);
 
 /*
+ * Attention heads of the inner step's model: queries and keys turned by their positions (rotary positions, beside the table of
+ * positions that the lookup adds), and normed head by head in the same pass, with the gradient of that.  Queries and keys are lists
+ * of heads: `tokens` x `heads` rows of head_dim channels, channel stride 1, any other strides (in elements), so that the heads may
+ * be part of a packed projection.  head_dim: even, 2 .. SPLC_MAX_HEAD_DIM.  k (with its outputs, gain and gradients) may be NULL.
+ *
+ * sparseloco_rotary turns pair i of a head, i < pairs, by the angle a = positions[token] * frequencies[i]:
+ *     (x, y) -> magnitude * (x cos a - y sin a, y cos a + x sin a)
+ * and copies channels 2 pairs .. head_dim - 1.  A pair is channels (i, pairs + i), or (2 i, 2 i + 1) with interleaved.  inverse: by
+ * the opposite angle, which is the operator's gradient.
+ *   positions: `tokens` int32 or int64 (position_bytes 4 or 8) of any sign; frequencies: radians per position, fp64.  Both device
+ *   memory, aligned to their elements.  Angles are formed in fp64, their sine and cosine within 2^-22.
+ * sparseloco_qk_norm_rotary norms every head first:
+ *     x -> gain x / sqrt(mean(x^2) + eps),      q_gain, k_gain: [head_dim] of gain_dtype
+ * sparseloco_qk_norm_rotary_grad is its gradient, from that of its outputs, with respect to q, k and both gains (fp32, sums over
+ * tokens and heads, added to what is there with accumulate).  ws: .._ws_bytes(tokens, ..) bytes, 4-byte aligned, need not be
+ * cleared; a workspace for more tokens serves fewer.  The same call gives the same bits.
+ * Everything is computed in fp32 (squares must not overflow there) and rounded once to dtype (SPLC_F32 or SPLC_BF16, that of all
+ * lists).  A list that is written may be one of the inputs, element for element (in place), and must overlap nothing otherwise; its
+ * own heads must not overlap one another.  A token or head of zeros has the norm's factor 1 / sqrt(eps); with eps = 0 it becomes NaN.
+ * What is not finite stays in its head (and in the gains' gradients).  tokens = 0: nothing but the gains' gradients is written.
+ */
+#define SPLC_MAX_HEAD_DIM 512
+#define SPLC_MAX_HEADS 65536
+typedef struct {
+    void* data;                  /* first channel of token 0, head 0; only read where the list is an input */
+    int64_t token_stride, head_stride;
+    int heads;
+} sparseloco_heads;
+typedef struct {
+    const void* positions;
+    const double* frequencies;
+    int position_bytes, pairs, interleaved;
+    double magnitude;
+} sparseloco_rotation;
+int sparseloco_rotary(const sparseloco_heads* q, const sparseloco_heads* k, int dtype, int64_t tokens, int head_dim,
+                      const sparseloco_rotation* how, int inverse, const sparseloco_heads* q_out, const sparseloco_heads* k_out,
+                      void* stream);
+int sparseloco_qk_norm_rotary(const sparseloco_heads* q, const sparseloco_heads* k, int dtype, int64_t tokens, int head_dim,
+                              const void* q_gain, const void* k_gain, int gain_dtype, double eps, const sparseloco_rotation* how,
+                              const sparseloco_heads* q_out, const sparseloco_heads* k_out, void* stream);
+int64_t sparseloco_qk_norm_rotary_grad_ws_bytes(int64_t tokens, int q_heads, int k_heads, int head_dim);
+int sparseloco_qk_norm_rotary_grad(const sparseloco_heads* grad_q_out, const sparseloco_heads* grad_k_out, const sparseloco_heads* q,
+                                   const sparseloco_heads* k, int dtype, int64_t tokens, int head_dim, const void* q_gain,
+                                   const void* k_gain, int gain_dtype, double eps, const sparseloco_rotation* how,
+                                   const sparseloco_heads* grad_q, const sparseloco_heads* grad_k, float* grad_q_gain,
+                                   float* grad_k_gain, int accumulate, void* ws, int64_t ws_bytes, void* stream);
+
+/*
  * Measurement aid: what the chip streams for the access patterns of the kernels above, with their launch shape
  * (one 256-lane workgroup per 4096 floats, 16-byte non-temporal accesses).  The practical ceiling next to which
  * the achieved bandwidths are read; not part of the method.

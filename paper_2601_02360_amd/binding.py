@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import math
 import operator
 import os
 import threading
@@ -47,6 +48,7 @@ EXPORTS = [
     "sparseloco_plan_num_flat_chunks", "sparseloco_grad_norm", "sparseloco_adamw_step", "sparseloco_adamw_step_8bit",
     "sparseloco_embedding_lookup", "sparseloco_embedding_grad_ws_bytes", "sparseloco_embedding_grad",
     "sparseloco_tensors_rebind", "sparseloco_messages_rebind",
+    "sparseloco_rotary", "sparseloco_qk_norm_rotary", "sparseloco_qk_norm_rotary_grad_ws_bytes", "sparseloco_qk_norm_rotary_grad",
 ]
 
 SPLC_OP_PROJECT, SPLC_OP_RECONSTRUCT, SPLC_OP_REPROJECT_PASS1, SPLC_OP_REPROJECT_PASS2 = 0, 1, 2, 3
@@ -60,6 +62,17 @@ class _AdamW(ctypes.Structure):
     """sparseloco_adamw: the numbers of one step."""
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
                 ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64)]
+
+
+class _Heads(ctypes.Structure):
+    """sparseloco_heads: queries or keys, [tokens, heads, head_dim]."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("heads", ctypes.c_int)]
+
+
+class _Rotation(ctypes.Structure):
+    """sparseloco_rotation: where the tokens are, and how their heads turn."""
+    _fields_ = [("positions", ctypes.c_void_p), ("frequencies", ctypes.c_void_p), ("position_bytes", ctypes.c_int),
+                ("pairs", ctypes.c_int), ("interleaved", ctypes.c_int), ("magnitude", ctypes.c_double)]
 
 
 class SparseLoCoError(RuntimeError):
@@ -79,7 +92,8 @@ def lib():
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
         pp = ctypes.POINTER(ctypes.c_void_p)
-        p64 = ctypes.POINTER(i64)
+        p64, f64 = ctypes.POINTER(i64), ctypes.c_double
+        hp, rp = ctypes.POINTER(_Heads), ctypes.POINTER(_Rotation)
         sig = {
             "sparseloco_plan_create": (i32, [pp, i32, p64, i32, i32, i32, vp]),
             "sparseloco_plan_create_2d": (i32, [pp, i32, p64, p64, i32, i32, i32, vp]),
@@ -118,6 +132,11 @@ def lib():
             "sparseloco_adamw_step": (i32, [vp, vp, vp, vp, vp, i32, ctypes.POINTER(_AdamW), vp, vp, vp, vp]),
             "sparseloco_adamw_step_8bit": (i32, [vp, vp, vp, i32, vp, vp, vp, vp, ctypes.POINTER(_AdamW), vp, vp, vp, vp]),
             "sparseloco_embedding_lookup": (i32, [vp, vp, i32, vp, i32, vp, i32, f32, vp, i32, i64, i32, vp]),
+            "sparseloco_rotary": (i32, [hp, hp, i32, i64, i32, rp, i32, hp, hp, vp]),
+            "sparseloco_qk_norm_rotary": (i32, [hp, hp, i32, i64, i32, vp, vp, i32, f64, rp, hp, hp, vp]),
+            "sparseloco_qk_norm_rotary_grad_ws_bytes": (i64, [i64, i32, i32, i32]),
+            "sparseloco_qk_norm_rotary_grad": (i32, [hp, hp, hp, hp, i32, i64, i32, vp, vp, i32, f64, rp, hp, hp, vp, vp, i32, vp, i64,
+                                                     vp]),
             "sparseloco_embedding_grad_ws_bytes": (i64, [i64, i32, i32]),
             "sparseloco_embedding_grad": (i32, [vp, i32, vp, i64, i32, i32, f32, i32, vp, i32, i32, vp, i64, vp]),
         }
@@ -947,3 +966,171 @@ def sparseloco_embedding_grad(grad_out: torch.Tensor, token_ids: torch.Tensor, g
                                          ws.data_ptr(), int(ws.numel()), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_embedding_grad")
+
+
+def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                       trained_length: int = 4096, fast: float = 32.0, slow: float = 1.0, device="cuda"):
+    """(frequencies, magnitude) of sparseloco_rotary for the first rotary_dim channels of a head: base^(-2 i / rotary_dim) radians per
+    position.  For contexts `factor` times trained_length, scaling:
+      "linear"   every frequency divided by factor;
+      "base"     the base times factor^(rotary_dim / (rotary_dim - 2)): the lowest frequency is divided by factor, the highest kept;
+      "by_parts" frequencies that make `slow` turns or fewer over trained_length are divided by factor, those that make `fast` or more
+                 kept, with a linear ramp between, and magnitude = 0.1 ln(factor) + 1."""
+    rotary_dim = operator.index(rotary_dim)
+    if rotary_dim < 2 or rotary_dim % 2 or not 0 < base < float("inf") or not 1 <= factor < float("inf"):
+        raise ValueError("rotary_frequencies: an even rotary_dim, base > 0, factor >= 1")
+    i = torch.arange(rotary_dim // 2, dtype=torch.float64)
+    magnitude = 1.0
+    if scaling == "base":
+        if rotary_dim == 2:
+            raise ValueError("scaling by the base needs two frequencies")
+        base = base * factor ** (rotary_dim / (rotary_dim - 2))
+    f = torch.pow(torch.tensor(float(base), dtype=torch.float64), -2 * i / rotary_dim)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "by_parts":
+        if not 0 <= slow < fast or trained_length < 1:
+            raise ValueError("scaling by parts: slow < fast, trained_length >= 1")
+        keep = ((trained_length * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+        f, magnitude = f * keep + f / factor * (1 - keep), 0.1 * math.log(factor) + 1
+    elif scaling not in (None, "base"):
+        raise ValueError("scaling: None, 'linear', 'base' or 'by_parts', got %r" % (scaling,))
+    return f.to(device), magnitude
+
+
+def _check_heads(lists, positions, frequencies):
+    """lists: (tensor, name), queries and keys in turn, keys None in all or none.  What all of them are, then where they live."""
+    q = lists[0][0]
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("%s: expected [tokens, heads, head_dim]" % lists[0][1])
+    if q.dtype not in _FLOATS:
+        raise ValueError("%s: dtype %s, expected float32 or bfloat16" % (lists[0][1], q.dtype))
+    tokens, _, d = q.shape
+    keys = lists[1][0]
+    for i, (t, name) in enumerate(lists):
+        like = lists[i % 2][0]
+        if keys is None and i % 2:
+            if t is not None:
+                raise ValueError("%s: given without keys" % name)
+            continue
+        if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape != like.shape or t.shape[0] != tokens or t.shape[2] != d:
+            raise ValueError("%s: expected [%d, heads, %d] like the list it belongs to, got %r"
+                             % (name, tokens, d, tuple(t.shape) if isinstance(t, torch.Tensor) else None))
+        if t.dtype != q.dtype:
+            raise ValueError("%s: dtype %s, expected %s" % (name, t.dtype, q.dtype))
+        if t.stride(2) != 1 and t.numel():
+            raise ValueError("%s: the channels of a head must lie side by side" % name)
+    for t, kinds, name in ((positions, (torch.int32, torch.int64), "positions"), (frequencies, (torch.float64,), "frequencies")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 1 or t.dtype not in kinds or not t.is_contiguous():
+            raise ValueError("%s: must be a contiguous vector of %s" % (name, " or ".join(str(k) for k in kinds)))
+    if positions.shape[0] != tokens:
+        raise ValueError("positions: %d, there are %d tokens" % (positions.shape[0], tokens))
+    _check_here([t for t, _ in lists] + [positions, frequencies])
+    return q.dtype, int(tokens), int(d)
+
+
+def _check_here(tensors):
+    """Tensors on the current GPU: the launch goes there."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("a tensor is not on a GPU")
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError("a tensor is on %s, the current device is cuda:%d" % (t.device, torch.cuda.current_device()))
+
+
+def _heads(t):
+    if t is None:
+        return None
+    return ctypes.byref(_Heads(t.data_ptr(), t.stride(0), t.stride(1), _integer(t.shape[1], 32, "heads")))
+
+
+def _rotation(positions, frequencies, interleaved, magnitude):
+    return ctypes.byref(_Rotation(positions.data_ptr(), frequencies.data_ptr(), positions.element_size(), frequencies.shape[0],
+                                  1 if interleaved else 0, float(magnitude)))
+
+
+def sparseloco_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: torch.Tensor, q_out: torch.Tensor,
+                      k_out: Optional[torch.Tensor], *, interleaved: bool = False, magnitude: float = 1.0, inverse: bool = False,
+                      stream=None) -> None:
+    """Heads turned by their positions: pair i by positions[token] * frequencies[i] radians, times magnitude.  q, k: [tokens, heads,
+    head_dim] fp32 or bf16, any strides but that of the channels; k may be None; the outputs may be the inputs.  positions: [tokens]
+    int32 or int64; frequencies: [pairs] fp64 (rotary_frequencies), fewer pairs than a head has leave its last channels as they are.
+    A pair is channels (i, pairs + i), or (2 i, 2 i + 1) with interleaved.  inverse: by the opposite angle (the gradient)."""
+    if _done(_native().rotary(q, k, positions, frequencies, q_out, k_out, 1 if interleaved else 0, magnitude, 1 if inverse else 0,
+                              _given(stream)), "sparseloco_rotary"):
+        return
+    dtype, tokens, d = _check_heads([(q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")], positions, frequencies)
+    rc = lib().sparseloco_rotary(_heads(q), _heads(k), _FLOATS[dtype], tokens, d, _rotation(positions, frequencies, interleaved, magnitude),
+                                 1 if inverse else 0, _heads(q_out), _heads(k_out), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_rotary")
+
+
+def _check_gains(q_gain, k_gain, d, keys):
+    if not isinstance(q_gain, torch.Tensor) or q_gain.dtype not in _FLOATS:
+        raise ValueError("q_gain: must be a vector of float32 or bfloat16")
+    if (k_gain is None) == keys:
+        raise ValueError("k_gain: goes with the keys")
+    specs = [(q_gain, (d,), "q_gain", q_gain.dtype)] + ([(k_gain, (d,), "k_gain", q_gain.dtype)] if keys else [])
+    _check_matrices(specs)
+    _check_here([q_gain, k_gain])
+    return _FLOATS[q_gain.dtype]
+
+
+def sparseloco_qk_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_gain: torch.Tensor, k_gain: Optional[torch.Tensor],
+                              positions: torch.Tensor, frequencies: torch.Tensor, q_out: torch.Tensor, k_out: Optional[torch.Tensor], *,
+                              eps: float = 1e-6, interleaved: bool = False, magnitude: float = 1.0, stream=None) -> None:
+    """sparseloco_rotary of heads that are normed first: gain * x / sqrt(mean(x^2) + eps) over each head.  q_gain, k_gain: [head_dim],
+    both fp32 or both bf16."""
+    if _done(_native().qk_norm_rotary(q, k, q_gain, k_gain, positions, frequencies, q_out, k_out, eps, 1 if interleaved else 0, magnitude,
+                                      _given(stream)), "sparseloco_qk_norm_rotary"):
+        return
+    dtype, tokens, d = _check_heads([(q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")], positions, frequencies)
+    gain_type = _check_gains(q_gain, k_gain, d, k is not None)
+    rc = lib().sparseloco_qk_norm_rotary(_heads(q), _heads(k), _FLOATS[dtype], tokens, d, q_gain.data_ptr(), _opt(k_gain), gain_type,
+                                         float(eps), _rotation(positions, frequencies, interleaved, magnitude), _heads(q_out),
+                                         _heads(k_out), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_qk_norm_rotary")
+
+
+def qk_norm_rotary_workspace(tokens: int, q_heads: int, k_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """A workspace of sparseloco_qk_norm_rotary_grad for up to `tokens` tokens."""
+    where = "sparseloco_qk_norm_rotary_grad_ws_bytes"
+    n = int(lib().sparseloco_qk_norm_rotary_grad_ws_bytes(_integer(tokens, 64, where), *(_integer(x, 32, where)
+                                                                                        for x in (q_heads, k_heads, head_dim))))
+    if n < 0:
+        raise SparseLoCoError(n, where)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def sparseloco_qk_norm_rotary_grad(grad_q_out: torch.Tensor, grad_k_out: Optional[torch.Tensor], q: torch.Tensor,
+                                   k: Optional[torch.Tensor], q_gain: torch.Tensor, k_gain: Optional[torch.Tensor],
+                                   positions: torch.Tensor, frequencies: torch.Tensor, grad_q: torch.Tensor,
+                                   grad_k: Optional[torch.Tensor], grad_q_gain: torch.Tensor, grad_k_gain: Optional[torch.Tensor],
+                                   ws: torch.Tensor, *, eps: float = 1e-6, interleaved: bool = False, magnitude: float = 1.0,
+                                   accumulate: bool = False, stream=None) -> None:
+    """The gradient of sparseloco_qk_norm_rotary from that of its outputs and from its inputs: grad_q, grad_k like q, k (they may be
+    grad_q_out, grad_k_out), grad_q_gain, grad_k_gain: [head_dim] fp32, added to what is there with accumulate.  ws:
+    qk_norm_rotary_workspace(tokens or more, ...)."""
+    if _done(_native().qk_norm_rotary_grad(grad_q_out, grad_k_out, q, k, q_gain, k_gain, positions, frequencies, grad_q, grad_k,
+                                           grad_q_gain, grad_k_gain, ws, eps, 1 if interleaved else 0, magnitude, 1 if accumulate else 0,
+                                           _given(stream)), "sparseloco_qk_norm_rotary_grad"):
+        return
+    dtype, tokens, d = _check_heads([(grad_q_out, "grad_q_out"), (grad_k_out, "grad_k_out"), (q, "q"), (k, "k"), (grad_q, "grad_q"),
+                                     (grad_k, "grad_k")], positions, frequencies)
+    gain_type = _check_gains(q_gain, k_gain, d, k is not None)
+    if (grad_k_gain is None) != (k is None):
+        raise ValueError("grad_k_gain: goes with the keys")
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.dim() != 1:
+        raise ValueError("ws: must be a contiguous uint8 tensor")
+    _check_matrices([(grad_q_gain, (d,), "grad_q_gain"), (ws, ws.shape, "ws", torch.uint8)]
+                    + ([] if k is None else [(grad_k_gain, (d,), "grad_k_gain")]))
+    _check_here([grad_q_gain, grad_k_gain, ws])
+    rc = lib().sparseloco_qk_norm_rotary_grad(
+        _heads(grad_q_out), _heads(grad_k_out), _heads(q), _heads(k), _FLOATS[dtype], tokens, d, q_gain.data_ptr(), _opt(k_gain), gain_type,
+        float(eps), _rotation(positions, frequencies, interleaved, magnitude), _heads(grad_q), _heads(grad_k), grad_q_gain.data_ptr(),
+        _opt(grad_k_gain), 1 if accumulate else 0, ws.data_ptr(), int(ws.numel()), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, "sparseloco_qk_norm_rotary_grad")

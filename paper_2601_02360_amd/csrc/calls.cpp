@@ -384,6 +384,155 @@ PyObject* embedding_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// Queries and keys, [tokens, heads, head_dim] with channels side by side, on the current device; None for lists of keys that are not there.
+struct Heads {
+    int64_t tokens = -1, d = -1;
+    int dtype = -1;
+    bool keys = true;
+    c10::DeviceIndex device = c10::hip::current_device();
+
+    bool take(Args& a, sparseloco_heads& h, bool key, int heads) {
+        if (key && !keys) {
+            if (!a.none()) a.ok = false;
+            return false;
+        }
+        PyObject* o = a.next();
+        if (!a.ok || !THPVariable_CheckExact(o)) { a.ok = false; return false; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        const at::ScalarType type = t.scalar_type();
+        if ((type != at::kFloat && type != at::kBFloat16) || !t.is_cuda() || t.device().index() != device || t.dim() != 3) {
+            a.ok = false;
+            return false;
+        }
+        const int is = type == at::kFloat ? SPLC_F32 : SPLC_BF16;
+        if (tokens < 0) {
+            tokens = t.size(0);
+            d = t.size(2);
+            dtype = is;
+        }
+        if (t.size(0) != tokens || t.size(2) != d || is != dtype || t.size(1) > INT_MAX || d > INT_MAX || t.stride(2) != 1 ||
+            (heads >= 0 && t.size(1) != heads)) {
+            a.ok = false;
+            return false;
+        }
+        h = {t.data_ptr(), t.stride(0), t.stride(1), (int)t.size(1)};
+        return true;
+    }
+};
+// A list of queries and the keys that go with it; those of the first list set whether there are keys, and how many heads there are.
+struct Pair {
+    sparseloco_heads q{}, k{};
+    bool keys = false;
+    const sparseloco_heads* key() const { return keys ? &k : nullptr; }
+};
+Pair pair(Args& a, Heads& all, const Pair* like) {
+    Pair p;
+    all.take(a, p.q, false, like ? like->q.heads : -1);
+    if (!like && a.none()) all.keys = false;
+    else p.keys = all.take(a, p.k, true, like && like->keys ? like->k.heads : -1);
+    return p;
+}
+const at::Tensor* here(Args& a, const Heads& all, at::ScalarType type) {
+    const at::Tensor* t = a.tensor(type);
+    if (t && t->device().index() == all.device) return t;
+    a.ok = false;
+    return nullptr;
+}
+// A vector of head_dim elements on the current device; of the keys: None where there are none.
+void* channels(Args& a, const Heads& all, at::ScalarType type, bool key) {
+    if (key && !all.keys) {
+        if (!a.none()) a.ok = false;
+        return nullptr;
+    }
+    const at::Tensor* t = here(a, all, type);
+    if (!t || t->dim() != 1 || t->size(0) != all.d) { a.ok = false; return nullptr; }
+    return t->data_ptr();
+}
+struct Gains {
+    const void *q = nullptr, *k = nullptr;
+    int dtype = SPLC_F32;
+};
+Gains gains(Args& a, const Heads& all) {
+    Gains g;
+    if (a.left > 0 && THPVariable_CheckExact(*a.at) && THPVariable_Unpack(*a.at).scalar_type() == at::kBFloat16) g.dtype = SPLC_BF16;
+    const at::ScalarType type = g.dtype == SPLC_BF16 ? at::kBFloat16 : at::kFloat;
+    g.q = channels(a, all, type, false);
+    g.k = channels(a, all, type, true);
+    return g;
+}
+sparseloco_rotation positions(Args& a, const Heads& all) {
+    sparseloco_rotation r{};
+    const bool wide = a.left > 0 && THPVariable_CheckExact(*a.at) && THPVariable_Unpack(*a.at).scalar_type() == at::kLong;
+    const at::Tensor* p = here(a, all, wide ? at::kLong : at::kInt);
+    const at::Tensor* f = here(a, all, at::kDouble);
+    if (!p || !f || p->dim() != 1 || p->size(0) != all.tokens || f->dim() != 1 || f->size(0) > INT_MAX) { a.ok = false; return r; }
+    r.positions = p->data_ptr();
+    r.frequencies = static_cast<const double*>(f->data_ptr());
+    r.position_bytes = wide ? 8 : 4;
+    r.pairs = (int)f->size(0);
+    return r;
+}
+
+PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        Heads all;
+        const Pair in = pair(a, all, nullptr);
+        sparseloco_rotation how = positions(a, all);
+        const Pair out = pair(a, all, &in);
+        how.interleaved = a.integer();
+        how.magnitude = a.real();
+        const int inverse = a.integer();
+        void* stream = a.stream();
+        return finish(a, [&] {
+            return sparseloco_rotary(&in.q, in.key(), all.dtype, all.tokens, (int)all.d, &how, inverse, &out.q, out.key(), stream);
+        });
+    });
+}
+
+PyObject* qk_norm_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        Heads all;
+        const Pair in = pair(a, all, nullptr);
+        const Gains g = gains(a, all);
+        sparseloco_rotation how = positions(a, all);
+        const Pair out = pair(a, all, &in);
+        const double eps = a.real();
+        how.interleaved = a.integer();
+        how.magnitude = a.real();
+        void* stream = a.stream();
+        return finish(a, [&] {
+            return sparseloco_qk_norm_rotary(&in.q, in.key(), all.dtype, all.tokens, (int)all.d, g.q, g.k, g.dtype, eps, &how, &out.q,
+                                             out.key(), stream);
+        });
+    });
+}
+
+PyObject* qk_norm_rotary_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded(args, n, [](Args a) {
+        Heads all;
+        const Pair grad = pair(a, all, nullptr);
+        const Pair in = pair(a, all, &grad);
+        const Gains g = gains(a, all);
+        sparseloco_rotation how = positions(a, all);
+        const Pair out = pair(a, all, &grad);
+        auto* q_sum = static_cast<float*>(channels(a, all, at::kFloat, false));
+        auto* k_sum = static_cast<float*>(channels(a, all, at::kFloat, true));
+        const auto* ws = here(a, all, at::kByte);
+        if (!ws || ws->dim() != 1) a.ok = false;
+        void* space = a.ok ? ws->data_ptr() : nullptr;
+        const int64_t space_bytes = a.ok ? ws->numel() : 0;
+        const double eps = a.real();
+        how.interleaved = a.integer();
+        how.magnitude = a.real();
+        const int accumulate = a.integer();
+        void* stream = a.stream();
+        return finish(a, [&] {
+            return sparseloco_qk_norm_rotary_grad(&grad.q, grad.key(), &in.q, in.key(), all.dtype, all.tokens, (int)all.d, g.q, g.k, g.dtype,
+                                                  eps, &how, &out.q, out.key(), q_sum, k_sum, accumulate, space, space_bytes, stream);
+        });
+    });
+}
+
 using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
 PyCFunction method(Fast f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
@@ -404,6 +553,9 @@ PyMODINIT_FUNC PyInit__calls() {
         {"adamw_step_8bit", method(adamw_step_8bit), METH_FASTCALL, nullptr},
         {"embedding_lookup", method(embedding_lookup), METH_FASTCALL, nullptr},
         {"embedding_grad", method(embedding_grad), METH_FASTCALL, nullptr},
+        {"rotary", method(rotary), METH_FASTCALL, nullptr},
+        {"qk_norm_rotary", method(qk_norm_rotary), METH_FASTCALL, nullptr},
+        {"qk_norm_rotary_grad", method(qk_norm_rotary_grad), METH_FASTCALL, nullptr},
         {nullptr, nullptr, 0, nullptr}};
     static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
     return PyModule_Create(&module);

@@ -1,0 +1,562 @@
+// Queries and keys of a replica's attention for gfx950 (MI355X): rotated by their positions, and normed for each head in the
+// same pass, with the gradient of that.
+//
+// A head of `d` channels is d / 2 pairs: pair i turns by position * frequencies[i] for i < r, and not at all behind.  A lane
+// holds V pairs of a head, L = 2^n lanes a head, 64 / L heads a wave at once; a wave takes a token (or, where there are few,
+// a share of its heads) and keeps the cosines and sines of its pairs for all of the token's heads.  Angles are formed in 64 bits
+// as turns, position * (frequency / 2 pi), of which only the fraction is kept: fp32 would be off by 2^-24 of the whole
+// angle, 1e-2 at position 131072.  Everything else is fp32, rounded once to the tensors' type.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "plan.h"
+#include "sparseloco.h"
+
+namespace {
+
+using namespace splc;
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMostDim = SPLC_MAX_HEAD_DIM;
+constexpr uint32_t kFillingWaves = 4096;                     // four a SIMD: where a token's heads are no longer shared out
+constexpr uint32_t kMostGroups = 1u << 20;                   // workgroups of a launch: those lanes are counted in 32 bits
+constexpr uint32_t kGradGroups = 1024, kJoinRows = 16;
+
+template <class T>
+struct View {
+    T* at;
+    int64_t token, head;                                     // strides in elements
+    int heads;
+};
+struct Rotation {
+    const void* positions;
+    const double* frequencies;
+    int wide;                                                // positions in 64 bits
+    int r;                                                   // pairs that turn
+    float magnitude, sign;
+};
+
+template <class T, int V>
+struct Vector {
+    typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+};
+template <class T>
+struct Vector<T, 1> {
+    typedef T type;
+};
+
+__device__ __forceinline__ float wide_of(float v) { return v; }
+__device__ __forceinline__ float wide_of(uint16_t v) { return widened(v); }
+
+template <class T, int V>
+__device__ __forceinline__ void load_wide(const T* p, float* x) {
+    const auto v = *(const SPLC_GLOBAL typename Vector<T, V>::type*)p;
+    if constexpr (V == 1) {
+        x[0] = wide_of(v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = wide_of(v[j]);
+    }
+}
+template <int V>
+__device__ __forceinline__ void store_narrow(float* p, const float* x) {
+    typename Vector<float, V>::type v;
+    if constexpr (V == 1) {
+        v = x[0];
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = x[j];
+    }
+    *(SPLC_GLOBAL typename Vector<float, V>::type*)p = v;
+}
+template <int V>
+__device__ __forceinline__ void store_narrow(uint16_t* p, const float* x) {
+    if constexpr (V == 1) {
+        *(SPLC_GLOBAL uint16_t*)p = (uint16_t)bf16_pair(x[0], 0.f);
+    } else {
+        typedef uint32_t words __attribute__((ext_vector_type(V / 2)));
+        words w;
+        if constexpr (V == 2) {
+            w = bf16_pair(x[0], x[1]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) w[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
+        }
+        *(SPLC_GLOBAL typename Vector<uint16_t, V>::type*)p = __builtin_bit_cast(typename Vector<uint16_t, V>::type, w);
+    }
+}
+
+// Pairs of a head as a lane holds them: C runs of V.  Of pair p the first coordinate is x[..][j], the second x[..][V + j] where
+// the halves lie apart; where pairs lie side by side x holds 2 V channels in their order.
+template <class T, int V, bool SIDE>
+struct Lanes {
+    static constexpr int C = V == 1 ? 4 : V == 2 ? 2 : 1;    // 64 lanes x C x V pairs: 512 channels at the least
+    int first[C], second[C];                                 // where the run's first and second V channels begin
+    bool there[C];
+
+    __device__ __forceinline__ Lanes(int lane, int per_head, int d, int r) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int p = (lane + c * per_head) * V;
+            there[c] = p < d / 2;
+            if (SIDE) {
+                first[c] = 2 * p;
+                second[c] = 2 * p + V;
+            } else if (p < r) {
+                first[c] = p;
+                second[c] = p + r;
+            } else {                                         // behind the rotated channels, halved likewise
+                first[c] = p + r;
+                second[c] = p + d / 2;
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const T* head, float (&x)[C][2 * V]) const {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (there[c]) {
+                load_wide<T, V>(head + first[c], x[c]);
+                load_wide<T, V>(head + second[c], x[c] + V);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 2 * V; ++j) x[c][j] = 0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T* head, const float (&x)[C][2 * V]) const {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (there[c]) {
+                store_narrow<V>(head + first[c], x[c]);
+                store_narrow<V>(head + second[c], x[c] + V);
+            }
+        }
+    }
+};
+
+template <int V, int C>
+struct Turn {
+    float cos[C][V], sin[C][V];
+
+    __device__ __forceinline__ void at(const Rotation& how, int64_t token, int lane, int per_head) {
+        const double position = how.wide ? (double)static_cast<const int64_t*>(how.positions)[token]
+                                         : (double)static_cast<const int32_t*>(how.positions)[token];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int p = (lane + c * per_head) * V + j;
+                cos[c][j] = 1.f;
+                sin[c][j] = 0.f;
+                if (p < how.r) {
+                    const double turns = position * (how.frequencies[p] * 0.15915494309189533577);
+                    sincospif(2.f * (float)(turns - rint(turns)), &sin[c][j], &cos[c][j]);
+                    cos[c][j] *= how.magnitude;
+                    sin[c][j] *= how.magnitude * how.sign;
+                }
+            }
+        }
+    }
+    // (x, y) by the angle; BACK: by its opposite.
+    template <bool SIDE, bool BACK>
+    __device__ __forceinline__ void turn(float (&x)[C][2 * V]) const {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float &a = x[c][SIDE ? 2 * j : j], &b = x[c][SIDE ? 2 * j + 1 : V + j];
+                const float s = BACK ? -sin[c][j] : sin[c][j], u = a, v = b;
+                a = fmaf(u, cos[c][j], -(v * s));
+                b = fmaf(v, cos[c][j], u * s);
+            }
+        }
+    }
+};
+
+// Sum over the lanes of a head, in all of them.
+__device__ __forceinline__ float head_sum(float x, int per_head) {
+    for (int step = per_head >> 1; step > 0; step >>= 1) x += __shfl_xor(x, step);
+    return x;
+}
+template <int N, int C>
+__device__ __forceinline__ float dot(const float (&x)[C][N], const float (&y)[C][N]) {
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum = fmaf(x[c][j], y[c][j], sum);
+    }
+    return sum;
+}
+template <class T, int V, bool SIDE, int C>
+__device__ __forceinline__ void load_gain(const Lanes<T, V, SIDE>& lanes, const void* gain, int bf16, float (&w)[C][2 * V]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int j = 0; j < 2 * V; ++j) {
+            const int at = j < V ? lanes.first[c] + j : lanes.second[c] + j - V;
+            w[c][j] = !lanes.there[c] ? 0.f
+                      : bf16          ? widened(static_cast<const uint16_t*>(gain)[at])
+                                      : static_cast<const float*>(gain)[at];
+        }
+    }
+}
+
+// How a launch's waves share the tokens: wave i takes heads `part`, part + parts, ... (in runs of 64 / L) of token i / parts.
+struct Shares {
+    int64_t tokens;
+    int d, per_head, lane_bits, parts;
+};
+
+template <class T>
+struct Forward {
+    View<const T> in[2];
+    View<T> out[2];
+    const void* gain[2];
+    int gain_bf16;
+    float eps, inverse_d;
+};
+
+template <class T, int V, bool SIDE, bool NORM>
+__global__ __launch_bounds__(kThreads) void heads_kernel(Forward<T> args, Rotation how, Shares share) {
+    using Mine = Lanes<T, V, SIDE>;
+    constexpr int C = Mine::C;
+    const int lane = threadIdx.x & 63, in_head = lane & (share.per_head - 1), slot = lane >> share.lane_bits;
+    const int at_once = 64 >> share.lane_bits;
+    const Mine mine(in_head, share.per_head, share.d, how.r);
+    const int64_t items = share.tokens * share.parts;
+    for (int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * kWaves) {
+        const int64_t token = item / share.parts;
+        int run = (int)(item - token * share.parts);
+        Turn<V, C> turn;
+        turn.at(how, token, in_head, share.per_head);
+        for (int side = 0; side < 2; ++side) {
+            const View<const T> in = args.in[side];
+            const View<T> out = args.out[side];
+            const int runs = (in.heads + at_once - 1) / at_once;
+            float w[C][2 * V];
+            if (NORM && run < runs) load_gain(mine, args.gain[side], args.gain_bf16, w);
+            for (; run < runs; run += share.parts) {
+                const int head = run * at_once + slot;
+                if (head >= in.heads) continue;              // (sums below are among the lanes of one head)
+                float x[C][2 * V];
+                mine.load(in.at + token * in.token + head * in.head, x);
+                if (NORM) {
+                    const float inverse = rsqrtf(fmaf(head_sum(dot(x, x), share.per_head), args.inverse_d, args.eps));
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+#pragma unroll
+                        for (int j = 0; j < 2 * V; ++j) x[c][j] = x[c][j] * inverse * w[c][j];
+                    }
+                }
+                turn.template turn<SIDE, false>(x);
+                mine.store(out.at + token * out.token + head * out.head, x);
+            }
+            run -= runs;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- gradient
+//
+// With n = 1 / sqrt(mean x^2 + eps), y = R (w x n), and g = R^T dy:  dw = sum of g x n over tokens and heads,
+// h = g w,  dx = n (h - x n mean(h x n)).  x is read again: n is one number for two passes over a head's registers.
+// Sums of dw stay in a lane's registers over all of its tokens; a workgroup's are joined in LDS, and the workgroups' by
+// join_kernel, each in an order that the sizes alone decide.
+template <class T>
+struct Backward {
+    View<const T> dy[2], x[2];
+    View<T> dx[2];
+    const void* gain[2];
+    int gain_bf16;
+    float eps, inverse_d;
+    float* partial;                                          // [workgroup][2][d]
+};
+
+template <class T, int V, bool SIDE>
+__global__ __launch_bounds__(kThreads) void heads_grad_kernel(Backward<T> args, Rotation how, Shares share) {
+    using Mine = Lanes<T, V, SIDE>;
+    constexpr int C = Mine::C;
+    __shared__ float sums[kWaves][kMostDim];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in_head = lane & (share.per_head - 1), slot = lane >> share.lane_bits;
+    const int at_once = 64 >> share.lane_bits;
+    const Mine mine(in_head, share.per_head, share.d, how.r);
+    const int64_t items = share.tokens * share.parts;
+    float dw[2][C][2 * V], w[2][C][2 * V];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        if (args.x[side].heads > 0) load_gain(mine, args.gain[side], args.gain_bf16, w[side]);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int j = 0; j < 2 * V; ++j) dw[side][c][j] = 0.f;
+        }
+    }
+    for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
+        const int64_t token = item / share.parts;
+        int run = (int)(item - token * share.parts);
+        Turn<V, C> turn;
+        turn.at(how, token, in_head, share.per_head);
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const int heads = args.x[side].heads, runs = (heads + at_once - 1) / at_once;
+            for (; run < runs; run += share.parts) {
+                const int head = run * at_once + slot;
+                if (head >= heads) continue;
+                float x[C][2 * V], g[C][2 * V];
+                mine.load(args.x[side].at + token * args.x[side].token + head * args.x[side].head, x);
+                mine.load(args.dy[side].at + token * args.dy[side].token + head * args.dy[side].head, g);
+                const float inverse = rsqrtf(fmaf(head_sum(dot(x, x), share.per_head), args.inverse_d, args.eps));
+                turn.template turn<SIDE, true>(g);
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+#pragma unroll
+                    for (int j = 0; j < 2 * V; ++j) {
+                        x[c][j] *= inverse;
+                        dw[side][c][j] = fmaf(g[c][j], x[c][j], dw[side][c][j]);
+                        g[c][j] *= w[side][c][j];
+                    }
+                }
+                const float mean = head_sum(dot(g, x), share.per_head) * args.inverse_d;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+#pragma unroll
+                    for (int j = 0; j < 2 * V; ++j) x[c][j] = inverse * fmaf(-mean, x[c][j], g[c][j]);
+                }
+                mine.store(args.dx[side].at + token * args.dx[side].token + head * args.dx[side].head, x);
+            }
+            run -= runs;
+        }
+    }
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        if (side == 1) __syncthreads();
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int j = 0; j < 2 * V; ++j) {
+                float sum = dw[side][c][j];
+                for (int step = share.per_head; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
+                if (slot == 0 && mine.there[c]) sums[wave][j < V ? mine.first[c] + j : mine.second[c] + j - V] = sum;
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < share.d; i += kThreads) {
+            float sum = sums[0][i];
+#pragma unroll
+            for (int v = 1; v < kWaves; ++v) sum += sums[v][i];
+            args.partial[((int64_t)blockIdx.x * 2 + side) * share.d + i] = sum;
+        }
+    }
+}
+
+// Sums of the workgroups' partial sums, 16 channels a workgroup.
+__global__ __launch_bounds__(kThreads) void heads_join_kernel(const float* __restrict__ partial, int groups, int d, float* dq_gain,
+                                                              float* dk_gain, int accumulate) {
+    __shared__ float sums[kThreads];
+    const int i = blockIdx.x * kJoinRows + threadIdx.x % kJoinRows;
+    float sum = 0.f;
+    if (i < 2 * d) {
+#pragma unroll 8
+        for (int g = threadIdx.x / kJoinRows; g < groups; g += kThreads / kJoinRows) sum += partial[(int64_t)g * 2 * d + i];
+    }
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x >= kJoinRows || i >= 2 * d) return;
+    for (int part = 1; part < kThreads / (int)kJoinRows; ++part) sum += sums[part * kJoinRows + threadIdx.x];
+    float* out = i < d ? dq_gain : dk_gain;
+    if (!out) return;
+    out += i < d ? i : i - d;
+    *out = accumulate ? *out + sum : sum;
+}
+
+// ---------------------------------------------------------------- host
+
+int units() {
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1)
+        return 256;
+    return n;
+}
+
+bool fine_rotation(const sparseloco_rotation* how, int d) {
+    return how && how->positions && how->frequencies && (how->position_bytes == 4 || how->position_bytes == 8) && how->pairs >= 1 &&
+           how->pairs <= d / 2 && std::isfinite((float)how->magnitude);
+}
+
+// A list of heads can be walked: strides that keep every offset in 62 bits, and for one that is written to no element twice.
+bool fine_heads(const sparseloco_heads* h, int64_t tokens, int d, bool written) {
+    constexpr int64_t kFar = (int64_t)1 << 40;
+    if (h->heads < 0 || h->heads > SPLC_MAX_HEADS) return false;
+    if (h->heads == 0 || tokens == 0) return true;
+    if (!h->data || h->token_stride < 0 || h->head_stride < 0 || h->token_stride > kFar || h->head_stride > kFar) return false;
+    if (tokens > 1 && h->token_stride > ((int64_t)1 << 61) / tokens) return false;
+    if (!written) return true;
+    const int64_t s = h->token_stride, t = h->head_stride;
+    const bool by_token = (tokens == 1 || s >= (h->heads - 1) * t + d) && (h->heads == 1 || t >= d);
+    const bool by_head = (h->heads == 1 || t >= (tokens - 1) * s + d) && (tokens == 1 || s >= d);
+    return by_token || by_head;
+}
+
+// Arguments that all three operators share; `lists`: queries and keys of the inputs and the outputs, keys NULL in all or none.
+struct List {
+    const sparseloco_heads *q, *k;
+    bool written;
+};
+int check(const List* lists, int n, int dtype, int64_t tokens, int d, const sparseloco_rotation* how) {
+    if ((dtype != SPLC_F32 && dtype != SPLC_BF16) || tokens < 0 || tokens > INT32_MAX || d < 2 || d > kMostDim || d % 2 != 0)
+        return SPLC_EINVAL;
+    for (int i = 0; i < n; ++i) {
+        if (!lists[i].q || (lists[i].k == nullptr) != (lists[0].k == nullptr)) return SPLC_EINVAL;
+        if (lists[i].q->heads != lists[0].q->heads || (lists[i].k && lists[i].k->heads != lists[0].k->heads)) return SPLC_EINVAL;
+        if (!fine_heads(lists[i].q, tokens, d, lists[i].written) || (lists[i].k && !fine_heads(lists[i].k, tokens, d, lists[i].written)))
+            return SPLC_EINVAL;
+    }
+    if (tokens > 0 && !fine_rotation(how, d)) return SPLC_EINVAL;
+    const size_t size = dtype == SPLC_F32 ? 4 : 2;
+    for (int i = 0; i < n; ++i)
+        if (!aligned(lists[i].q->data, size) || (lists[i].k && !aligned(lists[i].k->data, size))) return SPLC_EALIGN;
+    if (tokens > 0 && (!aligned(how->positions, (size_t)how->position_bytes) || !aligned(how->frequencies, 8))) return SPLC_EALIGN;
+    return SPLC_OK;
+}
+int check_gains(const void* q_gain, const void* k_gain, int gain_dtype, double eps, bool keys) {
+    if ((gain_dtype != SPLC_F32 && gain_dtype != SPLC_BF16) || !q_gain || (keys && !k_gain)) return SPLC_EINVAL;
+    if (!std::isfinite((float)eps) || eps < 0.0) return SPLC_EINVAL;
+    const size_t size = gain_dtype == SPLC_F32 ? 4 : 2;
+    return aligned(q_gain, size) && aligned(k_gain, size) ? SPLC_OK : SPLC_EALIGN;
+}
+
+template <class T>
+View<T> view(const sparseloco_heads* h) {
+    if (!h) return {nullptr, 0, 0, 0};
+    return {static_cast<T*>(h->data), h->token_stride, h->head_stride, h->heads};
+}
+Rotation rotation(const sparseloco_rotation* how, bool inverse) {
+    return {how->positions, how->frequencies, how->position_bytes == 8, how->pairs, (float)how->magnitude, inverse ? -1.f : 1.f};
+}
+
+// Pairs that a lane holds side by side: 16 bytes' worth, or as many as all runs can have.
+int run_of_pairs(int dtype, int d, int r, bool side) {
+    for (int v = dtype == SPLC_BF16 ? 8 : 4; v > 1; v /= 2)
+        if (side ? d / 2 % v == 0 : r % v == 0 && (d / 2 - r) % v == 0) return v;
+    return 1;
+}
+
+Shares shares(int64_t tokens, int d, int v, int q_heads, int k_heads) {
+    Shares s{tokens, d, 1, 0, 1};
+    while (s.per_head * v < d / 2 && s.per_head < 64) {
+        s.per_head *= 2;
+        ++s.lane_bits;
+    }
+    const int at_once = 64 / s.per_head;
+    const int runs = (q_heads + at_once - 1) / at_once + (k_heads + at_once - 1) / at_once;
+    s.parts = (int)std::min<int64_t>(runs, std::max<int64_t>(1, kFillingWaves / std::max<int64_t>(tokens, 1)));
+    return s;
+}
+
+template <class Run>
+int with_variant(int dtype, int v, bool side, Run run) {
+    auto of = [&](auto type, auto width) {
+        if (side) run(type, width, std::true_type());
+        else run(type, width, std::false_type());
+    };
+    auto narrow = [&](auto type) {
+        if (v == 4) of(type, std::integral_constant<int, 4>());
+        else if (v == 2) of(type, std::integral_constant<int, 2>());
+        else of(type, std::integral_constant<int, 1>());
+    };
+    if (dtype == SPLC_F32) narrow(float());
+    else if (v == 8) of(uint16_t(), std::integral_constant<int, 8>());
+    else narrow(uint16_t());
+    return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
+}
+
+template <bool NORM>
+int forward(const List& in, const List& out, int dtype, int64_t tokens, int d, const void* q_gain, const void* k_gain, int gain_dtype,
+            double eps, const sparseloco_rotation* how, bool inverse, void* stream) {
+    const int q_heads = in.q->heads, k_heads = in.k ? in.k->heads : 0;
+    if (tokens == 0 || q_heads + k_heads == 0) return SPLC_OK;
+    const bool side = how->interleaved != 0;
+    const int v = run_of_pairs(dtype, d, how->pairs, side);
+    const Shares s = shares(tokens, d, v, q_heads, k_heads);
+    const uint32_t groups = (uint32_t)std::min<int64_t>((tokens * s.parts + kWaves - 1) / kWaves, kMostGroups);
+    return with_variant(dtype, v, side, [&](auto type, auto width, auto pairs_side) {
+        using T = decltype(type);
+        const Forward<T> args{{view<const T>(in.q), view<const T>(in.k)}, {view<T>(out.q), view<T>(out.k)}, {q_gain, k_gain},
+                              gain_dtype == SPLC_BF16, (float)eps, 1.f / (float)d};
+        hipLaunchKernelGGL((heads_kernel<T, decltype(width)::value, decltype(pairs_side)::value, NORM>), dim3(groups), dim3(kThreads), 0,
+                           static_cast<hipStream_t>(stream), args, rotation(how, inverse), s);
+    });
+}
+
+uint32_t grad_groups(int64_t tokens) { return (uint32_t)std::min<int64_t>(std::max<int64_t>(tokens, 1), kGradGroups); }
+
+}  // namespace
+
+extern "C" {
+
+int sparseloco_rotary(const sparseloco_heads* q, const sparseloco_heads* k, int dtype, int64_t tokens, int head_dim,
+                      const sparseloco_rotation* how, int inverse, const sparseloco_heads* q_out, const sparseloco_heads* k_out,
+                      void* stream) {
+    const List lists[] = {{q, k, false}, {q_out, k_out, true}};
+    const int rc = check(lists, 2, dtype, tokens, head_dim, how);
+    if (rc != SPLC_OK) return rc;
+    return forward<false>(lists[0], lists[1], dtype, tokens, head_dim, nullptr, nullptr, SPLC_F32, 0.0, how, inverse != 0, stream);
+}
+
+int sparseloco_qk_norm_rotary(const sparseloco_heads* q, const sparseloco_heads* k, int dtype, int64_t tokens, int head_dim,
+                              const void* q_gain, const void* k_gain, int gain_dtype, double eps, const sparseloco_rotation* how,
+                              const sparseloco_heads* q_out, const sparseloco_heads* k_out, void* stream) {
+    const List lists[] = {{q, k, false}, {q_out, k_out, true}};
+    int rc = check(lists, 2, dtype, tokens, head_dim, how);
+    if (rc != SPLC_OK) return rc;
+    if ((rc = check_gains(q_gain, k_gain, gain_dtype, eps, k != nullptr)) != SPLC_OK) return rc;
+    return forward<true>(lists[0], lists[1], dtype, tokens, head_dim, q_gain, k_gain, gain_dtype, eps, how, false, stream);
+}
+
+int64_t sparseloco_qk_norm_rotary_grad_ws_bytes(int64_t tokens, int q_heads, int k_heads, int head_dim) {
+    if (tokens < 0 || tokens > INT32_MAX || q_heads < 0 || q_heads > SPLC_MAX_HEADS || k_heads < 0 || k_heads > SPLC_MAX_HEADS ||
+        head_dim < 2 || head_dim > kMostDim || head_dim % 2 != 0)
+        return SPLC_EINVAL;
+    return (int64_t)grad_groups(tokens) * 2 * head_dim * 4;
+}
+
+int sparseloco_qk_norm_rotary_grad(const sparseloco_heads* grad_q_out, const sparseloco_heads* grad_k_out, const sparseloco_heads* q,
+                                   const sparseloco_heads* k, int dtype, int64_t tokens, int head_dim, const void* q_gain,
+                                   const void* k_gain, int gain_dtype, double eps, const sparseloco_rotation* how,
+                                   const sparseloco_heads* grad_q, const sparseloco_heads* grad_k, float* grad_q_gain,
+                                   float* grad_k_gain, int accumulate, void* ws, int64_t ws_bytes, void* stream) {
+    const List lists[] = {{grad_q_out, grad_k_out, false}, {q, k, false}, {grad_q, grad_k, true}};
+    int rc = check(lists, 3, dtype, tokens, head_dim, how);
+    if (rc != SPLC_OK) return rc;
+    if ((rc = check_gains(q_gain, k_gain, gain_dtype, eps, k != nullptr)) != SPLC_OK) return rc;
+    const int q_heads = q->heads, k_heads = k ? k->heads : 0;
+    if (!grad_q_gain || (k != nullptr) != (grad_k_gain != nullptr) || !ws) return SPLC_EINVAL;
+    if (ws_bytes < sparseloco_qk_norm_rotary_grad_ws_bytes(tokens, q_heads, k_heads, head_dim)) return SPLC_EINVAL;
+    if (!aligned(grad_q_gain, 4) || !aligned(grad_k_gain, 4) || !aligned(ws, 4)) return SPLC_EALIGN;
+    uint32_t groups = 0;
+    if (tokens > 0 && q_heads + k_heads > 0) {
+        const bool side = how->interleaved != 0;
+        const int v = run_of_pairs(dtype, head_dim, how->pairs, side);
+        const Shares s = shares(tokens, head_dim, v, q_heads, k_heads);
+        groups = (uint32_t)std::min<int64_t>((tokens * s.parts + kWaves - 1) / kWaves, grad_groups(tokens));
+        rc = with_variant(dtype, v, side, [&](auto type, auto width, auto pairs_side) {
+            using T = decltype(type);
+            const Backward<T> args{{view<const T>(grad_q_out), view<const T>(grad_k_out)}, {view<const T>(q), view<const T>(k)},
+                                   {view<T>(grad_q), view<T>(grad_k)}, {q_gain, k_gain}, gain_dtype == SPLC_BF16, (float)eps,
+                                   1.f / (float)head_dim, static_cast<float*>(ws)};
+            hipLaunchKernelGGL((heads_grad_kernel<T, decltype(width)::value, decltype(pairs_side)::value>), dim3(groups), dim3(kThreads),
+                               0, static_cast<hipStream_t>(stream), args, rotation(how, false), s);
+        });
+        if (rc != SPLC_OK) return rc;
+    }
+    hipLaunchKernelGGL(heads_join_kernel, dim3((2 * head_dim + kJoinRows - 1) / kJoinRows), dim3(kThreads), 0,
+                       static_cast<hipStream_t>(stream), static_cast<const float*>(ws), (int)groups, head_dim, grad_q_gain, grad_k_gain,
+                       accumulate);
+    return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
+}
+
+}  // extern "C"

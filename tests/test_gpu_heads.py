@@ -1,0 +1,330 @@
+"""Rotary positions and normed heads on the GPU against a plain implementation in 64 bits.
+
+Tolerances, in steps of 2^-24 (u): a head's sum of squares is a chain of at most 16 products and 6 halvings, so its root's inverse is
+off by at most 12 u and the 2 u of the instruction; x n w adds 2 u, cosine and sine 4 u each (2^-22), the magnitude 1 u, the
+rotation's two operations 2 u: 23 u of |x| + |y|, taken as 32.  The result is rounded once, by half a step of its type.
+Gradient: g 8 u of its parts, x n 15 u, the mean over a head (23 + 8 + 15) u of the mean of magnitudes, the factor n 14 u: taken as
+24 u and 80 u of the two terms.  A gain's gradient adds its terms (23 u each) in a chain of at most the heads that a wave
+walks, and 120 for the joins."""
+import math
+
+import pytest
+import torch
+
+from paper_2601_02360_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def turned(x, positions, frequencies, magnitude, interleaved, back=False, absolute=False):
+    """The rotation of [tokens, heads, d] in 64 bits; absolute: magnitude (|x| + |y|) for every rotated coordinate."""
+    r = len(frequencies)
+    a = positions.double()[:, None, None] * frequencies
+    cos, sin = magnitude * a.cos(), magnitude * (-a.sin() if back else a.sin())
+    out = x.clone()
+    i = torch.arange(r, device=x.device)
+    first, second = (2 * i, 2 * i + 1) if interleaved else (i, r + i)
+    if absolute:
+        total = abs(magnitude) * (x[..., first].abs() + x[..., second].abs())
+        out = x.abs()
+        out[..., first], out[..., second] = total, total
+        return out
+    out[..., first] = x[..., first] * cos - x[..., second] * sin
+    out[..., second] = x[..., second] * cos + x[..., first] * sin
+    return out
+
+
+def normed(x, gain, eps):
+    return gain * x / (x.square().mean(-1, keepdim=True) + eps).sqrt()
+
+
+def gradient(dy, x, gain, positions, frequencies, magnitude, interleaved, eps):
+    """(dx, dgain) and the bounds of their errors in steps of u."""
+    n = 1 / (x.square().mean(-1, keepdim=True) + eps).sqrt()
+    unit, g = x * n, turned(dy, positions, frequencies, magnitude, interleaved, back=True)
+    s = turned(dy, positions, frequencies, magnitude, interleaved, absolute=True)
+    h, sh = g * gain, s * gain.abs()
+    dx = n * (h - unit * (h * unit).mean(-1, keepdim=True))
+    bound = n * (24 * sh + 80 * unit.abs() * (sh * unit.abs()).mean(-1, keepdim=True))
+    tokens, heads = x.shape[:2]
+    chain = 23 + heads * -(-tokens // 1024) + 120
+    return dx, (g * unit).sum((0, 1)), bound, chain * (s * unit.abs()).sum((0, 1))
+
+
+def close(got, want, bound):
+    """Within u bound and half a step of the result's type."""
+    wide = got.double()
+    limit = bound * U + (want.abs() + bound * U) * half_step(got.dtype) + torch.finfo(got.dtype).tiny
+    off = ((wide - want).abs() / limit)
+    assert torch.isfinite(wide).all() and off.max() <= 1, "off by %.3g of the bound" % off.max()
+
+
+def lists(tokens, hq, hk, d, dtype, seed, packed=True, scale=1.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(tokens, (hq + 2 * hk) * d + 3, generator=gen, device="cuda") * scale
+    x = x.to(dtype)
+    if not packed:
+        return x[:, :hq * d].reshape(tokens, hq, d).clone(), x[:, hq * d:(hq + hk) * d].reshape(tokens, hk, d).clone()
+    return x[:, :hq * d].unflatten(1, (hq, d)), x[:, hq * d:(hq + hk) * d].unflatten(1, (hk, d))
+
+
+CASES = [
+    # tokens, query heads, key heads, channels, pairs, type, gains, side by side, packed, positions, magnitude
+    (1, 1, 1, 2, 1, torch.float32, torch.float32, False, False, "near", 1.0),
+    (1, 32, 8, 128, 64, torch.bfloat16, torch.bfloat16, False, True, "far", 1.3),
+    (1, 32, 8, 128, 64, torch.float32, torch.bfloat16, True, True, "wide", 1.0),
+    (37, 12, 12, 64, 32, torch.float32, torch.float32, False, True, "near", 1.0),
+    (100, 3, 1, 128, 16, torch.bfloat16, torch.float32, True, True, "near", 1.0),
+    (101, 5, 2, 72, 36, torch.bfloat16, torch.bfloat16, False, True, "far", 1.0),
+    (65, 20, 4, 80, 40, torch.float32, torch.float32, True, False, "near", 1.0),
+    (33, 2, 1, 96, 17, torch.bfloat16, torch.bfloat16, False, True, "near", 1.0),
+    (33, 2, 1, 96, 17, torch.float32, torch.float32, True, True, "wide", 0.5),
+    (9, 1, 1, 100, 25, torch.bfloat16, torch.bfloat16, True, False, "near", 1.0),
+    (9, 7, 3, 6, 2, torch.bfloat16, torch.float32, False, True, "wide", 1.0),
+    (17, 2, 2, 512, 256, torch.float32, torch.float32, False, True, "near", 1.0),
+    (17, 2, 2, 512, 255, torch.bfloat16, torch.bfloat16, False, True, "near", 1.0),
+    (13, 3, 2, 508, 127, torch.float32, torch.bfloat16, True, True, "far", 1.0),
+    (13, 3, 2, 256, 2, torch.bfloat16, torch.bfloat16, False, True, "near", 1.0),
+    (5000, 4, 4, 64, 32, torch.bfloat16, torch.float32, False, True, "near", 1.0),
+    (4099, 3, 1, 40, 20, torch.float32, torch.float32, True, True, "wide", 1.0),
+]
+
+
+def positions_of(kind, tokens, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    if kind == "near":
+        return (torch.arange(tokens, device="cuda") % 29).to(torch.int32)
+    if kind == "far":
+        return torch.randint(0, 131072, (tokens,), generator=gen, device="cuda", dtype=torch.int32)
+    return torch.randint(-2 ** 40, 2 ** 40, (tokens,), generator=gen, device="cuda") // 2 ** 12
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(str(v) for v in c[:5]))
+def test_heads(case):
+    tokens, hq, hk, d, r, dtype, gain_type, side, packed, far, magnitude = case
+    q, k = lists(tokens, hq, hk, d, dtype, 1, packed)
+    positions = positions_of(far, tokens, 2)
+    f, _ = B.rotary_frequencies(2 * r)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    w = [(1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(gain_type) for _ in range(2)]
+    how = dict(interleaved=side, magnitude=magnitude)
+    angle = (positions, f, magnitude, side)
+
+    outs = [torch.full((tokens, h, d), float("nan"), dtype=dtype, device="cuda") for h in (hq, hk)]
+    for inverse in (False, True):
+        B.sparseloco_rotary(q, k, positions, f, *outs, inverse=inverse, **how)
+        for x, out in zip((q, k), outs):
+            close(out, turned(x.double(), *angle, back=inverse), 32 * turned(x.double(), *angle, absolute=True))
+            tail = slice(2 * r, d)
+            assert torch.equal(out[..., tail], x[..., tail])
+            out.fill_(float("nan"))
+    eps = 1e-5
+    B.sparseloco_qk_norm_rotary(q, k, *w, positions, f, *outs, eps=eps, **how)
+    for x, gain, out in zip((q, k), w, outs):
+        y = normed(x.double(), gain.double(), eps)
+        close(out, turned(y, *angle), 32 * turned(y, *angle, absolute=True))
+
+    dq, dk = lists(tokens, hq, hk, d, dtype, 4, packed, 1e-3)
+    for accumulate in (False, True):
+        dx = [torch.full((tokens, h, d), float("nan"), dtype=dtype, device="cuda") for h in (hq, hk)]
+        sums = [torch.full((d,), 0.25 if accumulate else float("nan"), device="cuda") for _ in range(2)]
+        ws = B.qk_norm_rotary_workspace(tokens, hq, hk, d).fill_(255)
+        B.sparseloco_qk_norm_rotary_grad(dq, dk, q, k, *w, positions, f, *dx, *sums, ws, eps=eps, accumulate=accumulate, **how)
+        for dy, x, gain, out, total in zip((dq, dk), (q, k), w, dx, sums):
+            want, dgain, bound, sum_bound = gradient(dy.double(), x.double(), gain.double(), *angle, eps)
+            close(out, want, bound)
+            base = 0.25 if accumulate else 0.0
+            close(total, dgain + base, sum_bound + base)
+
+
+def test_the_formula_of_the_gradient_against_differences():
+    gen = torch.Generator().manual_seed(0)
+    x, dy = (torch.randn(2, 2, 12, generator=gen, dtype=torch.float64) for _ in range(2))
+    gain = 1 + 0.2 * torch.randn(12, generator=gen, dtype=torch.float64)
+    positions, f = torch.tensor([3, 70]), torch.tensor([1.0, 0.3, 0.01], dtype=torch.float64)
+    for side in (False, True):
+        def value(x, gain):
+            return float((turned(normed(x, gain, 1e-3), positions, f, 1.2, side) * dy).sum())
+        dx, dgain, _, _ = gradient(dy, x, gain, positions, f, 1.2, side, 1e-3)
+        h = 1e-5                                             # differences: h^2 of the third derivative, and 2^-52 / h of the value
+        for i in range(x.numel()):
+            e = torch.zeros(x.numel(), dtype=torch.float64)
+            e[i] = h
+            e = e.view(x.shape)
+            assert abs((value(x + e, gain) - value(x - e, gain)) / (2 * h) - float(dx.flatten()[i])) < 1e-7
+        for i in range(12):
+            e = torch.zeros(12, dtype=torch.float64)
+            e[i] = h
+            assert abs((value(x, gain + e) - value(x, gain - e)) / (2 * h) - float(dgain[i])) < 1e-7
+
+
+def test_the_kernel_against_differences():
+    """The operator's own outputs a step apart, in fp32: off by 2^-20 of the sum of magnitudes over the step at most."""
+    q, _ = lists(3, 2, 0, 8, torch.float32, 5, False)
+    dy, _ = lists(3, 2, 0, 8, torch.float32, 6, False)
+    w = torch.linspace(0.5, 1.5, 8, device="cuda")
+    positions, (f, _) = torch.tensor([0, 5, 900], dtype=torch.int32, device="cuda"), B.rotary_frequencies(8)
+    dq, dw, ws = torch.empty_like(q), torch.empty(8, device="cuda"), B.qk_norm_rotary_workspace(3, 2, 0, 8)
+    B.sparseloco_qk_norm_rotary_grad(dy, None, q, None, w, None, positions, f, dq, None, dw, None, ws)
+
+    def value(x, gain):
+        out = torch.empty_like(x)
+        B.sparseloco_qk_norm_rotary(x, None, gain, None, positions, f, out, None)
+        return float((out.double() * dy.double()).sum()), float((out.double() * dy.double()).abs().sum())
+    h = 2.0 ** -6
+    for i in range(0, q.numel(), 5):
+        up, down = q.clone().flatten(), q.clone().flatten()
+        up[i] += h
+        down[i] -= h
+        (a, size), (b, _) = value(up.view_as(q), w), value(down.view_as(q), w)
+        x = q.double().flatten().view(3, 2, 8)[i // 16, i // 8 % 2]
+        n = float(1 / (x.square().mean() + 1e-6).sqrt())
+        # third derivative of x / |x| in one coordinate: below 15 / |x|^3 of its gain and gradient, over a head's 8
+        curve = 15 * n ** 3 * float(dy.abs().sum()) * 1.5 * h * h / 6 * 2
+        assert abs((a - b) / (2 * h) - float(dq.flatten()[i])) <= curve + size * 2.0 ** -20 / h
+    for i in range(8):
+        up, down = w.clone(), w.clone()
+        up[i] += h
+        down[i] -= h
+        (a, size), (b, _) = value(q, up), value(q, down)
+        assert abs((a - b) / (2 * h) - float(dw[i])) <= size * 2.0 ** -20 / h
+
+
+def test_in_place_and_other_strides():
+    tokens, hq, hk, d, r = 50, 6, 2, 64, 20
+    positions, (f, _) = positions_of("near", tokens, 1), B.rotary_frequencies(2 * r)
+    w = torch.linspace(0.5, 1.5, d, device="cuda").bfloat16()
+    for dtype in (torch.float32, torch.bfloat16):
+        q, k = lists(tokens, hq, hk, d, dtype, 7, False)
+        dq, dk = lists(tokens, hq, hk, d, dtype, 8, False)
+        want, back = [torch.empty_like(t) for t in (q, k)], [torch.empty_like(t) for t in (q, k)]
+        sums = [torch.empty(d, device="cuda") for _ in range(4)]
+        ws = B.qk_norm_rotary_workspace(tokens, hq, hk, d)
+        B.sparseloco_qk_norm_rotary(q, k, w, w, positions, f, *want)
+        B.sparseloco_qk_norm_rotary_grad(dq, dk, q, k, w, w, positions, f, *back, *sums[:2], ws)
+        # heads before tokens, as a batched product leaves them, and rows of a wider buffer with something behind them
+        q2, k2 = (t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k))
+        wide = torch.full((tokens + 3, hq + 1, d + 6), 7.0, dtype=dtype, device="cuda")
+        o2 = wide[1:-2, :hq, 3:-3]
+        B.sparseloco_qk_norm_rotary(q2, k2, w, w, positions, f, o2, k2)
+        assert torch.equal(o2, want[0]) and torch.equal(k2, want[1])
+        rest = wide.clone()
+        rest[1:-2, :hq, 3:-3] = 7.0
+        assert bool((rest == 7.0).all())
+        B.sparseloco_qk_norm_rotary_grad(dq, dk, q, k, w, w, positions, f, dq, dk, *sums[2:], ws)       # in place
+        assert torch.equal(dq, back[0]) and torch.equal(dk, back[1])
+        assert torch.equal(sums[0], sums[2]) and torch.equal(sums[1], sums[3])
+        B.sparseloco_qk_norm_rotary(q, k, w, w, positions, f, q, k)
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+        # one head for all: an input of stride 0
+        one = k[:, :1].expand(tokens, hq, d)
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        B.sparseloco_rotary(one, None, positions, f, a, None)
+        B.sparseloco_rotary(one.contiguous(), None, positions, f, b, None)
+        assert torch.equal(a, b)
+
+
+def test_zero_heads_and_what_is_not_finite():
+    tokens, h, d = 12, 3, 64
+    positions, (f, _) = positions_of("near", tokens, 1), B.rotary_frequencies(d)
+    q, k = lists(tokens, h, h, d, torch.float32, 9, False)
+    w = torch.ones(d, device="cuda")
+    q[4] = 0.0
+    clean = [torch.empty_like(q) for _ in range(4)]
+    sums, ws = [torch.empty(d, device="cuda") for _ in range(2)], B.qk_norm_rotary_workspace(tokens, h, h, d)
+    B.sparseloco_qk_norm_rotary(q, k, w, w, positions, f, *clean[:2])
+    B.sparseloco_qk_norm_rotary_grad(k, k, q, k, w, w, positions, f, *clean[2:], *sums, ws)
+    assert all(bool(torch.isfinite(t).all()) for t in clean + sums) and bool((clean[0][4] == 0).all())
+    bad = q.clone()
+    bad[7, 1, 5], bad[8, 2, 63] = float("nan"), float("inf")
+    dirty = [torch.empty_like(q) for _ in range(4)]
+    B.sparseloco_qk_norm_rotary(bad, k, w, w, positions, f, *dirty[:2])
+    B.sparseloco_qk_norm_rotary_grad(k, k, bad, k, w, w, positions, f, *dirty[2:], *sums, ws)
+    there = torch.ones(tokens, h, dtype=torch.bool, device="cuda")
+    there[7, 1] = there[8, 2] = False
+    for a, b in zip(clean, dirty):
+        assert torch.equal(a[there], b[there])
+    assert bool(torch.isnan(dirty[0][7, 1]).all()) and torch.equal(clean[1], dirty[1]) and torch.equal(clean[3], dirty[3])
+    assert bool(torch.isfinite(sums[1]).all())
+
+
+def test_no_tokens_and_no_keys():
+    f, _ = B.rotary_frequencies(8)
+    empty, none = torch.empty(0, 2, 8, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    w, sums = torch.ones(8, device="cuda"), [torch.full((8,), 3.0, device="cuda") for _ in range(2)]
+    B.sparseloco_rotary(empty, None, none, f, empty, None)
+    B.sparseloco_qk_norm_rotary(empty, empty, w, w, none, f, empty, empty)
+    ws = B.qk_norm_rotary_workspace(0, 2, 2, 8)
+    B.sparseloco_qk_norm_rotary_grad(empty, empty, empty, empty, w, w, none, f, empty, empty, *sums, ws, accumulate=True)
+    assert all(bool((s == 3).all()) for s in sums)
+    B.sparseloco_qk_norm_rotary_grad(empty, empty, empty, empty, w, w, none, f, empty, empty, *sums, ws)
+    assert all(bool((s == 0).all()) for s in sums)
+
+
+def test_offsets_beyond_32_bits():
+    d, f = 64, B.rotary_frequencies(64)[0]
+    far = torch.zeros(2 ** 31 + 4 * d, dtype=torch.bfloat16, device="cuda")
+    q = torch.as_strided(far, (2, 1, d), (2 ** 31 + 128, d, 1))
+    q.copy_(torch.randn(2, 1, d, device="cuda"))
+    positions, near = torch.tensor([3, 9], device="cuda"), q.clone()
+    want = torch.empty_like(near)
+    B.sparseloco_rotary(near, None, positions, f, want, None)
+    B.sparseloco_rotary(q, None, positions, f, q, None)
+    assert torch.equal(q, want) and int((far != 0).sum()) == int((want != 0).sum())
+
+
+def test_another_stream_and_replays_of_a_graph():
+    tokens, h, d = 700, 4, 64
+    positions, (f, _) = positions_of("near", tokens, 1), B.rotary_frequencies(d)
+    q, k = lists(tokens, h, h, d, torch.bfloat16, 10, False)
+    dq, dk = lists(tokens, h, h, d, torch.bfloat16, 11, False)
+    w = torch.linspace(0.5, 1.5, d, device="cuda")
+    ws = [B.qk_norm_rotary_workspace(tokens, h, h, d) for _ in range(2)]
+
+    def buffers():
+        return [torch.zeros_like(q) for _ in range(4)], [torch.zeros(d, device="cuda") for _ in range(2)]
+
+    def step(outs, sums, ws, stream=None):
+        B.sparseloco_qk_norm_rotary(q, k, w, w, positions, f, *outs[:2], stream=stream)
+        B.sparseloco_qk_norm_rotary_grad(dq, dk, outs[0], k, w, w, positions, f, *outs[2:], *sums, ws, stream=stream)
+    eager, first = buffers(), buffers()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    step(*first, ws[0], side)
+    torch.cuda.synchronize()
+    graph, replayed = torch.cuda.CUDAGraph(), buffers()
+    with torch.cuda.graph(graph):
+        step(*replayed, ws[1])
+    for seed in range(4):
+        if seed:
+            q.copy_(lists(tokens, h, h, d, torch.bfloat16, 20 + seed, False)[0])
+            for t in replayed[0] + replayed[1]:
+                t.zero_()
+        step(*eager, ws[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager[0] + eager[1], replayed[0] + replayed[1]):
+            assert torch.equal(a, b)
+        if seed == 0:
+            for a, b in zip(eager[0] + eager[1], first[0] + first[1]):
+                assert torch.equal(a, b)
+
+
+def test_frequencies():
+    f, m = B.rotary_frequencies(64, base=5000.0)
+    want = torch.tensor([5000.0 ** (-2 * i / 64) for i in range(32)], dtype=torch.float64)
+    assert m == 1.0 and torch.allclose(f.cpu(), want, rtol=1e-14, atol=0)
+    assert torch.allclose(B.rotary_frequencies(64, base=5000.0, scaling="linear", factor=4.0)[0].cpu(), want / 4, rtol=1e-14, atol=0)
+    wider, _ = B.rotary_frequencies(64, base=5000.0, scaling="base", factor=4.0)
+    assert math.isclose(float(wider[0]), 1.0) and math.isclose(float(wider[-1]), float(want[-1]) / 4, rel_tol=1e-12)
+    parts, m = B.rotary_frequencies(64, base=5000.0, scaling="by_parts", factor=4.0, trained_length=512)
+    turns = 512 * want / (2 * math.pi)
+    ratio = parts.cpu() / want
+    assert math.isclose(m, 0.1 * math.log(4.0) + 1)
+    assert torch.allclose(ratio[turns >= 32], torch.ones(1, dtype=torch.float64)) and torch.allclose(ratio[turns <= 1], torch.full((1,), 0.25, dtype=torch.float64))
+    assert bool(((ratio > 0.25) & (ratio < 1)).any())
