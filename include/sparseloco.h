@@ -293,7 +293,7 @@ int sparseloco_outer_step_batch(const sparseloco_plan* plan, int n_replicas,
  * Measured: 1.15-1.45 times the fp32 rate (the chip lowers its clock under the
  * bf16 matrix load, which caps the gain).  Another value: SPLC_EINVAL.
  */
-enum { SPLC_MATMUL_FP32 = 0, SPLC_MATMUL_BF16X3 = 1 };
+enum { SPLC_MATMUL_FP32 = 0, SPLC_MATMUL_BF16X3 = 1, SPLC_MATMUL_FP16 = 2, SPLC_MATMUL_FP16X3 = 3 /* the last two: sparseloco_orthogonalize */ };
 
 /*
  * Section 2.4 ("Token Embeddings and Heterogeneous Setting"): after every outer
@@ -430,6 +430,49 @@ int sparseloco_adamw_step_8bit(const sparseloco_plan* plan, const sparseloco_ten
                                int replica, uint8_t* m, float* m_scale, uint8_t* v, float* v_scale,
                                const sparseloco_adamw* how, const float* grad_scale, const float* decay,
                                const sparseloco_tensors* theta_bf16, void* stream);
+
+/*
+ * Orthogonalised updates: the inner step's optimiser for matrices.  Tensor i of the plan is taken as a row-major matrix of rows[i]
+ * rows (a host array, read during the call; rows[i] >= 1 divides the tensor's elements, rows and columns <= 2^22; the plan's layout
+ * plays no part), and every matrix is treated by itself.
+ *
+ * sparseloco_orthogonalize: X = M / (|M| + eps) with the Frobenius norm, then for each step, with n = min(rows, columns) rows (of X
+ * or its transpose),
+ *     A = X X^T,   X <- a X + (b A + c A^2) X,
+ * and out = X.  The singular values s of X become a s + b s^3 + c s^5 each time: with the usual (3.4445, -4.7750, 2.0315), five times,
+ * those above 0.002 come to lie between 0.68 and 1.14.  A matrix of zeros stays one.
+ *   x, out: fp32 or bf16 bindings; out may be x itself.  coefficients: 3 numbers a step (host), or NULL for the usual ones.
+ *   1 <= steps <= SPLC_MAX_ORTHO_STEPS; coefficients up to 1e4 whose polynomials keep the interval that starts as [0, 1] below 1024.
+ *   matmul: SPLC_MATMUL_FP16    operands of 11 bits, for results that are held in bf16: 2e-4 to 2e-3 off in the 2-norm
+ *           SPLC_MATMUL_FP16X3  operands of 22 bits in three products, as exact as fp32 ones
+ *   accumulation in fp32, norms in fp64.  ws: sparseloco_orthogonalize_ws_bytes(plan, rows, matmul) bytes, 128-byte aligned, need not
+ *   be cleared; two calls at once need one each.  The same call gives the same bits.  Inputs must be finite (a matrix with an element
+ *   that is not becomes NaN, the others are as they would be).
+ *
+ * sparseloco_muon_step: for every matrix, in place,
+ *     g     = grad_scale * grad
+ *     m     = momentum m + (1 - momentum) g
+ *     u     = nesterov ? momentum m + (1 - momentum) g : m
+ *     theta = theta (1 - lr weight_decay decay[tensor]) - lr f orthogonalized(u)
+ *     f     = 1 (SPLC_MUON_NONE), sqrt(max(1, rows / columns)) (SPLC_MUON_ASPECT), or 0.2 sqrt(max(rows, columns)) (SPLC_MUON_RMS: updates
+ *             as large as AdamW's are, so that the same lr serves both)
+ *   theta, m: fp32; grads: fp32 or bf16; replica, grad_scale, decay, theta_bf16 as for sparseloco_adamw_step; ws as above.  how: read
+ *   during the call.  lr, weight_decay, eps >= 0, 0 <= momentum < 1.  No buffer may overlap another.
+ */
+#define SPLC_MAX_ORTHO_STEPS 16
+enum { SPLC_MUON_NONE = 0, SPLC_MUON_ASPECT = 1, SPLC_MUON_RMS = 2 };
+typedef struct {
+    double lr, momentum, weight_decay, eps;
+    const double* coefficients;
+    int steps, nesterov, adjust, matmul;
+} sparseloco_muon;
+int64_t sparseloco_orthogonalize_ws_bytes(const sparseloco_plan* plan, const int64_t* rows, int matmul);
+int sparseloco_orthogonalize(const sparseloco_plan* plan, const int64_t* rows, const sparseloco_tensors* x, const sparseloco_tensors* out,
+                             int replica, const double* coefficients, int steps, double eps, int matmul, void* ws, int64_t ws_bytes,
+                             void* stream);
+int sparseloco_muon_step(const sparseloco_plan* plan, const int64_t* rows, const sparseloco_tensors* theta, const sparseloco_tensors* grads,
+                         const sparseloco_tensors* m, int replica, const sparseloco_muon* how, const float* grad_scale,
+                         const float* decay, const sparseloco_tensors* theta_bf16, void* ws, int64_t ws_bytes, void* stream);
 
 /*
  * Token embeddings of the split table of section 2.4 (and of a plain one):

@@ -30,7 +30,8 @@ SPLC_DELTA_FROM_PARAMS, SPLC_DELTA_DIRECT = 0, 1
 SPLC_QUANT_NONE, SPLC_QUANT_2BIT = 0, 1
 SPLC_SELECT_AUTO, SPLC_SELECT_RADIX = 0, 1
 SPLC_LAYOUT_FLAT, SPLC_LAYOUT_TILE64 = 0, 1
-SPLC_MATMUL_FP32, SPLC_MATMUL_BF16X3 = 0, 1
+SPLC_MATMUL_FP32, SPLC_MATMUL_BF16X3, SPLC_MATMUL_FP16, SPLC_MATMUL_FP16X3 = 0, 1, 2, 3
+SPLC_MUON_NONE, SPLC_MUON_ASPECT, SPLC_MUON_RMS = 0, 1, 2
 SPLC_NORM_WS_BYTES = 16384
 
 EXPORTS = [
@@ -49,6 +50,7 @@ EXPORTS = [
     "sparseloco_embedding_lookup", "sparseloco_embedding_grad_ws_bytes", "sparseloco_embedding_grad",
     "sparseloco_tensors_rebind", "sparseloco_messages_rebind",
     "sparseloco_rotary", "sparseloco_qk_norm_rotary", "sparseloco_qk_norm_rotary_grad_ws_bytes", "sparseloco_qk_norm_rotary_grad",
+    "sparseloco_orthogonalize_ws_bytes", "sparseloco_orthogonalize", "sparseloco_muon_step",
 ]
 
 SPLC_OP_PROJECT, SPLC_OP_RECONSTRUCT, SPLC_OP_REPROJECT_PASS1, SPLC_OP_REPROJECT_PASS2 = 0, 1, 2, 3
@@ -62,6 +64,13 @@ class _AdamW(ctypes.Structure):
     """sparseloco_adamw: the numbers of one step."""
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
                 ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64)]
+
+
+class _Muon(ctypes.Structure):
+    """sparseloco_muon: the numbers of one step."""
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("weight_decay", ctypes.c_double), ("eps", ctypes.c_double),
+                ("coefficients", ctypes.POINTER(ctypes.c_double)), ("steps", ctypes.c_int), ("nesterov", ctypes.c_int),
+                ("adjust", ctypes.c_int), ("matmul", ctypes.c_int)]
 
 
 class _Heads(ctypes.Structure):
@@ -132,6 +141,9 @@ def lib():
             "sparseloco_adamw_step": (i32, [vp, vp, vp, vp, vp, i32, ctypes.POINTER(_AdamW), vp, vp, vp, vp]),
             "sparseloco_adamw_step_8bit": (i32, [vp, vp, vp, i32, vp, vp, vp, vp, ctypes.POINTER(_AdamW), vp, vp, vp, vp]),
             "sparseloco_embedding_lookup": (i32, [vp, vp, i32, vp, i32, vp, i32, f32, vp, i32, i64, i32, vp]),
+            "sparseloco_orthogonalize_ws_bytes": (i64, [vp, p64, i32]),
+            "sparseloco_orthogonalize": (i32, [vp, p64, vp, vp, i32, ctypes.POINTER(f64), i32, f64, i32, vp, i64, vp]),
+            "sparseloco_muon_step": (i32, [vp, p64, vp, vp, vp, i32, ctypes.POINTER(_Muon), vp, vp, vp, vp, i64, vp]),
             "sparseloco_rotary": (i32, [hp, hp, i32, i64, i32, rp, i32, hp, hp, vp]),
             "sparseloco_qk_norm_rotary": (i32, [hp, hp, i32, i64, i32, vp, vp, i32, f64, rp, hp, hp, vp]),
             "sparseloco_qk_norm_rotary_grad_ws_bytes": (i64, [i64, i32, i32, i32]),
@@ -404,6 +416,7 @@ class Plan:
             self._h = ctypes.c_void_p()
             raise SparseLoCoError(rc, "sparseloco_plan_create")
         self.numels = numels
+        self.rows = (ctypes.c_int64 * max(n, 1))(*[r for r, _ in rc_list])      # of the tensors as matrices; 1-D ones have one
         self.tiled = bool(tiled)
         self.kappa = int(kappa)
         self.quant = bool(quant)
@@ -966,6 +979,71 @@ def sparseloco_embedding_grad(grad_out: torch.Tensor, token_ids: torch.Tensor, g
                                          ws.data_ptr(), int(ws.numel()), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, "sparseloco_embedding_grad")
+
+
+USUAL_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def _coefficients(c, where):
+    """(steps, array of 3 numbers each) of the polynomials."""
+    c = [tuple(float(x) for x in p) for p in c]
+    if not c or any(len(p) != 3 for p in c):
+        raise ValueError("%s: coefficients are (a, b, c) for every step" % where)
+    return len(c), (ctypes.c_double * (3 * len(c)))(*(x for p in c for x in p))
+
+
+def _check_ws(ws):
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.dim() != 1:
+        raise ValueError("ws: must be a contiguous uint8 tensor")
+    _check_here([ws])
+
+
+def orthogonalize_workspace(plan: Plan, *, matmul: int = SPLC_MATMUL_FP16X3, device="cuda") -> torch.Tensor:
+    """The workspace of sparseloco_orthogonalize and sparseloco_muon_step: up to 20 bytes an element of the 134 million or more that
+    are worked on at once."""
+    n = int(lib().sparseloco_orthogonalize_ws_bytes(plan.handle, plan.rows, _integer(matmul, 32, "sparseloco_orthogonalize_ws_bytes")))
+    if n < 0:
+        raise SparseLoCoError(n, "sparseloco_orthogonalize_ws_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def sparseloco_orthogonalize(plan: Plan, x, out, ws: torch.Tensor, *, coefficients=USUAL_COEFFICIENTS, eps: float = 1e-7,
+                             matmul: int = SPLC_MATMUL_FP16X3, replica: int = 0, stream=None) -> None:
+    """out = X after X = x / (|x| + eps) and, for every (a, b, c) of coefficients, X <- a X + (b A + c A^2) X, A = X X^T on the shorter
+    side: every matrix of the plan near to the orthogonal factor of its polar decomposition.  The plan's tensors are matrices as
+    given to Plan (leading dimensions folded into rows).  x, out: bindings or lists, fp32 or bf16; out may be x.  matmul:
+    SPLC_MATMUL_FP16X3 (as exact as fp32 products) or SPLC_MATMUL_FP16 (for results held in bf16).  ws: orthogonalize_workspace()."""
+    where = "sparseloco_orthogonalize"
+    steps, numbers = _coefficients(coefficients, where)
+    _check_ws(ws)
+    replica, matmul = _integer(replica, 32, where), _integer(matmul, 32, where)
+    with _Lists(plan, stream) as lists:
+        rc = lib().sparseloco_orthogonalize(plan.handle, plan.rows, _h(lists.tensors(x, _dtype_of(x))), _h(lists.tensors(out, _dtype_of(out))),
+                                            replica, numbers, steps, float(eps), matmul, ws.data_ptr(), int(ws.numel()), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, where)
+
+
+def sparseloco_muon_step(plan: Plan, theta, grads, m, ws: torch.Tensor, *, lr: float, momentum: float = 0.95, nesterov: bool = True,
+                         weight_decay: float = 0.1, eps: float = 1e-7, adjust: int = SPLC_MUON_RMS, coefficients=USUAL_COEFFICIENTS,
+                         matmul: int = SPLC_MATMUL_FP16X3, grad_scale: Optional[torch.Tensor] = None, decay: Optional[torch.Tensor] = None,
+                         theta_bf16=None, replica: int = 0, stream=None) -> None:
+    """One step over all matrices of the plan, theta and m (fp32) in place: m = momentum m + (1 - momentum) g, u = that average
+    once more (nesterov) or m, theta = theta (1 - lr weight_decay) - lr f orthogonalized(u).  adjust: f = 1 (SPLC_MUON_NONE),
+    sqrt(max(1, rows / columns)) (SPLC_MUON_ASPECT) or 0.2 sqrt(max(rows, columns)) (SPLC_MUON_RMS).  grads, grad_scale, decay,
+    theta_bf16 as in sparseloco_adamw_step; coefficients, eps, matmul, ws as in sparseloco_orthogonalize."""
+    where = "sparseloco_muon_step"
+    steps, numbers = _coefficients(coefficients, where)
+    _check_flat(_check_step(plan, grad_scale, decay))
+    _check_ws(ws)
+    replica, matmul, adjust = (_integer(v, 32, where) for v in (replica, matmul, adjust))
+    how = _Muon(lr, momentum, weight_decay, eps, numbers, steps, 1 if nesterov else 0, adjust, matmul)
+    with _Lists(plan, stream) as lists:
+        rc = lib().sparseloco_muon_step(plan.handle, plan.rows, _h(lists.tensors(theta)), _h(lists.tensors(grads, _dtype_of(grads))),
+                                        _h(lists.tensors(m)), replica, ctypes.byref(how), _opt(grad_scale), _opt(decay),
+                                        _h(lists.tensors(theta_bf16, torch.bfloat16)), ws.data_ptr(), int(ws.numel()), _stream(stream))
+    if rc != SPLC_OK:
+        raise SparseLoCoError(rc, where)
 
 
 def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,

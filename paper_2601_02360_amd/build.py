@@ -17,7 +17,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", name) for name in ("sparseloco.hip", "subspace.hip", "stream_probe.hip", "inner.hip",
-                                                          "embedding.hip", "heads.hip")]
+                                                          "embedding.hip", "heads.hip", "orthogonal.hip")]
 LIB = os.path.join(HERE, "libsparseloco.so")
 CALLS = os.path.join(HERE, "_calls.so")
 
