@@ -29,8 +29,8 @@ using namespace splc;
 
 constexpr int kThreads = 256;
 constexpr int kPad = 64;                                     // row lengths of the operands are multiples of it, zeros behind the end
-constexpr int kMostMatrices = 48;                            // of a batch: their descriptions are kernel arguments
-constexpr int64_t kBatchElements = (int64_t)1 << 27;         // a batch takes matrices until it has so many
+constexpr int kMostMatrices = 128;                           // of a batch: their descriptions are kernel arguments
+constexpr int64_t kBatchElements = (int64_t)1 << 29;         // of a batch, but one matrix at the least
 constexpr int kMostSide = 1 << 22;                           // rows and columns: offsets inside a tile's rows stay in 32 bits
 constexpr int kMostSteps = SPLC_MAX_ORTHO_STEPS;
 
@@ -39,48 +39,71 @@ typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 __host__ __device__ inline int padded(int n) { return (n + kPad - 1) / kPad * kPad; }
+// From a row to the next: an odd number of 128 bytes (256 where elements are hi + lo), so that the same piece of many rows lies in
+// many channels of the cache.
+__host__ __device__ inline int stride(int n) { return (n + kPad - 1) / kPad % 2 ? padded(n) : padded(n) + kPad; }
 
 struct Matrix {
     int64_t at;                                              // of its planes in the workspace, in elements
     int rows, cols, tensor, first;                           // first: of its workgroups in a launch
     __host__ __device__ int n() const { return rows < cols ? rows : cols; }
     __host__ __device__ bool tall() const { return rows > cols; }
-    __host__ __device__ int64_t r_plane() const { return (int64_t)rows * padded(cols); }
-    __host__ __device__ int64_t t_plane() const { return (int64_t)cols * padded(rows); }
-    __host__ __device__ int64_t a_plane() const { return (int64_t)n() * padded(n()); }
+    __host__ __device__ int64_t r_plane() const { return (int64_t)rows * stride(cols); }
+    __host__ __device__ int64_t t_plane() const { return (int64_t)cols * stride(rows); }
+    __host__ __device__ int64_t a_plane() const { return (int64_t)n() * stride(n()); }
 };
 struct Batch {
-    int count;
+    int count, groups;                                       // groups: that have work in a launch
     Matrix of[kMostMatrices];
 };
-// Planes of a matrix: R of this step and of the next (hi, lo), T likewise (hi, and lo if SPLIT), A and B.
+// Operands of a matrix: R and T of this step and of the next (one place for both where the third product does not read it: R of a
+// wide matrix, T of a tall one), A and B.  Their elements are hi + lo where they are split, 32 of hi and the same 32 of lo side by
+// side, so that a row of 32 for the products is 128 bytes; otherwise hi alone, and lo of R, which is no operand then, behind it.
 template <bool SPLIT>
 struct Planes {
     static constexpr int kParts = SPLIT ? 2 : 1;
-    _Float16 *r_first, *t_first, *a, *b;                     // lo follows hi
+    _Float16 *r_first, *t_first, *a, *b;
     int64_t r_next, t_next;
     __host__ __device__ static int64_t elements(const Matrix& m) {
-        return 4 * m.r_plane() + 2 * kParts * m.t_plane() + 2 * kParts * m.a_plane();
+        return 2 * m.r_plane() * (m.tall() ? 2 : 1) + kParts * m.t_plane() * (m.tall() ? 1 : 2) + 2 * kParts * m.a_plane();
     }
     __device__ __forceinline__ Planes(_Float16* ws, const Matrix& m) {
-        _Float16* p = ws + m.at;
-        r_first = p;
-        r_next = 2 * m.r_plane();
-        t_first = p += 2 * r_next;
-        t_next = kParts * m.t_plane();
-        a = p += 2 * t_next;
-        b = p + kParts * m.a_plane();
+        r_first = ws + m.at;
+        r_next = m.tall() ? 2 * m.r_plane() : 0;
+        t_first = r_first + 2 * m.r_plane() + r_next;
+        t_next = m.tall() ? 0 : kParts * m.t_plane();
+        a = t_first + kParts * m.t_plane() + t_next;
+        b = a + kParts * m.a_plane();
     }
+    // Of hi of element (row, col) from an operand's first, rows of `ld`; and of lo from there in R.
+    static __device__ __forceinline__ int64_t place(int row, int col, int ld) {
+        return (int64_t)row * ld * kParts + (SPLIT ? (col & ~31) * 2 + (col & 31) : col);
+    }
+    static __device__ __forceinline__ int64_t r_lo(const Matrix& m) { return SPLIT ? 32 : m.r_plane(); }
     __device__ __forceinline__ _Float16* r(int odd) const { return r_first + odd * r_next; }
     __device__ __forceinline__ _Float16* t(int odd) const { return t_first + odd * t_next; }
 };
 
 // The matrix of a workgroup, and the workgroup's place in it.
-__device__ __forceinline__ const Matrix& matrix_of(const Batch& batch, uint32_t group, int& place) {
-    int i = 0;
-    while (i + 1 < batch.count && (uint32_t)batch.of[i + 1].first <= group) ++i;
-    place = (int)group - batch.of[i].first;
-    return batch.of[i];
+__device__ __forceinline__ const Matrix& matrix_of(const Batch& batch, int group, int& place) {
+    int low = 0, high = batch.count;                         // the last one that begins at `group` or before is in [low, high)
+    while (high - low > 1) {
+        const int middle = (low + high) / 2;
+        if (batch.of[middle].first <= group) low = middle;
+        else high = middle;
+    }
+    place = group - batch.of[low].first;
+    return batch.of[low];
+}
+
+// Which of `groups` pieces of work a workgroup takes: neighbouring ones go to the same of the eight dies, which has 32 compute units
+// and a cache of its own, 32 after another; those that do not fill all dies that way are shared out evenly.  -1: none.
+__device__ __forceinline__ int group_of(int groups) {
+    constexpr int kDies = 8, kRun = 32;
+    const int die = blockIdx.x % kDies, i = blockIdx.x / kDies, full = groups / (kDies * kRun);
+    if (i < full * kRun) return (i / kRun * kDies + die) * kRun + i % kRun;
+    const int left = groups - full * kDies * kRun, each = (left + kDies - 1) / kDies, j = i - full * kRun;
+    return j < each && die * each + j < left ? full * kDies * kRun + die * each + j : -1;
 }
 
 __device__ __forceinline__ void split(float x, _Float16& hi, _Float16& lo) {
@@ -187,18 +210,18 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Batch batch, From from,
     float factor;
     if (!gradient_factor(grad_scale, factor)) return;
     int place;
-    const Matrix& m = matrix_of(batch, blockIdx.x, place);
+    const Matrix& m = matrix_of(batch, (int)blockIdx.x, place);
     const Planes<SPLIT> planes(ws, m);
     const int across = padded(m.cols) / 64, r0 = place / across * 64, c0 = place % across * 64;
-    const int ldc = padded(m.cols), ldr = padded(m.rows), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int ldc = stride(m.cols), ldr = stride(m.rows), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const double scale = inverse[m.tensor] * (double)range;
     for (int i = wave; i < 64; i += kThreads / 64) {
         const int r = r0 + i, c = c0 + lane;
         const float x = r < m.rows && c < m.cols ? (float)((double)from(m.tensor, (int64_t)r * m.cols + c, factor) * scale) : 0.f;
         tile[i][lane] = x;
         if (r < m.rows) {
-            _Float16* p = planes.r(0) + (int64_t)r * ldc + c;
-            split(x, p[0], p[m.r_plane()]);
+            _Float16* p = planes.r(0) + planes.place(r, c, ldc);
+            split(x, p[0], p[planes.r_lo(m)]);
         }
     }
     __syncthreads();
@@ -207,9 +230,9 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Batch batch, From from,
         if (c >= m.cols) break;
         _Float16 hi, lo;
         split(tile[lane][i], hi, lo);
-        _Float16* p = planes.t(0) + (int64_t)c * ldr + r;
+        _Float16* p = planes.t(0) + planes.place(c, r, ldr);
         p[0] = hi;
-        if (SPLIT) p[m.t_plane()] = lo;
+        if (SPLIT) p[32] = lo;
     }
 }
 
@@ -217,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Batch batch, From from,
 
 enum { GRAM = 0, POLYNOMIAL = 1, APPLY = 2, LAST = 3 };
 
-// The factors of one product: its result is old * own + sum * product, in the result's range.
+// The factors of one product: its result is sum * product + old * own, in the result's range.
 struct Factors {
     float own, product;
 };
@@ -233,227 +256,346 @@ struct Result {                                              // of the last step
 typedef __attribute__((address_space(1))) const void global_void;
 typedef __attribute__((address_space(3))) void shared_void;
 
-// A tile of T x T elements of C = P Q^T, kept in the registers of W x W waves; BK elements of every row of P and Q at a time go
-// to LDS, without passing registers, while the BK before them are multiplied.  A row of BK fp16 numbers is BK / 8 pieces of 16
-// bytes; the pieces of a row are exchanged by its number, so that 8 lanes that read a piece of 8 rows find them in 8 different
-// places of the 128 bytes that LDS gives a cycle.
-template <int T, int W, int BK, bool SPLIT, int STEP>
-__global__ __launch_bounds__(W* W * 64) void product_kernel(Batch batch, Factors f, Result result, int odd,
-                                                           const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
-    constexpr int kParts = SPLIT ? 2 : 1, kWaves = W * W, kSide = T / W / 32, kPieces = BK / 8, kRowsALoad = 64 / kPieces;
-    constexpr int kLoads = T * BK * 2 / 1024 / kWaves;       // of a wave for one plane of one operand
-    constexpr int kPlane = T * BK;
-    static_assert(kLoads * kWaves * 1024 == T * BK * 2, "whole loads");
-    __shared__ __align__(1024) _Float16 lds[2][2 * kParts][kPlane];
+// How a tile of C = P Q^T is shared out: WR x WC waves with IR x 1 blocks of 64 x 64 elements each in their registers, or (WK) WK
+// waves with the same block, which take turns along k.
+template <int WR_, int WC_, int WK_, int IR_, int BK_, bool SPLIT_>
+struct Shape {
+    static constexpr int WR = WR_, WC = WC_, WK = WK_, IR = IR_, BK = BK_, kWaves = WR_ * WC_ * WK_, kLanes = kWaves * 64;
+    static constexpr int kRows = WR_ * IR_ * 64, kCols = WC_ * 64, kTall = kRows / kCols;
+    static constexpr bool SPLIT = SPLIT_;
+    static_assert(kRows % kCols == 0, "a tile is as many columns wide, or a multiple of that in rows");
+    static_assert(WK_ == 1 || (WC_ == 1 && IR_ == 1 && WR_ == 1), "one block where waves share k");
+    // Workgroups of a launch for a matrix: all of its tiles, or those that reach its diagonal or what lies above it, `kTall` columns
+    // of tiles with u + 1 tiles each after another.
+    static int64_t tiles(const Matrix& m) { return (int64_t)((m.rows + kRows - 1) / kRows) * ((m.cols + kCols - 1) / kCols); }
+    static int64_t triangle(const Matrix& m) {
+        const int64_t across = (m.n() + kCols - 1) / kCols, u = across / kTall;
+        return kTall * (u * (u + 1) / 2) + across % kTall * (u + 1);
+    }
+    static __device__ __forceinline__ void triangle_place(int place, int& ti, int& tj) {
+        int u = (int)((sqrtf(8.f / kTall * (float)place + 1.f) - 1.f) * 0.5f);
+        while (kTall * (u * (u + 1) / 2) > place) --u;
+        while (kTall * ((u + 1) * (u + 2) / 2) <= place) ++u;
+        place -= kTall * (u * (u + 1) / 2);
+        ti = place % (u + 1);
+        tj = u * kTall + place / (u + 1);
+    }
+};
+constexpr int kBlock = 64 * 64;
+
+// Element (row, col) of a wave's block of 64 x 64 sums in LDS: groups of four columns are exchanged by the row, so that writing four
+// columns of many rows, reading eight columns of eight rows and reading eight rows of eight columns each find all banks.
+__device__ __forceinline__ int in_block(int row, int group) { return row * 64 + ((group ^ row ^ (row >> 3)) & 15) * 4; }
+
+// A row of fp16 numbers in LDS is ROW / 8 pieces of 16 bytes, and the pieces of a row are exchanged by its number: of 16 consecutive
+// rows, the same piece lies in 16 different places of the 256 bytes that the banks are wide, as reading it in 16 lanes at once needs.
+template <int ROW>
+__device__ __forceinline__ int exchange(int row) {
+    constexpr int kPieces = ROW / 8, kBeside = 16 / kPieces > 1 ? 16 / kPieces : 1;   // rows that lie side by side in the banks
+    return row / kBeside & (kPieces < 16 ? kPieces - 1 : 15);
+}
+
+// BK elements (hi, lo) of every row of P and Q at a time go to LDS, without passing registers, while the BK before them are multiplied.  Then the sums pass LDS, block by block, to be
+// finished and stored along rows of C, 16 bytes a lane, and once more along its columns for the transposed (or mirrored) copy.
+template <class S, int STEP>
+__global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Factors f, Result result, int odd,
+                                                            const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
+    constexpr bool SPLIT = S::SPLIT;
+    constexpr int kParts = SPLIT ? 2 : 1, BK = S::BK, kRow = BK * kParts, kPieces = kRow / 8, kRowsALoad = 64 / kPieces;
+    constexpr int kLoads[2] = {S::kRows * kRow / 512 / S::kWaves, S::kCols * kRow / 512 / S::kWaves};     // of a wave for P and Q
+    static_assert(kLoads[1] * S::kWaves * 512 == S::kCols * kRow, "whole loads");
+    __shared__ __align__(1024) union {
+        struct {
+            _Float16 p[S::kRows * kRow], q[S::kCols * kRow];
+        } operands[2];
+        float blocks[S::kWaves][kBlock];
+    } lds;
+    static_assert(sizeof(lds) <= 160 * 1024, "LDS");
 
     float factor;
     if (!gradient_factor(grad_scale, factor)) return;
     int place;
-    const Matrix m = matrix_of(batch, blockIdx.x, place);
+    const int group = group_of(batch.groups);
+    if (group < 0) return;
+    const Matrix m = matrix_of(batch, group, place);
     const Planes<SPLIT> planes(ws, m);
-    const int n = m.n(), ldn = padded(n), ldc = padded(m.cols), ldr = padded(m.rows);
+    const int n = m.n(), ldn = stride(n), ldc = stride(m.cols), ldr = stride(m.rows);
     int ti, tj;
-    if (STEP == GRAM || STEP == POLYNOMIAL) {                // column by column of the upper triangle
-        tj = (int)((sqrtf(8.f * (float)place + 1.f) - 1.f) * 0.5f);
-        while (tj * (tj + 1) / 2 > place) --tj;
-        while ((tj + 1) * (tj + 2) / 2 <= place) ++tj;
-        ti = place - tj * (tj + 1) / 2;
+    if (STEP == GRAM || STEP == POLYNOMIAL) {
+        S::triangle_place(place, ti, tj);
     } else {
-        const int down = (m.rows + T - 1) / T;
+        const int down = (m.rows + S::kRows - 1) / S::kRows;
         ti = place % down;
         tj = place / down;
     }
     const _Float16 *p, *q;
-    int64_t p_lo = 0, q_lo = 0;                              // from hi to lo
-    int p_rows, q_rows, depth;
+    int p_rows, q_rows, depth, ld_p, ld_q;
     if (STEP == GRAM) {
         p = q = m.tall() ? planes.t(odd) : planes.r(odd);
-        p_lo = q_lo = m.tall() ? m.t_plane() : m.r_plane();
         p_rows = q_rows = n;
-        depth = m.tall() ? ldr : ldc;
+        depth = padded(m.tall() ? m.rows : m.cols);
+        ld_p = ld_q = m.tall() ? ldr : ldc;
     } else if (STEP == POLYNOMIAL) {
         p = q = planes.a;
-        p_lo = q_lo = m.a_plane();
         p_rows = q_rows = n;
-        depth = ldn;
+        depth = padded(n);
+        ld_p = ld_q = ldn;
     } else {
         p = m.tall() ? planes.r(odd) : planes.b;
         q = m.tall() ? planes.b : planes.t(odd);
-        p_lo = m.tall() ? m.r_plane() : m.a_plane();
-        q_lo = m.tall() ? m.a_plane() : m.t_plane();
         p_rows = m.rows;
         q_rows = m.cols;
-        depth = ldn;
+        depth = padded(n);
+        ld_p = ld_q = ldn;
     }
+    depth *= kParts;                                         // fp16 numbers of a row
+    ld_p *= kParts;
+    ld_q *= kParts;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row0 = ti * T, col0 = tj * T;
-    const _Float16* from[2] = {p + (int64_t)row0 * depth, q + (int64_t)col0 * depth};
-    const int64_t to_lo[2] = {p_lo, q_lo};
-    uint32_t offset[2][kLoads];                              // of this lane's 16 bytes from the tile's first element, in elements
+    const int row0 = ti * S::kRows, col0 = tj * S::kCols;
+    const _Float16* from[2] = {p + (int64_t)row0 * ld_p, q + (int64_t)col0 * ld_q};
+    uint32_t offset[2][kLoads[0]];                           // of this lane's 16 bytes from the tile's first element, in elements
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int row = (wave + i * kWaves) * kRowsALoad + lane / kPieces;
-        const int piece = (lane % kPieces) ^ (BK == 64 ? row & 7 : (row >> 1) & 3);
-        const int in_p = row0 + row < p_rows ? row : p_rows - 1 - row0, in_q = col0 + row < q_rows ? row : q_rows - 1 - col0;
-        offset[0][i] = (uint32_t)in_p * (uint32_t)depth + (uint32_t)piece * 8u;
-        offset[1][i] = (uint32_t)in_q * (uint32_t)depth + (uint32_t)piece * 8u;
+    for (int side = 0; side < 2; ++side) {
+        const int last = (side ? q_rows - col0 : p_rows - row0) - 1;
+#pragma unroll
+        for (int i = 0; i < kLoads[side]; ++i) {
+            const int row = (wave + i * S::kWaves) * kRowsALoad + lane / kPieces, piece = (lane % kPieces) ^ exchange<kRow>(row);
+            offset[side][i] = (uint32_t)(row < last ? row : last) * (uint32_t)(side ? ld_q : ld_p) + (uint32_t)piece * 8u;
+        }
     }
     auto fetch = [&](int k, int buffer) {
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
+            _Float16* to = side ? lds.operands[buffer].q : lds.operands[buffer].p;
 #pragma unroll
-            for (int part = 0; part < kParts; ++part) {
-                const _Float16* base = from[side] + (part ? to_lo[side] : 0) + k;
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i)
-                    __builtin_amdgcn_global_load_lds((global_void*)(base + offset[side][i]),
-                                                     (shared_void*)&lds[buffer][side * kParts + part][(wave + i * kWaves) * 512], 16, 0, 0);
-            }
+            for (int i = 0; i < kLoads[side]; ++i)
+                __builtin_amdgcn_global_load_lds((global_void*)(from[side] + k + offset[side][i]),
+                                                 (shared_void*)(to + (wave + i * S::kWaves) * 512), 16, 0, 0);
         }
     };
-    v16f sum[kSide][kSide];
+    constexpr int kI = 2 * S::IR, kJ = 2, kSteps = BK / 16 / S::WK;
+    v16f sum[kI][kJ];
 #pragma unroll
-    for (int i = 0; i < kSide; ++i) {
+    for (int i = 0; i < kI; ++i) {
 #pragma unroll
-        for (int j = 0; j < kSide; ++j) {
+        for (int j = 0; j < kJ; ++j) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum[i][j][e] = 0.f;
         }
     }
-    const int wave_row = wave / W * (T / W), wave_col = wave % W * (T / W);
-    const int swap = BK == 64 ? lane & 7 : (lane >> 1) & 3;
+    const int wave_k = wave % S::WK, wave_at = wave / S::WK;
+    const int wave_row = wave_at / S::WC * (64 * S::IR), wave_col = wave_at % S::WC * 64;
+    struct Operands {
+        half8 x[kI][kParts], y[kJ][kParts];
+    };
+    const int swap = exchange<kRow>(lane & 31);
+    auto load = [&](Operands& o, int buffer, int kk) {
+        const int at = (wave_k * kSteps + kk) * 2 + (lane >> 5), hi = SPLIT ? (at & ~3) * 2 + (at & 3) : at;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            const int piece = ((hi + part * 4) ^ swap) * 8;
+#pragma unroll
+            for (int i = 0; i < kI; ++i)
+                o.x[i][part] = *(const half8*)&lds.operands[buffer].p[(wave_row + i * 32 + (lane & 31)) * kRow + piece];
+#pragma unroll
+            for (int j = 0; j < kJ; ++j)
+                o.y[j][part] = *(const half8*)&lds.operands[buffer].q[(wave_col + j * 32 + (lane & 31)) * kRow + piece];
+        }
+    };
+    Operands now, next;
     fetch(0, 0);
-    for (int k = 0, buffer = 0; k < depth; k += BK, buffer ^= 1) {
-        __syncthreads();                                     // what was fetched is there, and the other buffer has been read
-        if (k + BK < depth) fetch(k + BK, buffer ^ 1);
+    __syncthreads();
+    if (kRow < depth) fetch(kRow, 1);
+    load(now, 0, 0);
+    // The operands of the next 16 of k come from LDS while those at hand are multiplied, across the barrier too: it says that all waves
+    // have read a buffer to its end, and that the other one has arrived.
+    for (int k = 0, buffer = 0; k < depth; k += kRow, buffer ^= 1) {
 #pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk) {
-            const int piece = ((kk * 2 + (lane >> 5)) ^ swap) * 8;
-            half8 x[kSide][kParts], y[kSide][kParts];
-#pragma unroll
-            for (int part = 0; part < kParts; ++part) {
-#pragma unroll
-                for (int i = 0; i < kSide; ++i) {
-                    x[i][part] = *(const half8*)&lds[buffer][part][(wave_row + i * 32 + (lane & 31)) * BK + piece];
-                    y[i][part] = *(const half8*)&lds[buffer][kParts + part][(wave_col + i * 32 + (lane & 31)) * BK + piece];
-                }
+        for (int kk = 0; kk < kSteps; ++kk) {
+            if (kk + 1 < kSteps) {
+                load(next, buffer, kk + 1);
+            } else if (k + kRow < depth) {
+                __syncthreads();
+                if (k + 2 * kRow < depth) fetch(k + 2 * kRow, buffer);
+                load(next, buffer ^ 1, 0);
             }
 #pragma unroll
             for (int term = SPLIT ? 2 : 0; term >= 0; --term) {
 #pragma unroll
-                for (int i = 0; i < kSide; ++i) {
+                for (int i = 0; i < kI; ++i) {
 #pragma unroll
-                    for (int j = 0; j < kSide; ++j)          // columns of C in a lane's registers, rows over the lanes
-                        sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(y[j][term == 1], x[i][term == 2], sum[i][j], 0, 0, 0);
+                    for (int j = 0; j < kJ; ++j)             // columns of C in a lane's registers, rows over the lanes
+                        sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now.y[j][term == 1], now.x[i][term == 2], sum[i][j], 0, 0, 0);
                 }
             }
+            now = next;
         }
     }
-    // Register e of lane l: row l % 32, column 8 (e / 4) + 4 (l / 32) + e % 4.
-    const float keep = STEP == LAST && result.to < 0 ? 1.f - (result.decay ? result.shrink * result.decay[m.tensor] : result.shrink) : 0.f;
-    float size = 0.f;
+    float keep = 0.f, size = 0.f;
     if (STEP == LAST && result.to < 0) {
         const float rows = (float)m.rows, cols = (float)m.cols;
+        keep = 1.f - (result.decay ? result.shrink * result.decay[m.tensor] : result.shrink);
         size = result.size * (result.adjust == SPLC_MUON_ASPECT ? sqrtf(fmaxf(1.f, rows / cols))
                               : result.adjust == SPLC_MUON_RMS  ? 0.2f * sqrtf(fmaxf(rows, cols))
                                                                 : 1.f);
     }
+    constexpr bool kTriangle = STEP == GRAM || STEP == POLYNOMIAL;
+    const int rows = kTriangle ? n : m.rows, cols = kTriangle ? n : m.cols, ld = kTriangle ? ldn : ldc, ld_t = kTriangle ? ldn : ldr;
+    // a X is added here, to X as hi + lo, and not as part of B: its sums would be four times as large, and so would their roundings
+    // (1.4 times the error of fp32 products where it is 0.7 times so).
+    constexpr bool kOld = STEP != GRAM, kOldLo = STEP != POLYNOMIAL || SPLIT;
+    const int64_t r_lo = planes.r_lo(m);
+    const _Float16* old = STEP == POLYNOMIAL ? planes.a : planes.r(odd);
+    _Float16* to = STEP == GRAM ? planes.a : STEP == POLYNOMIAL ? planes.b : planes.r(odd ^ 1);
+    _Float16* to_t = kTriangle ? to : planes.t(odd ^ 1);
+    // Passes over a block: by one wave, or by all that share it.
+    constexpr int kPasses = 8 / S::WK;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSide; ++i) {
-        const int row = row0 + wave_row + i * 32 + (lane & 31);
+    for (int half = 0; half < S::IR; ++half) {
+        const int block_row = row0 + wave_row + half * 64, block_col = col0 + wave_col;
+        if (kTriangle && block_row > block_col) continue;    // below the diagonal: another block's mirror image
+        float* mine = lds.blocks[wave];
+        half8 old_hi[kOld ? kPasses : 1], old_lo[kOld && kOldLo ? kPasses : 1];
+        if (kOld) {
 #pragma unroll
-        for (int j = 0; j < kSide; ++j) {
+            for (int pass = 0; pass < kPasses; ++pass) {
+                const int row = block_row + (wave_k * kPasses + pass) * 8 + (lane >> 3), col = block_col + (lane & 7) * 8;
+                if (row >= rows || col >= ld) continue;
+                const _Float16* from_old = old + planes.place(row, col, ld);
+                old_hi[pass] = *(const half8*)from_old;
+                if (kOldLo) old_lo[pass] = *(const half8*)(from_old + (STEP == POLYNOMIAL ? 32 : r_lo));
+            }
+        }
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = col0 + wave_col + j * 32 + g * 8 + (lane >> 5) * 4;
-                float v[4];
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = f.product * sum[i][j][g * 4 + e];
-                if (STEP == GRAM || STEP == POLYNOMIAL) {
-                    _Float16* to = STEP == GRAM ? planes.a : planes.b;
-                    if (row < n && col < ldn) {
-                        const int64_t at = (int64_t)row * ldn + col;
-                        if (STEP == POLYNOMIAL) {
-                            const half4 hi = *(const half4*)(planes.a + at);
+            for (int j = 0; j < 2; ++j) {
+                // register e of lane l: row l % 32, column 8 (e / 4) + 4 (l / 32) + e % 4
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] = fmaf(f.own, (float)hi[e], v[e]);
-                            if (SPLIT) {
-                                const half4 lo = *(const half4*)(planes.a + m.a_plane() + at);
+                for (int g = 0; g < 4; ++g) {
+                    vfloat4 v;
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) v[e] = fmaf(f.own, (float)lo[e], v[e]);
-                            }
+                    for (int e = 0; e < 4; ++e) v[e] = f.product * sum[half * 2 + i][j][g * 4 + e];
+                    *(float4*)&mine[in_block(i * 32 + (lane & 31), j * 8 + g * 2 + (lane >> 5))] = make_float4(v.x, v.y, v.z, v.w);
+                }
+            }
+        }
+        if (S::WK > 1) {
+            __syncthreads();
+            mine = lds.blocks[0];
+        }
+#pragma unroll
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const int in_row = (wave_k * kPasses + pass) * 8 + (lane >> 3), row = block_row + in_row, col = block_col + (lane & 7) * 8;
+            float* at[2] = {mine + in_block(in_row, (lane & 7) * 2), mine + in_block(in_row, (lane & 7) * 2 + 1)};
+            float v[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float4 x = *(const float4*)at[h];
+#pragma unroll
+                for (int w = 1; w < S::WK; ++w) {
+                    const float4 y = *(const float4*)(at[h] + w * kBlock);
+                    x.x += y.x;
+                    x.y += y.y;
+                    x.z += y.z;
+                    x.w += y.w;
+                }
+                v[4 * h] = x.x;
+                v[4 * h + 1] = x.y;
+                v[4 * h + 2] = x.z;
+                v[4 * h + 3] = x.w;
+            }
+            const bool there = row < rows && col < ld;
+            if (kOld && there) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(f.own, (float)old_hi[pass][e] + (kOldLo ? (float)old_lo[pass][e] : 0.f), v[e]);
+            }
+            if (STEP != LAST) {
+                half8 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (!there || col + e >= cols) v[e] = 0.f;
+                    _Float16 h, l;
+                    split(v[e], h, l);
+                    hi[e] = h;
+                    lo[e] = l;
+                }
+                if (there) {
+                    _Float16* dst = to + planes.place(row, col, ld);
+                    *(half8*)dst = hi;
+                    if (SPLIT || STEP == APPLY) *(half8*)(dst + (STEP == APPLY ? r_lo : 32)) = lo;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) *(float4*)at[h] = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+            } else if (there) {
+                const int64_t place_of = (int64_t)row * m.cols + col;
+                const int count = m.cols - col < 8 ? m.cols - col : 8;
+                if (result.to < 0) {
+                    float* theta = static_cast<float*>(result.out[m.tensor]) + place_of;
+                    uint16_t* copy = result.copy ? result.copy[m.tensor] + place_of : nullptr;
+                    if (count == 8) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float4 x = cached_load4(theta + 4 * h);
+                            x.x = fmaf(-size, v[4 * h], x.x * keep);
+                            x.y = fmaf(-size, v[4 * h + 1], x.y * keep);
+                            x.z = fmaf(-size, v[4 * h + 2], x.z * keep);
+                            x.w = fmaf(-size, v[4 * h + 3], x.w * keep);
+                            stream_store4(theta + 4 * h, x);
+                            if (copy) stream_store4(copy + 4 * h, x);
                         }
-                        half4 hi, lo;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            _Float16 h, l;
-                            split(col + e < n ? v[e] : 0.f, h, l);
-                            hi[e] = h;
-                            lo[e] = l;
+                    } else {
+                        for (int e = 0; e < count; ++e) {
+                            const float now = fmaf(-size, v[e], theta[e] * keep);
+                            theta[e] = now;
+                            if (copy) copy[e] = (uint16_t)bf16_pair(now, 0.f);
                         }
-                        *(half4*)(to + at) = hi;
-                        if (SPLIT) *(half4*)(to + m.a_plane() + at) = lo;
-                        if (ti != tj) {                      // (row < n: this tile lies above the diagonal, all of its rows exist)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if (col + e >= n) break;
-                                _Float16* mirrored = to + (int64_t)(col + e) * ldn + row;
-                                mirrored[0] = hi[e];
-                                if (SPLIT) mirrored[m.a_plane()] = lo[e];
-                            }
-                        }
+                    }
+                } else if (result.to == SPLC_BF16) {
+                    uint16_t* out = static_cast<uint16_t*>(result.out[m.tensor]) + place_of;
+                    if (count == 8) {
+                        stream_store4(out, make_float4(v[0], v[1], v[2], v[3]));
+                        stream_store4(out + 4, make_float4(v[4], v[5], v[6], v[7]));
+                    } else {
+                        for (int e = 0; e < count; ++e) out[e] = (uint16_t)bf16_pair(v[e], 0.f);
                     }
                 } else {
-                    const bool there = row < m.rows && col < ldc;
-                    if (there) {
-                        const int64_t at = (int64_t)row * ldc + col;
-                        const half4 hi = *(const half4*)(planes.r(odd) + at), lo = *(const half4*)(planes.r(odd) + m.r_plane() + at);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = fmaf(f.own, (float)hi[e] + (float)lo[e], v[e]);
-                    }
-                    if (STEP == APPLY) {
-                        half4 hi, lo;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            _Float16 h, l;
-                            split(there && col + e < m.cols ? v[e] : 0.f, h, l);
-                            hi[e] = h;
-                            lo[e] = l;
-                        }
-                        if (there) {
-                            _Float16* to = planes.r(odd ^ 1) + (int64_t)row * ldc + col;
-                            *(half4*)to = hi;
-                            *(half4*)(to + m.r_plane()) = lo;
-                        }
-                        if (row < ldr) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if (col + e >= m.cols) break;
-                                _Float16* to = planes.t(odd ^ 1) + (int64_t)(col + e) * ldr + row;
-                                to[0] = hi[e];
-                                if (SPLIT) to[m.t_plane()] = lo[e];
-                            }
-                        }
-                    } else if (there) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (col + e >= m.cols) break;
-                            const int64_t at = (int64_t)row * m.cols + col + e;
-                            if (result.to < 0) {
-                                float* theta = static_cast<float*>(result.out[m.tensor]) + at;
-                                const float now = fmaf(-size, v[e], *theta * keep);
-                                *theta = now;
-                                if (result.copy) result.copy[m.tensor][at] = (uint16_t)bf16_pair(now, 0.f);
-                            } else if (result.to == SPLC_BF16) {
-                                static_cast<uint16_t*>(result.out[m.tensor])[at] = (uint16_t)bf16_pair(v[e], 0.f);
-                            } else {
-                                static_cast<float*>(result.out[m.tensor])[at] = v[e];
-                            }
-                        }
+                    float* out = static_cast<float*>(result.out[m.tensor]) + place_of;
+                    if (count == 8) {
+                        stream_store4(out, make_float4(v[0], v[1], v[2], v[3]));
+                        stream_store4(out + 4, make_float4(v[4], v[5], v[6], v[7]));
+                    } else {
+                        for (int e = 0; e < count; ++e) out[e] = v[e];
                     }
                 }
             }
         }
+        if (STEP == LAST || (kTriangle && block_row == block_col)) {
+            if (S::IR > 1) __builtin_amdgcn_wave_barrier();
+            continue;
+        }
+        if (S::WK > 1) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();                // (LDS takes a wave's accesses in their order)
+#pragma unroll 2
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const int in_col = (wave_k * kPasses + pass) * 8 + (lane & 7), in_row = lane >> 3 << 3, col = block_col + in_col, row = block_row + in_row;
+            half8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                _Float16 h, l;
+                split(mine[in_block(in_row + e, in_col >> 2) + (in_col & 3)], h, l);
+                hi[e] = h;
+                lo[e] = l;
+            }
+            if (col < cols && row < ld_t) {
+                _Float16* dst = to_t + planes.place(col, row, ld_t);
+                *(half8*)dst = hi;
+                if (SPLIT) *(half8*)(dst + 32) = lo;
+            }
+        }
+        if (S::IR > 1) __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -526,57 +668,89 @@ int shapes(const sparseloco_plan* plan, const int64_t* rows, int matmul, Shapes&
     if (!plan || !rows || (matmul != SPLC_MATMUL_FP16 && matmul != SPLC_MATMUL_FP16X3)) return SPLC_EINVAL;
     const bool three = matmul == SPLC_MATMUL_FP16X3;
     s.chunks = plan->n_update;
-    int64_t elements = 0, at = 0;
+    std::vector<Matrix> all;
+    int64_t total = 0;
     for (int i = 0; i < plan->n_tensors; ++i) {
         const int64_t n = plan->numel[(size_t)i];
         if (rows[i] < 0 || (n > 0 && (rows[i] < 1 || n % rows[i] != 0))) return SPLC_EINVAL;
         if (n == 0) continue;
         if (rows[i] > kMostSide || n / rows[i] > kMostSide) return SPLC_EINVAL;
-        const Matrix m{0, (int)rows[i], (int)(n / rows[i]), i, 0};
-        if (s.batches.empty() || s.batches.back().count == kMostMatrices || elements >= kBatchElements) {
-            s.batches.push_back(Batch{0, {}});
+        all.push_back(Matrix{0, (int)rows[i], (int)(n / rows[i]), i, 0});
+        total += n;
+    }
+    // Batches of like size; the longest products first, so that those that are left at the end of a launch are short ones.
+    const int64_t each = total / std::max<int64_t>(1, (total + kBatchElements - 1) / kBatchElements);
+    int64_t elements = 0, at = 0;
+    for (const Matrix& m : all) {
+        if (s.batches.empty() || s.batches.back().count == kMostMatrices || elements >= each) {
+            s.batches.push_back(Batch{0, 0, {}});
             elements = at = 0;
         }
         Batch& b = s.batches.back();
         b.of[b.count] = m;
         b.of[b.count++].at = at;
         at += three ? Planes<true>::elements(m) : Planes<false>::elements(m);
-        elements += n;
+        elements += (int64_t)m.rows * m.cols;
         s.planes = std::max(s.planes, at);
     }
+    for (Batch& b : s.batches)
+        std::stable_sort(b.of, b.of + b.count, [](const Matrix& x, const Matrix& y) { return std::max(x.rows, x.cols) > std::max(y.rows, y.cols); });
     return SPLC_OK;
 }
 
 // The number of workgroups of a launch, and where each matrix's begin.
 template <class Count>
-uint32_t place(Batch& b, Count count) {
+int place(Batch& b, Count count) {
     int64_t total = 0;
     for (int i = 0; i < b.count; ++i) {
         b.of[i].first = (int)total;
         total += count(b.of[i]);
     }
-    return (uint32_t)total;
+    b.groups = (int)total;
+    return b.groups;
 }
 
-template <int T, int W, int BK, bool SPLIT>
+// What a launch of `tiles` tiles takes, in times that a compute unit needs for one of 256 x 256: it holds one of those at a time, or
+// two smaller ones.  MI355X, whole calls with many tiles: 0.9B model, FP16X3, 92.5 ms with tiles of 256, 102 of 128, 142 of 64; 8 of
+// 2048 x 5632, FP16, 4.91, 4.97 and 10.3 ms.
+enum { LARGE, MIDDLE, SMALL };
+int tile_of(int64_t large, int64_t middle, int64_t small, bool split) {
+    auto rounds = [](int64_t tiles, int64_t at_once) { return (double)((tiles + at_once - 1) / at_once); };
+    const double cost[] = {rounds(large, 256), 0.575 * rounds(middle, 512), (split ? 0.2 : 0.27) * rounds(small, 512)};
+    return (int)(std::min_element(cost, cost + 3) - cost);
+}
+
+// One product of every matrix of the batch.
+template <bool SPLIT, int STEP>
+void product(Batch& b, Factors f, const Result& result, int odd, const float* grad_scale, _Float16* ws, hipStream_t st) {
+    using Large = Shape<2, 4, 1, 2, SPLIT ? 32 : 64, SPLIT>;
+    using Middle = Shape<2, 2, 1, 1, SPLIT ? 32 : 64, SPLIT>;
+    using Small = Shape<1, 1, 4, 1, 64, SPLIT>;
+    auto launch = [&](auto shape) {
+        using S = decltype(shape);
+        const int groups = place(b, STEP == GRAM || STEP == POLYNOMIAL ? S::triangle : S::tiles);
+        hipLaunchKernelGGL((product_kernel<S, STEP>), dim3((unsigned)(groups + 7) / 8 * 8), dim3(S::kLanes), 0, st, b, f, result, odd,
+                           grad_scale, ws);
+    };
+    auto count = [&](auto shape) {
+        using S = decltype(shape);
+        return place(b, STEP == GRAM || STEP == POLYNOMIAL ? S::triangle : S::tiles);
+    };
+    switch (tile_of(count(Large()), count(Middle()), count(Small()), SPLIT)) {
+        case LARGE: return launch(Large());
+        case MIDDLE: return launch(Middle());
+        default: return launch(Small());
+    }
+}
+
+template <bool SPLIT>
 void products(Batch& b, const Steps& s, const Result& result, const float* grad_scale, _Float16* ws, hipStream_t st) {
-    constexpr int kLanes = W * W * 64;
-    auto half = [](const Matrix& m) { const int64_t t = (m.n() + T - 1) / T; return t * (t + 1) / 2; };
-    auto all = [](const Matrix& m) { return (int64_t)((m.rows + T - 1) / T) * ((m.cols + T - 1) / T); };
     for (int k = 0; k < s.count; ++k) {
         const int odd = k & 1;
-        const uint32_t sides = place(b, half);
-        hipLaunchKernelGGL((product_kernel<T, W, BK, SPLIT, GRAM>), dim3(sides), dim3(kLanes), 0, st, b, s.gram[k], result, odd, grad_scale,
-                           ws);
-        hipLaunchKernelGGL((product_kernel<T, W, BK, SPLIT, POLYNOMIAL>), dim3(sides), dim3(kLanes), 0, st, b, s.polynomial[k], result, odd,
-                           grad_scale, ws);
-        const uint32_t tiles = place(b, all);
-        if (k + 1 < s.count)
-            hipLaunchKernelGGL((product_kernel<T, W, BK, SPLIT, APPLY>), dim3(tiles), dim3(kLanes), 0, st, b, s.apply[k], result, odd,
-                               grad_scale, ws);
-        else
-            hipLaunchKernelGGL((product_kernel<T, W, BK, SPLIT, LAST>), dim3(tiles), dim3(kLanes), 0, st, b, s.apply[k], result, odd,
-                               grad_scale, ws);
+        product<SPLIT, GRAM>(b, s.gram[k], result, odd, grad_scale, ws, st);
+        product<SPLIT, POLYNOMIAL>(b, s.polynomial[k], result, odd, grad_scale, ws, st);
+        if (k + 1 < s.count) product<SPLIT, APPLY>(b, s.apply[k], result, odd, grad_scale, ws, st);
+        else product<SPLIT, LAST>(b, s.apply[k], result, odd, grad_scale, ws, st);
     }
 }
 
@@ -584,13 +758,13 @@ template <class From>
 int orthogonalised(Shapes& shape, int matmul, const Steps& steps, const From& from, const float* grad_scale, const double* inverse,
                    const Result& result, _Float16* ws, hipStream_t st) {
     for (Batch& b : shape.batches) {
-        const uint32_t tiles = place(b, [](const Matrix& m) { return (int64_t)(padded(m.rows) / 64) * (padded(m.cols) / 64); });
+        const int tiles = place(b, [](const Matrix& m) { return (int64_t)(padded(m.rows) / 64) * (padded(m.cols) / 64); });
         if (matmul == SPLC_MATMUL_FP16X3) {
-            hipLaunchKernelGGL((scale_kernel<From, true>), dim3(tiles), dim3(kThreads), 0, st, b, from, grad_scale, inverse, steps.first, ws);
-            products<128, 2, 32, true>(b, steps, result, grad_scale, ws, st);
+            hipLaunchKernelGGL((scale_kernel<From, true>), dim3((unsigned)tiles), dim3(kThreads), 0, st, b, from, grad_scale, inverse, steps.first, ws);
+            products<true>(b, steps, result, grad_scale, ws, st);
         } else {
-            hipLaunchKernelGGL((scale_kernel<From, false>), dim3(tiles), dim3(kThreads), 0, st, b, from, grad_scale, inverse, steps.first, ws);
-            products<128, 2, 64, false>(b, steps, result, grad_scale, ws, st);
+            hipLaunchKernelGGL((scale_kernel<From, false>), dim3((unsigned)tiles), dim3(kThreads), 0, st, b, from, grad_scale, inverse, steps.first, ws);
+            products<false>(b, steps, result, grad_scale, ws, st);
         }
     }
     return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
