@@ -84,16 +84,25 @@ struct Planes {
     __device__ __forceinline__ _Float16* t(int odd) const { return t_first + odd * t_next; }
 };
 
+// The batch of a kernel whose first argument it is, where the arguments lie: it is indexed, and would be copied for that.
+typedef __attribute__((address_space(4))) const Batch ArgumentBatch;
+__device__ __forceinline__ ArgumentBatch* batch_argument() { return (ArgumentBatch*)__builtin_amdgcn_kernarg_segment_ptr(); }
+
 // The matrix of a workgroup, and the workgroup's place in it.
-__device__ __forceinline__ const Matrix& matrix_of(const Batch& batch, int group, int& place) {
-    int low = 0, high = batch.count;                         // the last one that begins at `group` or before is in [low, high)
-    while (high - low > 1) {
-        const int middle = (low + high) / 2;
-        if (batch.of[middle].first <= group) low = middle;
-        else high = middle;
+__device__ __forceinline__ Matrix matrix_of(ArgumentBatch* batch, int group, int& place) {
+    auto at = [&](int i) { return Matrix{batch->of[i].at, batch->of[i].rows, batch->of[i].cols, batch->of[i].tensor, batch->of[i].first}; };
+    Matrix m = at(0);                                        // (a load that waits for no other: the usual one of a small launch)
+    if (batch->count > 1) {
+        int low = 0, high = batch->count;                    // the last one that begins at `group` or before is in [low, high)
+        while (high - low > 1) {
+            const int middle = (low + high) / 2;
+            if (batch->of[middle].first <= group) low = middle;
+            else high = middle;
+        }
+        m = at(low);
     }
-    place = group - batch.of[low].first;
-    return batch.of[low];
+    place = group - m.first;
+    return m;
 }
 
 // Which of `groups` pieces of work a workgroup takes: neighbouring ones go to the same of the eight dies, which has 32 compute units
@@ -148,6 +157,23 @@ __device__ __forceinline__ double group_sum(double x, double* shared) {
     return x;
 }
 
+// Four consecutive elements from `at` on of a chunk that has n of them, +0 behind its end.
+template <class T>
+__device__ __forceinline__ float4 four(const T* p, uint32_t at, uint32_t n) {
+    if (at + 4 <= n) return widened(cached_load4(p + at));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (at < n) v.x = widened(p[at]);
+    if (at + 1 < n) v.y = widened(p[at + 1]);
+    if (at + 2 < n) v.z = widened(p[at + 2]);
+    return v;
+}
+__device__ __forceinline__ double squares(float4 v, double sum) {
+    sum = fma((double)v.x, (double)v.x, sum);
+    sum = fma((double)v.y, (double)v.y, sum);
+    sum = fma((double)v.z, (double)v.z, sum);
+    return fma((double)v.w, (double)v.w, sum);
+}
+
 // m = beta m + (1 - beta) g, and the sum of squares of a chunk of the update.
 template <class G>
 __global__ __launch_bounds__(kThreads) void momentum_kernel(const ChunkDesc* __restrict__ chunks, Update<G> update,
@@ -156,16 +182,38 @@ __global__ __launch_bounds__(kThreads) void momentum_kernel(const ChunkDesc* __r
     const ChunkDesc d = chunks[blockIdx.x];
     float factor;
     if (!gradient_factor(grad_scale, factor)) return;
-    float* m = update.m[d.tensor];
-    const G* grad = update.grad[d.tensor];
+    float* m = update.m[d.tensor] + d.offset;
+    const G* grad = update.grad[d.tensor] + d.offset;
+    const Momentum how = update.how;
+    float4 g[4], x[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const uint32_t at = s * 1024 + threadIdx.x * 4;
+        g[s] = four(grad, at, d.n_c);
+        x[s] = four(m, at, d.n_c);
+    }
     double sum = 0.0;
-    for (uint32_t i = threadIdx.x; i < d.n_c; i += kThreads) {
-        const int64_t at = (int64_t)d.offset + i;
-        const float g = factor * widened(grad[at]);
-        const float moment = fmaf(update.how.rest, g, update.how.beta * m[at]);
-        m[at] = moment;
-        const double u = update.how.nesterov ? fmaf(update.how.beta, moment, update.how.rest * g) : moment;
-        sum = fma(u, u, sum);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const uint32_t at = s * 1024 + threadIdx.x * 4;
+        auto one = [&](float& moment, float gradient) {
+            gradient *= factor;
+            moment = fmaf(how.rest, gradient, how.beta * moment);
+            return how.nesterov ? fmaf(how.beta, moment, how.rest * gradient) : moment;
+        };
+        float4 u;
+        u.x = one(x[s].x, g[s].x);
+        u.y = one(x[s].y, g[s].y);
+        u.z = one(x[s].z, g[s].z);
+        u.w = one(x[s].w, g[s].w);
+        if (at + 4 <= d.n_c) {
+            stream_store4(m + at, x[s]);
+        } else {
+            if (at < d.n_c) m[at] = x[s].x;
+            if (at + 1 < d.n_c) m[at + 1] = x[s].y;
+            if (at + 2 < d.n_c) m[at + 2] = x[s].z;
+        }
+        sum = squares(u, sum);
     }
     sum = group_sum(sum, shared);
     if (threadIdx.x == 0) partial[d.id] = sum;
@@ -177,8 +225,12 @@ __global__ __launch_bounds__(kThreads) void squares_kernel(const ChunkDesc* __re
     __shared__ double shared[kThreads / 64];
     const ChunkDesc d = chunks[blockIdx.x];
     const T* p = x[d.tensor] + d.offset;
+    float4 v[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) v[s] = four(p, s * 1024 + threadIdx.x * 4, d.n_c);
     double sum = 0.0;
-    for (uint32_t i = threadIdx.x; i < d.n_c; i += kThreads) sum = fma((double)widened(p[i]), (double)widened(p[i]), sum);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) sum = squares(v[s], sum);
     sum = group_sum(sum, shared);
     if (threadIdx.x == 0) partial[d.id] = sum;
 }
@@ -204,32 +256,41 @@ __global__ __launch_bounds__(kThreads) void inverse_norm_kernel(const int64_t* _
 
 // X of the first step in both layouts, 64 x 64 elements a workgroup.
 template <class From, bool SPLIT>
-__global__ __launch_bounds__(kThreads) void scale_kernel(Batch batch, From from, const float* __restrict__ grad_scale,
+__global__ __launch_bounds__(kThreads) void scale_kernel(Batch, From from, const float* __restrict__ grad_scale,
                                                          const double* __restrict__ inverse, float range, _Float16* __restrict__ ws) {
     __shared__ float tile[64][65];
     float factor;
     if (!gradient_factor(grad_scale, factor)) return;
     int place;
-    const Matrix& m = matrix_of(batch, (int)blockIdx.x, place);
+    const Matrix m = matrix_of(batch_argument(), (int)blockIdx.x, place);
     const Planes<SPLIT> planes(ws, m);
     const int across = padded(m.cols) / 64, r0 = place / across * 64, c0 = place % across * 64;
     const int ldc = stride(m.cols), ldr = stride(m.rows), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const double scale = inverse[m.tensor] * (double)range;
-    for (int i = wave; i < 64; i += kThreads / 64) {
-        const int r = r0 + i, c = c0 + lane;
-        const float x = r < m.rows && c < m.cols ? (float)((double)from(m.tensor, (int64_t)r * m.cols + c, factor) * scale) : 0.f;
-        tile[i][lane] = x;
+    constexpr int kEach = 64 / (kThreads / 64);
+    float x[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int r = r0 + wave * kEach + i, c = c0 + lane;
+        x[i] = r < m.rows && c < m.cols ? from(m.tensor, (int64_t)r * m.cols + c, factor) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int r = r0 + wave * kEach + i, c = c0 + lane;
+        const float scaled = (float)((double)x[i] * scale);
+        tile[wave * kEach + i][lane] = scaled;
         if (r < m.rows) {
             _Float16* p = planes.r(0) + planes.place(r, c, ldc);
-            split(x, p[0], p[planes.r_lo(m)]);
+            split(scaled, p[0], p[planes.r_lo(m)]);
         }
     }
     __syncthreads();
-    for (int i = wave; i < 64; i += kThreads / 64) {
-        const int c = c0 + i, r = r0 + lane;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int c = c0 + wave * kEach + i, r = r0 + lane;
         if (c >= m.cols) break;
         _Float16 hi, lo;
-        split(tile[lane][i], hi, lo);
+        split(tile[lane][wave * kEach + i], hi, lo);
         _Float16* p = planes.t(0) + planes.place(c, r, ldr);
         p[0] = hi;
         if (SPLIT) p[32] = lo;
@@ -256,20 +317,23 @@ struct Result {                                              // of the last step
 typedef __attribute__((address_space(1))) const void global_void;
 typedef __attribute__((address_space(3))) void shared_void;
 
-// How a tile of C = P Q^T is shared out: WR x WC waves with IR x 1 blocks of 64 x 64 elements each in their registers, or (WK) WK
-// waves with the same block, which take turns along k.
-template <int WR_, int WC_, int WK_, int IR_, int BK_, bool SPLIT_>
+// How a tile of C = P Q^T is shared out: WR x WC waves with IR x 1 blocks of SIDE x SIDE elements each in their registers, or (WK) WK
+// waves with the same block, which take turns along k.  DEEP: buffers for BK of k.
+template <int WR_, int WC_, int WK_, int IR_, int SIDE_, int BK_, int DEEP_, bool SPLIT_>
 struct Shape {
-    static constexpr int WR = WR_, WC = WC_, WK = WK_, IR = IR_, BK = BK_, kWaves = WR_ * WC_ * WK_, kLanes = kWaves * 64;
-    static constexpr int kRows = WR_ * IR_ * 64, kCols = WC_ * 64, kTall = kRows / kCols;
+    static constexpr int WR = WR_, WC = WC_, WK = WK_, IR = IR_, kSide = SIDE_, BK = BK_, kDeep = DEEP_, kWaves = WR_ * WC_ * WK_, kLanes = kWaves * 64;
+    static constexpr int kRows = WR_ * IR_ * SIDE_, kCols = WC_ * SIDE_, kTall = kRows / kCols;
     static constexpr bool SPLIT = SPLIT_;
+    static_assert(kPad % BK_ == 0, "whole rows of operands");
     static_assert(kRows % kCols == 0, "a tile is as many columns wide, or a multiple of that in rows");
     static_assert(WK_ == 1 || (WC_ == 1 && IR_ == 1 && WR_ == 1), "one block where waves share k");
     // Workgroups of a launch for a matrix: all of its tiles, or those that reach its diagonal or what lies above it, `kTall` columns
     // of tiles with u + 1 tiles each after another.
-    static int64_t tiles(const Matrix& m) { return (int64_t)((m.rows + kRows - 1) / kRows) * ((m.cols + kCols - 1) / kCols); }
+    // Tiles cover the padding of rows of operands, which they clear, too.
+    static __host__ __device__ int down(const Matrix& m) { return (padded(m.rows) + kRows - 1) / kRows; }
+    static int64_t tiles(const Matrix& m) { return (int64_t)down(m) * ((padded(m.cols) + kCols - 1) / kCols); }
     static int64_t triangle(const Matrix& m) {
-        const int64_t across = (m.n() + kCols - 1) / kCols, u = across / kTall;
+        const int64_t across = (padded(m.n()) + kCols - 1) / kCols, u = across / kTall;
         return kTall * (u * (u + 1) / 2) + across % kTall * (u + 1);
     }
     static __device__ __forceinline__ void triangle_place(int place, int& ti, int& tj) {
@@ -281,11 +345,11 @@ struct Shape {
         tj = u * kTall + place / (u + 1);
     }
 };
-constexpr int kBlock = 64 * 64;
 
-// Element (row, col) of a wave's block of 64 x 64 sums in LDS: groups of four columns are exchanged by the row, so that writing four
-// columns of many rows, reading eight columns of eight rows and reading eight rows of eight columns each find all banks.
-__device__ __forceinline__ int in_block(int row, int group) { return row * 64 + ((group ^ row ^ (row >> 3)) & 15) * 4; }
+// Element (row, col) of a wave's block of sums in LDS: groups of four columns are exchanged by the row, so that writing four columns
+// of many rows, reading eight columns of eight rows and reading eight rows of eight columns each find all banks (where SIDE is 64).
+template <int SIDE>
+__device__ __forceinline__ int in_block(int row, int group) { return row * SIDE + ((group ^ row ^ (row >> 3)) & (SIDE / 4 - 1)) * 4; }
 
 // A row of fp16 numbers in LDS is ROW / 8 pieces of 16 bytes, and the pieces of a row are exchanged by its number: of 16 consecutive
 // rows, the same piece lies in 16 different places of the 256 bytes that the banks are wide, as reading it in 16 lanes at once needs.
@@ -298,35 +362,33 @@ __device__ __forceinline__ int exchange(int row) {
 // BK elements (hi, lo) of every row of P and Q at a time go to LDS, without passing registers, while the BK before them are multiplied.  Then the sums pass LDS, block by block, to be
 // finished and stored along rows of C, 16 bytes a lane, and once more along its columns for the transposed (or mirrored) copy.
 template <class S, int STEP>
-__global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Factors f, Result result, int odd,
+__global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Factors f, Result result, int odd,
                                                             const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
     constexpr bool SPLIT = S::SPLIT;
+    constexpr int SIDE = S::kSide;
     constexpr int kParts = SPLIT ? 2 : 1, BK = S::BK, kRow = BK * kParts, kPieces = kRow / 8, kRowsALoad = 64 / kPieces;
     constexpr int kLoads[2] = {S::kRows * kRow / 512 / S::kWaves, S::kCols * kRow / 512 / S::kWaves};     // of a wave for P and Q
     static_assert(kLoads[1] * S::kWaves * 512 == S::kCols * kRow, "whole loads");
     __shared__ __align__(1024) union {
         struct {
             _Float16 p[S::kRows * kRow], q[S::kCols * kRow];
-        } operands[2];
-        float blocks[S::kWaves][kBlock];
+        } operands[S::kDeep];
+        float blocks[S::kWaves][SIDE * SIDE];
     } lds;
     static_assert(sizeof(lds) <= 160 * 1024, "LDS");
 
-    float factor;
-    if (!gradient_factor(grad_scale, factor)) return;
     int place;
-    const int group = group_of(batch.groups);
+    const int group = group_of(batch_argument()->groups);
     if (group < 0) return;
-    const Matrix m = matrix_of(batch, group, place);
+    const Matrix m = matrix_of(batch_argument(), group, place);
     const Planes<SPLIT> planes(ws, m);
     const int n = m.n(), ldn = stride(n), ldc = stride(m.cols), ldr = stride(m.rows);
     int ti, tj;
     if (STEP == GRAM || STEP == POLYNOMIAL) {
         S::triangle_place(place, ti, tj);
     } else {
-        const int down = (m.rows + S::kRows - 1) / S::kRows;
-        ti = place % down;
-        tj = place / down;
+        ti = place % S::down(m);
+        tj = place / S::down(m);
     }
     const _Float16 *p, *q;
     int p_rows, q_rows, depth, ld_p, ld_q;
@@ -353,11 +415,13 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
     ld_q *= kParts;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = ti * S::kRows, col0 = tj * S::kCols;
-    const _Float16* from[2] = {p + (int64_t)row0 * ld_p, q + (int64_t)col0 * ld_q};
+    // (rows that are not there, up to all of a tile's, are read as the last one that is)
+    const int first[2] = {row0 < p_rows ? row0 : p_rows - 1, col0 < q_rows ? col0 : q_rows - 1};
+    const _Float16* from[2] = {p + (int64_t)first[0] * ld_p, q + (int64_t)first[1] * ld_q};
     uint32_t offset[2][kLoads[0]];                           // of this lane's 16 bytes from the tile's first element, in elements
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        const int last = (side ? q_rows - col0 : p_rows - row0) - 1;
+        const int last = (side ? q_rows : p_rows) - 1 - first[side];
 #pragma unroll
         for (int i = 0; i < kLoads[side]; ++i) {
             const int row = (wave + i * S::kWaves) * kRowsALoad + lane / kPieces, piece = (lane % kPieces) ^ exchange<kRow>(row);
@@ -374,7 +438,7 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
                                                  (shared_void*)(to + (wave + i * S::kWaves) * 512), 16, 0, 0);
         }
     };
-    constexpr int kI = 2 * S::IR, kJ = 2, kSteps = BK / 16 / S::WK;
+    constexpr int kI = SIDE / 32 * S::IR, kJ = SIDE / 32, kSteps = BK / 16 / S::WK;
     v16f sum[kI][kJ];
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
@@ -385,10 +449,35 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
         }
     }
     const int wave_k = wave % S::WK, wave_at = wave / S::WK;
-    const int wave_row = wave_at / S::WC * (64 * S::IR), wave_col = wave_at % S::WC * 64;
+    const int wave_row = wave_at / S::WC * (SIDE * S::IR), wave_col = wave_at % S::WC * SIDE;
     struct Operands {
         half8 x[kI][kParts], y[kJ][kParts];
     };
+    constexpr bool kTriangle = STEP == GRAM || STEP == POLYNOMIAL;
+    const int rows = kTriangle ? n : m.rows, cols = kTriangle ? n : m.cols, ld = kTriangle ? ldn : ldc, ld_t = kTriangle ? ldn : ldr;
+    // a X is added here, to X as hi + lo, and not as part of B: its sums would be four times as large, and so would their roundings
+    // (1.4 times the error of fp32 products where it is 0.7 times so).
+    constexpr bool kOld = STEP != GRAM, kOldLo = STEP != POLYNOMIAL || SPLIT;
+    const int64_t r_lo = planes.r_lo(m);
+    const _Float16* old = STEP == POLYNOMIAL ? planes.a : planes.r(odd);
+    _Float16* to = STEP == GRAM ? planes.a : STEP == POLYNOMIAL ? planes.b : planes.r(odd ^ 1);
+    _Float16* to_t = kTriangle ? to : planes.t(odd ^ 1);
+    // Passes over a block, by one wave or by all that share it: 8 columns a lane along its rows, then 8 rows a lane along its columns.
+    constexpr int kAcross = SIDE / 8, kDown = 64 / kAcross, kPasses = SIDE / kDown / S::WK > 0 ? SIDE / kDown / S::WK : 1;
+    const bool passes = wave_k * kPasses * kDown < SIDE;
+    half8 old_hi[kOld ? kPasses : 1], old_lo[kOld && kOldLo ? kPasses : 1];
+    auto load_old = [&](int block_row, int block_col) {
+        if (!kOld || !passes) return;
+#pragma unroll
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const int row = block_row + (wave_k * kPasses + pass) * kDown + lane / kAcross, col = block_col + lane % kAcross * 8;
+            if (row >= rows || col >= ld) continue;
+            const _Float16* from_old = old + planes.place(row, col, ld);
+            old_hi[pass] = *(const half8*)from_old;
+            if (kOldLo) old_lo[pass] = *(const half8*)(from_old + (STEP == POLYNOMIAL ? 32 : r_lo));
+        }
+    };
+    if (S::WK > 1) load_old(row0, col0);                     // (few registers: their latency passes beside the products')
     const int swap = exchange<kRow>(lane & 31);
     auto load = [&](Operands& o, int buffer, int kk) {
         const int at = (wave_k * kSteps + kk) * 2 + (lane >> 5), hi = SPLIT ? (at & ~3) * 2 + (at & 3) : at;
@@ -403,22 +492,35 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
                 o.y[j][part] = *(const half8*)&lds.operands[buffer].q[(wave_col + j * 32 + (lane & 31)) * kRow + piece];
         }
     };
+    // Waits for what was fetched first of so many fetches, and for the operands from LDS; then for all waves.
+    constexpr int kAhead = S::kDeep - 1, kWaiting = (kAhead - 1) * (kLoads[0] + kLoads[1]);
+    static_assert(kWaiting < 64, "loads that a wave counts");
+    auto arrived = [&](bool all_ahead) {
+        asm volatile("" ::: "memory");
+        if (all_ahead) __builtin_amdgcn_s_waitcnt((kWaiting & 15) | kWaiting >> 4 << 14 | 7 << 4);
+        else __builtin_amdgcn_s_waitcnt(7 << 4);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
     Operands now, next;
-    fetch(0, 0);
-    __syncthreads();
-    if (kRow < depth) fetch(kRow, 1);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (i * kRow < depth) fetch(i * kRow, i);
+    arrived(kAhead * kRow <= depth);
+    if (kAhead * kRow < depth) fetch(kAhead * kRow, kAhead);
     load(now, 0, 0);
     // The operands of the next 16 of k come from LDS while those at hand are multiplied, across the barrier too: it says that all waves
-    // have read a buffer to its end, and that the other one has arrived.
-    for (int k = 0, buffer = 0; k < depth; k += kRow, buffer ^= 1) {
+    // have read a buffer to its end, and that the next one has arrived.
+    for (int k = 0, buffer = 0; k < depth; k += kRow) {
+        const int after = buffer + 1 < S::kDeep ? buffer + 1 : 0;
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) {
             if (kk + 1 < kSteps) {
                 load(next, buffer, kk + 1);
             } else if (k + kRow < depth) {
-                __syncthreads();
-                if (k + 2 * kRow < depth) fetch(k + 2 * kRow, buffer);
-                load(next, buffer ^ 1, 0);
+                arrived(k + (kAhead + 1) * kRow <= depth);
+                if (k + S::kDeep * kRow < depth) fetch(k + S::kDeep * kRow, buffer);
+                load(next, after, 0);
             }
 #pragma unroll
             for (int term = SPLIT ? 2 : 0; term >= 0; --term) {
@@ -431,6 +533,11 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
             }
             now = next;
         }
+        buffer = after;
+    }
+    if (STEP == LAST && result.to < 0) {
+        float factor;
+        if (!gradient_factor(grad_scale, factor)) return;
     }
     float keep = 0.f, size = 0.f;
     if (STEP == LAST && result.to < 0) {
@@ -440,45 +547,24 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
                               : result.adjust == SPLC_MUON_RMS  ? 0.2f * sqrtf(fmaxf(rows, cols))
                                                                 : 1.f);
     }
-    constexpr bool kTriangle = STEP == GRAM || STEP == POLYNOMIAL;
-    const int rows = kTriangle ? n : m.rows, cols = kTriangle ? n : m.cols, ld = kTriangle ? ldn : ldc, ld_t = kTriangle ? ldn : ldr;
-    // a X is added here, to X as hi + lo, and not as part of B: its sums would be four times as large, and so would their roundings
-    // (1.4 times the error of fp32 products where it is 0.7 times so).
-    constexpr bool kOld = STEP != GRAM, kOldLo = STEP != POLYNOMIAL || SPLIT;
-    const int64_t r_lo = planes.r_lo(m);
-    const _Float16* old = STEP == POLYNOMIAL ? planes.a : planes.r(odd);
-    _Float16* to = STEP == GRAM ? planes.a : STEP == POLYNOMIAL ? planes.b : planes.r(odd ^ 1);
-    _Float16* to_t = kTriangle ? to : planes.t(odd ^ 1);
-    // Passes over a block: by one wave, or by all that share it.
-    constexpr int kPasses = 8 / S::WK;
     __syncthreads();
 #pragma unroll
     for (int half = 0; half < S::IR; ++half) {
-        const int block_row = row0 + wave_row + half * 64, block_col = col0 + wave_col;
+        const int block_row = row0 + wave_row + half * SIDE, block_col = col0 + wave_col;
         if (kTriangle && block_row > block_col) continue;    // below the diagonal: another block's mirror image
         float* mine = lds.blocks[wave];
-        half8 old_hi[kOld ? kPasses : 1], old_lo[kOld && kOldLo ? kPasses : 1];
-        if (kOld) {
+        if (S::WK == 1) load_old(block_row, block_col);
 #pragma unroll
-            for (int pass = 0; pass < kPasses; ++pass) {
-                const int row = block_row + (wave_k * kPasses + pass) * 8 + (lane >> 3), col = block_col + (lane & 7) * 8;
-                if (row >= rows || col >= ld) continue;
-                const _Float16* from_old = old + planes.place(row, col, ld);
-                old_hi[pass] = *(const half8*)from_old;
-                if (kOldLo) old_lo[pass] = *(const half8*)(from_old + (STEP == POLYNOMIAL ? 32 : r_lo));
-            }
-        }
+        for (int i = 0; i < SIDE / 32; ++i) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < SIDE / 32; ++j) {
                 // register e of lane l: row l % 32, column 8 (e / 4) + 4 (l / 32) + e % 4
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     vfloat4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = f.product * sum[half * 2 + i][j][g * 4 + e];
-                    *(float4*)&mine[in_block(i * 32 + (lane & 31), j * 8 + g * 2 + (lane >> 5))] = make_float4(v.x, v.y, v.z, v.w);
+                    for (int e = 0; e < 4; ++e) v[e] = f.product * sum[half * (SIDE / 32) + i][j][g * 4 + e];
+                    *(float4*)&mine[in_block<SIDE>(i * 32 + (lane & 31), j * 8 + g * 2 + (lane >> 5))] = make_float4(v.x, v.y, v.z, v.w);
                 }
             }
         }
@@ -488,15 +574,17 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
         }
 #pragma unroll
         for (int pass = 0; pass < kPasses; ++pass) {
-            const int in_row = (wave_k * kPasses + pass) * 8 + (lane >> 3), row = block_row + in_row, col = block_col + (lane & 7) * 8;
-            float* at[2] = {mine + in_block(in_row, (lane & 7) * 2), mine + in_block(in_row, (lane & 7) * 2 + 1)};
+            if (!passes) break;
+            const int in_row = (wave_k * kPasses + pass) * kDown + lane / kAcross, row = block_row + in_row;
+            const int in_col = lane % kAcross * 8, col = block_col + in_col;
+            float* at[2] = {mine + in_block<SIDE>(in_row, in_col / 4), mine + in_block<SIDE>(in_row, in_col / 4 + 1)};
             float v[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float4 x = *(const float4*)at[h];
 #pragma unroll
                 for (int w = 1; w < S::WK; ++w) {
-                    const float4 y = *(const float4*)(at[h] + w * kBlock);
+                    const float4 y = *(const float4*)(at[h] + w * SIDE * SIDE);
                     x.x += y.x;
                     x.y += y.y;
                     x.z += y.z;
@@ -580,12 +668,14 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch batch, Fact
         else __builtin_amdgcn_wave_barrier();                // (LDS takes a wave's accesses in their order)
 #pragma unroll 2
         for (int pass = 0; pass < kPasses; ++pass) {
-            const int in_col = (wave_k * kPasses + pass) * 8 + (lane & 7), in_row = lane >> 3 << 3, col = block_col + in_col, row = block_row + in_row;
+            if (!passes) break;
+            const int in_col = (wave_k * kPasses + pass) * kDown + lane % kDown, in_row = lane / kDown * 8;
+            const int col = block_col + in_col, row = block_row + in_row;
             half8 hi, lo;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 _Float16 h, l;
-                split(mine[in_block(in_row + e, in_col >> 2) + (in_col & 3)], h, l);
+                split(mine[in_block<SIDE>(in_row + e, in_col >> 2) + (in_col & 3)], h, l);
                 hi[e] = h;
                 lo[e] = l;
             }
@@ -712,7 +802,9 @@ int place(Batch& b, Count count) {
 
 // What a launch of `tiles` tiles takes, in times that a compute unit needs for one of 256 x 256: it holds one of those at a time, or
 // two smaller ones.  MI355X, whole calls with many tiles: 0.9B model, FP16X3, 92.5 ms with tiles of 256, 102 of 128, 142 of 64; 8 of
-// 2048 x 5632, FP16, 4.91, 4.97 and 10.3 ms.
+// 2048 x 5632, FP16, 4.91, 4.97 and 10.3 ms.  Where tiles of 32 x 32 all run at once (one on a compute unit for FP16X3, two for FP16),
+// latency counts, and those are shortest: one of 512 x 512, FP16X3, 126 instead of 163 us with tiles of 64; of 768 x 768, which has
+// more of them, 217 instead of 201.
 enum { LARGE, MIDDLE, SMALL };
 int tile_of(int64_t large, int64_t middle, int64_t small, bool split) {
     auto rounds = [](int64_t tiles, int64_t at_once) { return (double)((tiles + at_once - 1) / at_once); };
@@ -723,9 +815,10 @@ int tile_of(int64_t large, int64_t middle, int64_t small, bool split) {
 // One product of every matrix of the batch.
 template <bool SPLIT, int STEP>
 void product(Batch& b, Factors f, const Result& result, int odd, const float* grad_scale, _Float16* ws, hipStream_t st) {
-    using Large = Shape<2, 4, 1, 2, SPLIT ? 32 : 64, SPLIT>;
-    using Middle = Shape<2, 2, 1, 1, SPLIT ? 32 : 64, SPLIT>;
-    using Small = Shape<1, 1, 4, 1, 64, SPLIT>;
+    using Large = Shape<2, 4, 1, 2, 64, SPLIT ? 32 : 64, 2, SPLIT>;
+    using Middle = Shape<2, 2, 1, 1, 64, SPLIT ? 32 : 64, 2, SPLIT>;
+    using Small = Shape<1, 1, 4, 1, 64, 64, 4, SPLIT>;
+    using Tiny = Shape<1, 1, 4, 1, 32, 64, 8, SPLIT>;
     auto launch = [&](auto shape) {
         using S = decltype(shape);
         const int groups = place(b, STEP == GRAM || STEP == POLYNOMIAL ? S::triangle : S::tiles);
@@ -736,6 +829,7 @@ void product(Batch& b, Factors f, const Result& result, int odd, const float* gr
         using S = decltype(shape);
         return place(b, STEP == GRAM || STEP == POLYNOMIAL ? S::triangle : S::tiles);
     };
+    if (count(Tiny()) <= (SPLIT ? 256 : 512)) return launch(Tiny());
     switch (tile_of(count(Large()), count(Middle()), count(Small()), SPLIT)) {
         case LARGE: return launch(Large());
         case MIDDLE: return launch(Middle());
