@@ -23,7 +23,8 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMostDim = SPLC_MAX_HEAD_DIM;
 constexpr uint32_t kFillingWaves = 4096;                     // four a SIMD: where a token's heads are no longer shared out
 constexpr uint32_t kMostGroups = 1u << 20;                   // workgroups of a launch: those lanes are counted in 32 bits
-constexpr uint32_t kGradGroups = 1024, kJoinRows = 16;
+constexpr uint32_t kGradGroups = 1024;
+constexpr int kJoinThreads = 1024, kJoinRows = 16;         // lanes of a row of workgroups' sums: 16 channels
 
 template <class T>
 struct View {
@@ -52,8 +53,7 @@ __device__ __forceinline__ float wide_of(float v) { return v; }
 __device__ __forceinline__ float wide_of(uint16_t v) { return widened(v); }
 
 template <class T, int V>
-__device__ __forceinline__ void load_wide(const T* p, float* x) {
-    const auto v = *(const SPLC_GLOBAL typename Vector<T, V>::type*)p;
+__device__ __forceinline__ void widen(typename Vector<T, V>::type v, float* x) {
     if constexpr (V == 1) {
         x[0] = wide_of(v);
     } else {
@@ -70,7 +70,7 @@ __device__ __forceinline__ void store_narrow(float* p, const float* x) {
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = x[j];
     }
-    *(SPLC_GLOBAL typename Vector<float, V>::type*)p = v;
+    __builtin_nontemporal_store(v, (SPLC_GLOBAL typename Vector<float, V>::type*)p);
 }
 template <int V>
 __device__ __forceinline__ void store_narrow(uint16_t* p, const float* x) {
@@ -85,12 +85,13 @@ __device__ __forceinline__ void store_narrow(uint16_t* p, const float* x) {
 #pragma unroll
             for (int j = 0; j < V / 2; ++j) w[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
         }
-        *(SPLC_GLOBAL typename Vector<uint16_t, V>::type*)p = __builtin_bit_cast(typename Vector<uint16_t, V>::type, w);
+        __builtin_nontemporal_store(__builtin_bit_cast(typename Vector<uint16_t, V>::type, w), (SPLC_GLOBAL typename Vector<uint16_t, V>::type*)p);
     }
 }
 
-// Pairs of a head as a lane holds them: C runs of V.  Of pair p the first coordinate is x[..][j], the second x[..][V + j] where
-// the halves lie apart; where pairs lie side by side x holds 2 V channels in their order.
+// Pairs of a head as a lane holds them: C runs of V, in two vectors of V channels each that neighbouring lanes continue.  Where the
+// halves lie apart, the vectors hold the first and the second coordinates; where pairs lie side by side, one vector lies in each half
+// of the head (or is one of two coordinates, V = 1).
 template <class T, int V, bool SIDE>
 struct Lanes {
     static constexpr int C = V == 1 ? 4 : V == 2 ? 2 : 1;    // 64 lanes x C x V pairs: 512 channels at the least
@@ -103,8 +104,8 @@ struct Lanes {
             const int p = (lane + c * per_head) * V;
             there[c] = p < d / 2;
             if (SIDE) {
-                first[c] = 2 * p;
-                second[c] = 2 * p + V;
+                first[c] = V == 1 ? 2 * p : p;
+                second[c] = V == 1 ? 2 * p + 1 : p + d / 2;
             } else if (p < r) {
                 first[c] = p;
                 second[c] = p + r;
@@ -114,12 +115,24 @@ struct Lanes {
             }
         }
     }
-    __device__ __forceinline__ void load(const T* head, float (&x)[C][2 * V]) const {
+    // A head's channels as they are in memory.
+    struct Raw {
+        typename Vector<T, V>::type a[C], b[C];
+    };
+    __device__ __forceinline__ void load(const T* head, Raw& raw) const {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (!there[c]) continue;
+            raw.a[c] = *(const SPLC_GLOBAL typename Vector<T, V>::type*)(head + first[c]);
+            raw.b[c] = *(const SPLC_GLOBAL typename Vector<T, V>::type*)(head + second[c]);
+        }
+    }
+    __device__ __forceinline__ void take(const Raw& raw, float (&x)[C][2 * V]) const {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if (there[c]) {
-                load_wide<T, V>(head + first[c], x[c]);
-                load_wide<T, V>(head + second[c], x[c] + V);
+                widen<T, V>(raw.a[c], x[c]);
+                widen<T, V>(raw.b[c], x[c] + V);
             } else {
 #pragma unroll
                 for (int j = 0; j < 2 * V; ++j) x[c][j] = 0.f;
@@ -141,22 +154,31 @@ template <int V, int C>
 struct Turn {
     float cos[C][V], sin[C][V];
 
-    __device__ __forceinline__ void at(const Rotation& how, int64_t token, int lane, int per_head) {
+    // A wave's lanes form the angles of a token, one pair each, and take what their own pairs need from LDS, which keeps a wave's
+    // accesses in their order.
+    template <bool SIDE>
+    __device__ __forceinline__ void at(const Rotation& how, int64_t token, int wave_lane, int lane, int per_head, int d, float2* shared) {
         const double position = how.wide ? (double)static_cast<const int64_t*>(how.positions)[token]
                                          : (double)static_cast<const int32_t*>(how.positions)[token];
+        __builtin_amdgcn_wave_barrier();
+        for (int p = wave_lane; p < how.r; p += 64) {
+            const double turns = position * (how.frequencies[p] * 0.15915494309189533577);
+            float2 v;
+            sincospif(2.f * (float)(turns - rint(turns)), &v.y, &v.x);
+            v.x *= how.magnitude;
+            v.y *= how.magnitude * how.sign;
+            shared[p] = v;
+        }
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int p = (lane + c * per_head) * V + j;
-                cos[c][j] = 1.f;
-                sin[c][j] = 0.f;
-                if (p < how.r) {
-                    const double turns = position * (how.frequencies[p] * 0.15915494309189533577);
-                    sincospif(2.f * (float)(turns - rint(turns)), &sin[c][j], &cos[c][j]);
-                    cos[c][j] *= how.magnitude;
-                    sin[c][j] *= how.magnitude * how.sign;
-                }
+                const int run = (lane + c * per_head) * V;
+                const int p = !SIDE || V == 1 ? run + j : j < V / 2 ? run / 2 + j : (run + d / 2) / 2 + j - V / 2;
+                const float2 v = shared[p < kMostDim / 2 ? p : 0];
+                cos[c][j] = p < how.r ? v.x : 1.f;
+                sin[c][j] = p < how.r ? v.y : 0.f;
             }
         }
     }
@@ -191,16 +213,21 @@ __device__ __forceinline__ float dot(const float (&x)[C][N], const float (&y)[C]
     }
     return sum;
 }
+// Gains as fp32 in LDS for all waves of a workgroup, and a lane's from there: in registers they would cost waves.
+__device__ __forceinline__ void keep_gain(float* kept, const void* gain, int bf16, int d) {
+    if (!gain) return;
+    for (int i = threadIdx.x; i < d; i += kThreads)
+        kept[i] = bf16 ? widened(static_cast<const uint16_t*>(gain)[i]) : static_cast<const float*>(gain)[i];
+}
 template <class T, int V, bool SIDE, int C>
-__device__ __forceinline__ void load_gain(const Lanes<T, V, SIDE>& lanes, const void* gain, int bf16, float (&w)[C][2 * V]) {
+__device__ __forceinline__ void take_gain(const Lanes<T, V, SIDE>& lanes, const float* kept, float (&w)[C][2 * V]) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+        const int a = lanes.there[c] ? lanes.first[c] : 0, b = lanes.there[c] ? lanes.second[c] : 0;
 #pragma unroll
-        for (int j = 0; j < 2 * V; ++j) {
-            const int at = j < V ? lanes.first[c] + j : lanes.second[c] + j - V;
-            w[c][j] = !lanes.there[c] ? 0.f
-                      : bf16          ? widened(static_cast<const uint16_t*>(gain)[at])
-                                      : static_cast<const float*>(gain)[at];
+        for (int j = 0; j < V; ++j) {
+            w[c][j] = kept[a + j];
+            w[c][V + j] = kept[b + j];
         }
     }
 }
@@ -220,32 +247,54 @@ struct Forward {
     float eps, inverse_d;
 };
 
+// Loads of so many runs of heads are under way at once, the first of them while the angles are formed.  More cost registers, and with
+// them waves.  16384 x 32 heads of 128 bf16 channels: norm 55 us (4: 72, of one wave less a SIMD), gradient 96 (2: 109).
+constexpr int kRunsAhead = 3, kWavesASimd = 5;
+constexpr int grad_runs_ahead(int v) { return v == 8 ? 1 : 2; }
+constexpr int grad_waves_a_simd(int v) { return v == 8 ? 4 : 3; }
+
 template <class T, int V, bool SIDE, bool NORM>
-__global__ __launch_bounds__(kThreads) void heads_kernel(Forward<T> args, Rotation how, Shares share) {
+__global__ __launch_bounds__(kThreads, kWavesASimd) void heads_kernel(Forward<T> args, Rotation how, Shares share) {
     using Mine = Lanes<T, V, SIDE>;
     constexpr int C = Mine::C;
+    __shared__ float2 angles[kWaves][kMostDim / 2];
     const int lane = threadIdx.x & 63, in_head = lane & (share.per_head - 1), slot = lane >> share.lane_bits;
-    const int at_once = 64 >> share.lane_bits;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at_once = 64 >> share.lane_bits;
     const Mine mine(in_head, share.per_head, share.d, how.r);
     const int64_t items = share.tokens * share.parts;
-    for (int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * kWaves) {
+    const int first_runs = (args.in[0].heads + at_once - 1) / at_once, runs = first_runs + (args.in[1].heads + at_once - 1) / at_once;
+    __shared__ __align__(16) float gains[NORM ? 2 : 1][NORM ? kMostDim : 1];
+    if (NORM) {
+        keep_gain(gains[0], args.gain[0], args.gain_bf16, share.d);
+        keep_gain(gains[NORM], args.gain[1], args.gain_bf16, share.d);
+        __syncthreads();
+    }
+    for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
         const int64_t token = item / share.parts;
-        int run = (int)(item - token * share.parts);
+        const int part = (int)(item - token * share.parts);
         Turn<V, C> turn;
-        turn.at(how, token, in_head, share.per_head);
-        for (int side = 0; side < 2; ++side) {
-            const View<const T> in = args.in[side];
-            const View<T> out = args.out[side];
-            const int runs = (in.heads + at_once - 1) / at_once;
-            float w[C][2 * V];
-            if (NORM && run < runs) load_gain(mine, args.gain[side], args.gain_bf16, w);
-            for (; run < runs; run += share.parts) {
-                const int head = run * at_once + slot;
-                if (head >= in.heads) continue;              // (sums below are among the lanes of one head)
+        for (int run = part; run < runs; run += kRunsAhead * share.parts) {
+            typename Mine::Raw raw[kRunsAhead];
+#pragma unroll
+            for (int u = 0; u < kRunsAhead; ++u) {
+                const int r = run + u * share.parts, side = r >= first_runs;
+                const int head = (side ? r - first_runs : r) * at_once + slot;
+                const View<const T>& in = side ? args.in[1] : args.in[0];
+                if (r < runs && head < in.heads) mine.load(in.at + token * in.token + head * in.head, raw[u]);
+            }
+            if (run == part) turn.template at<SIDE>(how, token, lane, in_head, share.per_head, share.d, angles[wave]);
+#pragma unroll
+            for (int u = 0; u < kRunsAhead; ++u) {
+                const int r = run + u * share.parts, side = r >= first_runs;
+                const int head = (side ? r - first_runs : r) * at_once + slot;
+                const View<T>& out = side ? args.out[1] : args.out[0];
+                if (r >= runs || head >= out.heads) continue;    // (sums below are among the lanes of one head)
                 float x[C][2 * V];
-                mine.load(in.at + token * in.token + head * in.head, x);
+                mine.take(raw[u], x);
                 if (NORM) {
                     const float inverse = rsqrtf(fmaf(head_sum(dot(x, x), share.per_head), args.inverse_d, args.eps));
+                    float w[C][2 * V];
+                    take_gain(mine, gains[side ? NORM : 0], w);
 #pragma unroll
                     for (int c = 0; c < C; ++c) {
 #pragma unroll
@@ -255,7 +304,6 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(Forward<T> args, Rotati
                 turn.template turn<SIDE, false>(x);
                 mine.store(out.at + token * out.token + head * out.head, x);
             }
-            run -= runs;
         }
     }
 }
@@ -277,68 +325,78 @@ struct Backward {
 };
 
 template <class T, int V, bool SIDE>
-__global__ __launch_bounds__(kThreads) void heads_grad_kernel(Backward<T> args, Rotation how, Shares share) {
+__global__ __launch_bounds__(kThreads, grad_waves_a_simd(V)) void heads_grad_kernel(Backward<T> args, Rotation how, Shares share) {
     using Mine = Lanes<T, V, SIDE>;
     constexpr int C = Mine::C;
+    constexpr int kAhead = grad_runs_ahead(V);
     __shared__ float sums[kWaves][kMostDim];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in_head = lane & (share.per_head - 1), slot = lane >> share.lane_bits;
-    const int at_once = 64 >> share.lane_bits;
+    __shared__ float2 angles[kWaves][kMostDim / 2];
+    const int lane = threadIdx.x & 63, in_head = lane & (share.per_head - 1), slot = lane >> share.lane_bits;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at_once = 64 >> share.lane_bits;
     const Mine mine(in_head, share.per_head, share.d, how.r);
     const int64_t items = share.tokens * share.parts;
-    float dw[2][C][2 * V], w[2][C][2 * V];
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        if (args.x[side].heads > 0) load_gain(mine, args.gain[side], args.gain_bf16, w[side]);
+    __shared__ __align__(16) float gain[kMostDim];
+    for (int side = 0; side < 2; ++side) {                   // queries, then keys: the sums of one gain take registers at a time
+        const View<const T> in = args.x[side], grad = args.dy[side];
+        const View<T> out = args.dx[side];
+        const int runs = (in.heads + at_once - 1) / at_once;
+        __syncthreads();
+        keep_gain(gain, args.gain[side], args.gain_bf16, share.d);
+        __syncthreads();
+        float dw[C][2 * V];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
-            for (int j = 0; j < 2 * V; ++j) dw[side][c][j] = 0.f;
+            for (int j = 0; j < 2 * V; ++j) dw[c][j] = 0.f;
         }
-    }
-    for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
-        const int64_t token = item / share.parts;
-        int run = (int)(item - token * share.parts);
-        Turn<V, C> turn;
-        turn.at(how, token, in_head, share.per_head);
+        for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
+            const int64_t token = item / share.parts;
+            const int part = (int)(item - token * share.parts);
+            Turn<V, C> turn;
+            for (int run = part; run < runs; run += kAhead * share.parts) {
+                typename Mine::Raw raw_x[kAhead], raw_g[kAhead];
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            const int heads = args.x[side].heads, runs = (heads + at_once - 1) / at_once;
-            for (; run < runs; run += share.parts) {
-                const int head = run * at_once + slot;
-                if (head >= heads) continue;
-                float x[C][2 * V], g[C][2 * V];
-                mine.load(args.x[side].at + token * args.x[side].token + head * args.x[side].head, x);
-                mine.load(args.dy[side].at + token * args.dy[side].token + head * args.dy[side].head, g);
-                const float inverse = rsqrtf(fmaf(head_sum(dot(x, x), share.per_head), args.inverse_d, args.eps));
-                turn.template turn<SIDE, true>(g);
+                for (int u = 0; u < kAhead; ++u) {
+                    const int head = (run + u * share.parts) * at_once + slot;
+                    if (head >= in.heads) continue;
+                    mine.load(in.at + token * in.token + head * in.head, raw_x[u]);
+                    mine.load(grad.at + token * grad.token + head * grad.head, raw_g[u]);
+                }
+                if (run == part) turn.template at<SIDE>(how, token, lane, in_head, share.per_head, share.d, angles[wave]);
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
+                for (int u = 0; u < kAhead; ++u) {
+                    const int head = (run + u * share.parts) * at_once + slot;
+                    if (head >= in.heads) continue;          // (sums below are among the lanes of one head)
+                    float x[C][2 * V], g[C][2 * V], w[C][2 * V];
+                    mine.take(raw_x[u], x);
+                    mine.take(raw_g[u], g);
+                    const float inverse = rsqrtf(fmaf(head_sum(dot(x, x), share.per_head), args.inverse_d, args.eps));
+                    turn.template turn<SIDE, true>(g);
+                    take_gain(mine, gain, w);
 #pragma unroll
-                    for (int j = 0; j < 2 * V; ++j) {
-                        x[c][j] *= inverse;
-                        dw[side][c][j] = fmaf(g[c][j], x[c][j], dw[side][c][j]);
-                        g[c][j] *= w[side][c][j];
+                    for (int c = 0; c < C; ++c) {
+#pragma unroll
+                        for (int j = 0; j < 2 * V; ++j) {
+                            x[c][j] *= inverse;
+                            dw[c][j] = fmaf(g[c][j], x[c][j], dw[c][j]);
+                            g[c][j] *= w[c][j];
+                        }
                     }
-                }
-                const float mean = head_sum(dot(g, x), share.per_head) * args.inverse_d;
+                    const float mean = head_sum(dot(g, x), share.per_head) * args.inverse_d;
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
+                    for (int c = 0; c < C; ++c) {
 #pragma unroll
-                    for (int j = 0; j < 2 * V; ++j) x[c][j] = inverse * fmaf(-mean, x[c][j], g[c][j]);
+                        for (int j = 0; j < 2 * V; ++j) x[c][j] = inverse * fmaf(-mean, x[c][j], g[c][j]);
+                    }
+                    mine.store(out.at + token * out.token + head * out.head, x);
                 }
-                mine.store(args.dx[side].at + token * args.dx[side].token + head * args.dx[side].head, x);
             }
-            run -= runs;
         }
-    }
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        if (side == 1) __syncthreads();
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
             for (int j = 0; j < 2 * V; ++j) {
-                float sum = dw[side][c][j];
+                float sum = dw[c][j];
                 for (int step = share.per_head; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
                 if (slot == 0 && mine.there[c]) sums[wave][j < V ? mine.first[c] + j : mine.second[c] + j - V] = sum;
             }
@@ -353,20 +411,27 @@ __global__ __launch_bounds__(kThreads) void heads_grad_kernel(Backward<T> args, 
     }
 }
 
-// Sums of the workgroups' partial sums, 16 channels a workgroup.
-__global__ __launch_bounds__(kThreads) void heads_join_kernel(const float* __restrict__ partial, int groups, int d, float* dq_gain,
-                                                              float* dk_gain, int accumulate) {
-    __shared__ float sums[kThreads];
-    const int i = blockIdx.x * kJoinRows + threadIdx.x % kJoinRows;
-    float sum = 0.f;
-    if (i < 2 * d) {
-#pragma unroll 8
-        for (int g = threadIdx.x / kJoinRows; g < groups; g += kThreads / kJoinRows) sum += partial[(int64_t)g * 2 * d + i];
+// Sums of the workgroups' partial sums, 16 channels a workgroup, all of its loads at once.
+__global__ __launch_bounds__(kJoinThreads) void heads_join_kernel(const float* __restrict__ partial, int groups, int d, float* dq_gain,
+                                                                  float* dk_gain, int accumulate) {
+    constexpr int kParts = kJoinThreads / kJoinRows, kEach = kGradGroups / kParts;
+    __shared__ float sums[kJoinThreads];
+    const int i = blockIdx.x * kJoinRows + threadIdx.x % kJoinRows, part = threadIdx.x / kJoinRows;
+    float v[kEach], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int g = part + e * kParts;
+        v[e] = i < 2 * d && g < groups ? partial[(int64_t)g * 2 * d + i] : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) sum += v[e];
     sums[threadIdx.x] = sum;
     __syncthreads();
-    if (threadIdx.x >= kJoinRows || i >= 2 * d) return;
-    for (int part = 1; part < kThreads / (int)kJoinRows; ++part) sum += sums[part * kJoinRows + threadIdx.x];
+    for (int half = kParts / 2; half > 0; half /= 2) {
+        if (part < half) sums[threadIdx.x] = sum += sums[threadIdx.x + half * kJoinRows];
+        __syncthreads();
+    }
+    if (part > 0 || i >= 2 * d) return;
     float* out = i < d ? dq_gain : dk_gain;
     if (!out) return;
     out += i < d ? i : i - d;
@@ -553,7 +618,7 @@ int sparseloco_qk_norm_rotary_grad(const sparseloco_heads* grad_q_out, const spa
         });
         if (rc != SPLC_OK) return rc;
     }
-    hipLaunchKernelGGL(heads_join_kernel, dim3((2 * head_dim + kJoinRows - 1) / kJoinRows), dim3(kThreads), 0,
+    hipLaunchKernelGGL(heads_join_kernel, dim3((2 * head_dim + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), 0,
                        static_cast<hipStream_t>(stream), static_cast<const float*>(ws), (int)groups, head_dim, grad_q_gain, grad_k_gain,
                        accumulate);
     return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
