@@ -30,7 +30,7 @@ using namespace splc;
 constexpr int kThreads = 256;
 constexpr int kPad = 64;                                     // row lengths of the operands are multiples of it, zeros behind the end
 constexpr int kMostMatrices = 128;                           // of a batch: their descriptions are kernel arguments
-constexpr int64_t kBatchElements = (int64_t)1 << 29;         // of a batch, but one matrix at the least
+constexpr int64_t kBatchElements = (int64_t)1 << 30;         // of a batch, but one matrix at the least
 constexpr int kMostSide = 1 << 22;                           // rows and columns: offsets inside a tile's rows stay in 32 bits
 constexpr int kMostSteps = SPLC_MAX_ORTHO_STEPS;
 
@@ -57,29 +57,30 @@ struct Batch {
     Matrix of[kMostMatrices];
 };
 // Operands of a matrix: R and T of this step and of the next (one place for both where the third product does not read it: R of a
-// wide matrix, T of a tall one), A and B.  Their elements are hi + lo where they are split, 32 of hi and the same 32 of lo side by
+// wide matrix, T of a tall one), and squares: A, B and more.  Their elements are hi + lo where they are split, 32 of hi and the same 32 of lo side by
 // side, so that a row of 32 for the products is 128 bytes; otherwise hi alone, and lo of R, which is no operand then, behind it.
 template <bool SPLIT>
 struct Planes {
     static constexpr int kParts = SPLIT ? 2 : 1;
-    _Float16 *r_first, *t_first, *a, *b;
-    int64_t r_next, t_next;
-    __host__ __device__ static int64_t elements(const Matrix& m) {
-        return 2 * m.r_plane() * (m.tall() ? 2 : 1) + kParts * m.t_plane() * (m.tall() ? 1 : 2) + 2 * kParts * m.a_plane();
+    _Float16 *r_first, *t_first, *s_first;
+    int64_t r_next, t_next, s_next;
+    __host__ __device__ static int64_t elements(const Matrix& m, int squares) {
+        return 2 * m.r_plane() * (m.tall() ? 2 : 1) + kParts * m.t_plane() * (m.tall() ? 1 : 2) + squares * kParts * m.a_plane();
     }
     __device__ __forceinline__ Planes(_Float16* ws, const Matrix& m) {
         r_first = ws + m.at;
         r_next = m.tall() ? 2 * m.r_plane() : 0;
         t_first = r_first + 2 * m.r_plane() + r_next;
         t_next = m.tall() ? 0 : kParts * m.t_plane();
-        a = t_first + kParts * m.t_plane() + t_next;
-        b = a + kParts * m.a_plane();
+        s_first = t_first + kParts * m.t_plane() + t_next;
+        s_next = kParts * m.a_plane();
     }
     // Of hi of element (row, col) from an operand's first, rows of `ld`; and of lo from there in R.
     static __device__ __forceinline__ int64_t place(int row, int col, int ld) {
         return (int64_t)row * ld * kParts + (SPLIT ? (col & ~31) * 2 + (col & 31) : col);
     }
     static __device__ __forceinline__ int64_t r_lo(const Matrix& m) { return SPLIT ? 32 : m.r_plane(); }
+    __device__ __forceinline__ _Float16* square(int i) const { return s_first + i * s_next; }
     __device__ __forceinline__ _Float16* r(int odd) const { return r_first + odd * r_next; }
     __device__ __forceinline__ _Float16* t(int odd) const { return t_first + odd * t_next; }
 };
@@ -299,11 +300,15 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Batch, From from, const
 
 // ---------------------------------------------------------------- products
 
-enum { GRAM = 0, POLYNOMIAL = 1, APPLY = 2, LAST = 3 };
+// GRAM: X X^T into a square.  SQUARE: a square times a square, which commute.  APPLY: a square times X; LAST: the result's step.
+enum { GRAM = 0, SQUARE = 1, APPLY = 2, LAST = 3 };
 
-// The factors of one product: its result is sum * product + old * own, in the result's range.
-struct Factors {
-    float own, product;
+// One product: sum * product + old * own + other * more, in the result's range.  The squares p and q that it multiplies (APPLY: p alone),
+// those that it adds (other: -1, none) and the one that it writes; APPLY adds to X itself.
+struct Product {
+    int step;
+    float product, own, more;
+    int8_t p, q, old, other, out;
 };
 struct Result {                                              // of the last step
     int to;                                                  // SPLC_F32, SPLC_BF16: the matrix itself; -1: the parameters' step
@@ -362,7 +367,7 @@ __device__ __forceinline__ int exchange(int row) {
 // BK elements (hi, lo) of every row of P and Q at a time go to LDS, without passing registers, while the BK before them are multiplied.  Then the sums pass LDS, block by block, to be
 // finished and stored along rows of C, 16 bytes a lane, and once more along its columns for the transposed (or mirrored) copy.
 template <class S, int STEP>
-__global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Factors f, Result result, int odd,
+__global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f, Result result, int odd,
                                                             const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
     constexpr bool SPLIT = S::SPLIT;
     constexpr int SIDE = S::kSide;
@@ -384,7 +389,7 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Factors f,
     const Planes<SPLIT> planes(ws, m);
     const int n = m.n(), ldn = stride(n), ldc = stride(m.cols), ldr = stride(m.rows);
     int ti, tj;
-    if (STEP == GRAM || STEP == POLYNOMIAL) {
+    if (STEP == GRAM || STEP == SQUARE) {
         S::triangle_place(place, ti, tj);
     } else {
         ti = place % S::down(m);
@@ -397,14 +402,15 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Factors f,
         p_rows = q_rows = n;
         depth = padded(m.tall() ? m.rows : m.cols);
         ld_p = ld_q = m.tall() ? ldr : ldc;
-    } else if (STEP == POLYNOMIAL) {
-        p = q = planes.a;
+    } else if (STEP == SQUARE) {
+        p = planes.square(f.p);
+        q = planes.square(f.q);
         p_rows = q_rows = n;
         depth = padded(n);
         ld_p = ld_q = ldn;
     } else {
-        p = m.tall() ? planes.r(odd) : planes.b;
-        q = m.tall() ? planes.b : planes.t(odd);
+        p = m.tall() ? planes.r(odd) : planes.square(f.p);
+        q = m.tall() ? planes.square(f.p) : planes.t(odd);
         p_rows = m.rows;
         q_rows = m.cols;
         depth = padded(n);
@@ -453,14 +459,14 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Factors f,
     struct Operands {
         half8 x[kI][kParts], y[kJ][kParts];
     };
-    constexpr bool kTriangle = STEP == GRAM || STEP == POLYNOMIAL;
+    constexpr bool kTriangle = STEP == GRAM || STEP == SQUARE;
     const int rows = kTriangle ? n : m.rows, cols = kTriangle ? n : m.cols, ld = kTriangle ? ldn : ldc, ld_t = kTriangle ? ldn : ldr;
     // a X is added here, to X as hi + lo, and not as part of B: its sums would be four times as large, and so would their roundings
     // (1.4 times the error of fp32 products where it is 0.7 times so).
-    constexpr bool kOld = STEP != GRAM, kOldLo = STEP != POLYNOMIAL || SPLIT;
+    constexpr bool kOld = STEP != GRAM, kOldLo = STEP != SQUARE || SPLIT;
     const int64_t r_lo = planes.r_lo(m);
-    const _Float16* old = STEP == POLYNOMIAL ? planes.a : planes.r(odd);
-    _Float16* to = STEP == GRAM ? planes.a : STEP == POLYNOMIAL ? planes.b : planes.r(odd ^ 1);
+    const _Float16* old = STEP == SQUARE ? planes.square(f.old) : planes.r(odd);
+    _Float16* to = kTriangle ? planes.square(f.out) : planes.r(odd ^ 1);
     _Float16* to_t = kTriangle ? to : planes.t(odd ^ 1);
     // Passes over a block, by one wave or by all that share it: 8 columns a lane along its rows, then 8 rows a lane along its columns.
     constexpr int kAcross = SIDE / 8, kDown = 64 / kAcross, kPasses = SIDE / kDown / S::WK > 0 ? SIDE / kDown / S::WK : 1;
@@ -474,7 +480,7 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Factors f,
             if (row >= rows || col >= ld) continue;
             const _Float16* from_old = old + planes.place(row, col, ld);
             old_hi[pass] = *(const half8*)from_old;
-            if (kOldLo) old_lo[pass] = *(const half8*)(from_old + (STEP == POLYNOMIAL ? 32 : r_lo));
+            if (kOldLo) old_lo[pass] = *(const half8*)(from_old + (STEP == SQUARE ? 32 : r_lo));
         }
     };
     if (S::WK > 1) load_old(row0, col0);                     // (few registers: their latency passes beside the products')
@@ -600,6 +606,12 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Factors f,
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = fmaf(f.own, (float)old_hi[pass][e] + (kOldLo ? (float)old_lo[pass][e] : 0.f), v[e]);
             }
+            if (STEP == SQUARE && SPLIT && f.other >= 0 && there) {
+                const _Float16* from_other = planes.square(f.other) + planes.place(row, col, ld);
+                const half8 hi = *(const half8*)from_other, lo = *(const half8*)(from_other + 32);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(f.more, (float)hi[e] + (float)lo[e], v[e]);
+            }
             if (STEP != LAST) {
                 half8 hi, lo;
 #pragma unroll
@@ -717,74 +729,187 @@ double largest_even(double b, double c, double most) {       // of |b y + c y^2|
     return found;
 }
 
-// The powers of two that A, B and X are held times, and the factors of the three products of every step.
+// The products of all steps in their order, with the powers of two that their results are held times.
 struct Steps {
-    int count = 0;
+    std::vector<Product> of;
     float first = 0.f;                                       // of X before the first step
-    Factors gram[kMostSteps], polynomial[kMostSteps], apply[kMostSteps];
 };
-bool ranges(const double* coefficients, int steps, Steps& s) {
+// Several steps at once in squares alone, which are the smaller matrices where X is wide: one step, X <- p(A) X with p(A) = a + B,
+// makes A into p A p, and for several of them
+//     A = X X^T;   for each:  B = b A + c A^2,  Q <- p Q,  A <- p (p A);   X <- Q X,
+// where only the first A and the last product have X's long side.  Q is held without its multiple of 1, alpha, as B is: both are zero
+// where X is small.  alpha is what roundings of Q and of A grow by before they come to X: at most 64, of at most three steps
+// (40 for the usual polynomial; five steps without a new A from X: 60 times the error).
+constexpr double kMostAlpha = 64.0;
+constexpr int kMostAtOnce = 3, kSquares = 2, kSquaresAtOnce = 5;
+
+bool steps_of(const double* coefficients, int steps, bool at_once, Steps& s) {
     static const double usual[] = {3.4445, -4.7750, 2.0315};
     if (steps < 1 || steps > kMostSteps) return false;
     auto range = [](double bound) { return 14 - (int)std::ceil(std::log2(std::max(bound, 1e-3))); };
+    auto power = [](double v, int exponent) { return (float)std::ldexp(v, exponent); };
+    auto at = [&](int k) { return coefficients ? coefficients + 3 * k : usual; };
     double most = 1.0;                                       // bound on the singular values of X
     int x = range(most);
-    s.count = steps;
-    s.first = (float)std::ldexp(1.0, x);
-    for (int k = 0; k < steps; ++k) {
-        const double* p = coefficients ? coefficients + 3 * k : usual;
+    s.of.clear();
+    s.first = power(1.0, x);
+    for (int k = 0; k < steps; ++k)
         for (int i = 0; i < 3; ++i)
-            if (!finite64(p[i]) || std::fabs(p[i]) > 1e4) return false;
-        const int a = range(most * most), b = range(largest_even(p[1], p[2], most * most));
-        const bool last = k + 1 == steps;
-        most = largest(p[0], p[1], p[2], most);
-        if (!finite64(most) || most > 1024.0) return false;
-        const int next = last ? 0 : range(most);
-        s.gram[k] = {0.f, (float)std::ldexp(1.0, a - 2 * x)};
-        s.polynomial[k] = {(float)std::ldexp(p[1], b - a), (float)std::ldexp(p[2], b - 2 * a)};
-        s.apply[k] = {(float)std::ldexp(p[0], next - x), (float)std::ldexp(1.0, next - b - x)};
+            if (!finite64(at(k)[i]) || std::fabs(at(k)[i]) > 1e4) return false;
+    for (int k = 0; k < steps;) {
+        int count = 1;
+        double alpha = at(k)[0];
+        while (at_once && count < kMostAtOnce && k + count < steps && std::fabs(alpha * at(k + count)[0]) <= kMostAlpha)
+            alpha *= at(k + count++)[0];
+        // |Q - alpha| for singular values up to the bound, at many of them; half as much again for those between.
+        std::vector<double> largest_q((size_t)count, 0.0);
+        for (int i = 0; count > 1 && i <= 512; ++i) {
+            double v = most * i / 512, q = 1.0, of_one = 1.0;
+            for (int j = 0; j < count; ++j) {
+                const double* p = at(k + j);
+                const double f = p[0] + v * v * (p[1] + v * v * p[2]);
+                q *= f;
+                v *= f;
+                of_one *= p[0];
+                largest_q[(size_t)j] = std::max(largest_q[(size_t)j], 1.5 * std::fabs(q - of_one));
+            }
+        }
+        int a = range(most * most), q = 0, in_q = 0, in_b = 1, free = 3;
+        s.of.push_back({GRAM, power(1.0, a - 2 * x), 0.f, 0.f, 0, 0, 0, -1, 0});
+        alpha = 1.0;
+        for (int j = 0; j < count; ++j) {
+            const double* p = at(k + j);
+            const int b = range(largest_even(p[1], p[2], most * most));
+            s.of.push_back({SQUARE, power(p[2], b - 2 * a), power(p[1], b - a), 0.f, 0, 0, 0, -1, (int8_t)in_b});
+            if (j == 0) {
+                q = b;
+                in_q = in_b;
+                in_b = 3;
+                free = 4;
+            } else {
+                const int next_q = range(largest_q[(size_t)j]);
+                s.of.push_back({SQUARE, power(1.0, next_q - b - q), power(p[0], next_q - q), power(alpha, next_q - b), (int8_t)in_b,
+                                (int8_t)in_q, (int8_t)in_q, (int8_t)in_b, (int8_t)free});
+                q = next_q;
+                std::swap(in_q, free);                       // (what was Q is free, and B is below)
+                std::swap(in_b, free);
+            }
+            alpha *= p[0];
+            const double grown = largest(p[0], p[1], p[2], most);
+            if (!finite64(grown) || grown > 1024.0) return false;
+            if (j + 1 < count) {
+                const int holds_b = j == 0 ? in_q : free;    // B of this step
+                const int t = range(most * grown), next_a = range(grown * grown);
+                s.of.push_back({SQUARE, power(1.0, t - b - a), power(p[0], t - a), 0.f, (int8_t)holds_b, 0, 0, -1, 2});
+                s.of.push_back({SQUARE, power(1.0, next_a - b - t), power(p[0], next_a - t), 0.f, (int8_t)holds_b, 2, 2, -1, 0});
+                a = next_a;
+            }
+            most = grown;
+        }
+        k += count;
+        const int next = k < steps ? range(most) : 0;
+        s.of.push_back({k < steps ? APPLY : LAST, power(1.0, next - q - x), power(alpha, next - x), 0.f, (int8_t)in_q, 0, 0, -1, 0});
         x = next;
     }
     return true;
 }
 
+// Tiles of a launch by their side, 32 << size, and what they take (us) where the longest product has `depth` terms: as many rounds as
+// tiles fit on 256 compute units, one, or two of those that LDS holds twice (of which the last half, alone on its units, takes 0.55 of
+// a round), and for a round what was measured.  MI355X, us: 32 of 2048 x 2048, FP16X3, products of 2048 terms, 8 rounds of 256 tiles 1500;
+// 3 of 5630 x 2050, symmetric ones of 2050 and of 5630 terms, a round of 128 tiles 125 and 301; 9 of 768 x 2048, of 768 and 2048 terms, 3
+// rounds of 64 tiles 38 and 72.  Where tiles of 32 x 32 all run at once latency counts, and those are shortest: one of 512 x 512, the
+// whole call, 126 us, with tiles of 64 163; of 768 x 768, which has more of them, 217 and 201.
+enum { TINY, SMALL, MIDDLE, LARGE };
+struct Tile {
+    int size;
+    double us;
+};
+Tile tile_of(const int64_t (&tiles)[4], double depth, bool split) {
+    if (tiles[TINY] <= (split ? 256 : 512)) return {TINY, 3.0 + depth * 0.006};
+    auto rounds = [](int64_t n, bool twice) {
+        if (!twice) return (double)((n + 255) / 256);
+        return (double)(n / 512) + (n % 512 == 0 ? 0.0 : n % 512 <= 256 ? 0.55 : 1.0);
+    };
+    const double us[3] = {rounds(tiles[SMALL], !split) * (split ? 4.5 + 0.0103 * depth : 2.0 + 0.0116 * depth),
+                          rounds(tiles[MIDDLE], true) * (split ? 6.0 + 0.055 * depth : 7.0 + 0.0226 * depth),
+                          rounds(tiles[LARGE], false) * (split ? 37.0 + 0.07 * depth : 40.0 + 0.0245 * depth)};
+    const int best = (int)(std::min_element(us, us + 3) - us);
+    return {SMALL + best, us[best]};
+}
+// Of a product of some matrices: symmetric or not, along their longer sides or their shorter ones.
+template <class Matrices>
+Tile tile_of(const Matrices& all, int count, bool triangle, bool along, bool split) {
+    int64_t tiles[4] = {0, 0, 0, 0}, depth = 0;
+    for (int m = 0; m < count; ++m) {
+        for (int i = 0; i < 4; ++i) {
+            const int64_t side = 32 << i, down = (padded(all[m].rows) + side - 1) / side, across = (padded(all[m].cols) + side - 1) / side;
+            const int64_t n = std::min(down, across);
+            tiles[i] += triangle ? n * (n + 1) / 2 : down * across;
+        }
+        depth = std::max<int64_t>(depth, along ? std::max(all[m].rows, all[m].cols) : all[m].n());
+    }
+    return tile_of(tiles, (double)depth, split);
+}
+
+// Whether matrices that are wide enough take several steps at once (with operands as exact as fp32 only).  In flops of five steps, units
+// of n^3 and m = r n, that is 6 r + 14 instead of 15 r + 5, but 18 launches instead of 15, and apart from the others.  So by what the
+// launches take, where that is 15 % less.  MI355X, ms, apart and together: 9 of 768 x 2048 beside 12 of 768 x 768 1.68 and 1.43, 3 of
+// 5630 x 2050 3.11 and 4.45, the 0.9B model 75.7 and 92.6.
+bool wide(const Matrix& m) { return 2 * std::max(m.rows, m.cols) >= 3 * m.n(); }
+double estimated(const std::vector<Matrix>& all, int grams, int squares, int applies) {
+    auto launch = [&](bool triangle, bool along) { return 2.0 + tile_of(all, (int)all.size(), triangle, along, true).us; };
+    return all.empty() ? 0.0 : grams * launch(true, true) + squares * launch(true, false) + applies * launch(false, false);
+}
+
 struct Shapes {
-    std::vector<Batch> batches;
+    std::vector<Batch> batches;                              // first those whose matrices take several steps at once
+    size_t at_once = 0;                                      // so many
     int64_t planes = 0, chunks = 0;                          // elements of the largest batch's planes; chunks of all tensors
 };
 int64_t ws_bytes(const Shapes& s, int tensors) { return 2 * s.planes + 8 * (s.chunks + tensors) + 128; }
 
-int shapes(const sparseloco_plan* plan, const int64_t* rows, int matmul, Shapes& s) {
-    if (!plan || !rows || (matmul != SPLC_MATMUL_FP16 && matmul != SPLC_MATMUL_FP16X3)) return SPLC_EINVAL;
-    const bool three = matmul == SPLC_MATMUL_FP16X3;
-    s.chunks = plan->n_update;
-    std::vector<Matrix> all;
-    int64_t total = 0;
-    for (int i = 0; i < plan->n_tensors; ++i) {
-        const int64_t n = plan->numel[(size_t)i];
-        if (rows[i] < 0 || (n > 0 && (rows[i] < 1 || n % rows[i] != 0))) return SPLC_EINVAL;
-        if (n == 0) continue;
-        if (rows[i] > kMostSide || n / rows[i] > kMostSide) return SPLC_EINVAL;
-        all.push_back(Matrix{0, (int)rows[i], (int)(n / rows[i]), i, 0});
-        total += n;
-    }
-    // Batches of like size; the longest products first, so that those that are left at the end of a launch are short ones.
+// Batches of like size; the longest products first, so that those that are left at the end of a launch are short ones.
+void add_batches(std::vector<Matrix>& all, bool split, int squares, Shapes& s) {
+    std::stable_sort(all.begin(), all.end(), [](const Matrix& x, const Matrix& y) { return std::max(x.rows, x.cols) > std::max(y.rows, y.cols); });
+    int64_t total = 0, elements = 0, at = 0;
+    for (const Matrix& m : all) total += (int64_t)m.rows * m.cols;
     const int64_t each = total / std::max<int64_t>(1, (total + kBatchElements - 1) / kBatchElements);
-    int64_t elements = 0, at = 0;
     for (const Matrix& m : all) {
-        if (s.batches.empty() || s.batches.back().count == kMostMatrices || elements >= each) {
+        if (&m == all.data() || s.batches.back().count == kMostMatrices || elements >= each) {
             s.batches.push_back(Batch{0, 0, {}});
             elements = at = 0;
         }
         Batch& b = s.batches.back();
         b.of[b.count] = m;
         b.of[b.count++].at = at;
-        at += three ? Planes<true>::elements(m) : Planes<false>::elements(m);
+        at += split ? Planes<true>::elements(m, squares) : Planes<false>::elements(m, squares);
         elements += (int64_t)m.rows * m.cols;
         s.planes = std::max(s.planes, at);
     }
-    for (Batch& b : s.batches)
-        std::stable_sort(b.of, b.of + b.count, [](const Matrix& x, const Matrix& y) { return std::max(x.rows, x.cols) > std::max(y.rows, y.cols); });
+}
+
+int shapes(const sparseloco_plan* plan, const int64_t* rows, int matmul, Shapes& s) {
+    if (!plan || !rows || (matmul != SPLC_MATMUL_FP16 && matmul != SPLC_MATMUL_FP16X3)) return SPLC_EINVAL;
+    const bool split = matmul == SPLC_MATMUL_FP16X3;
+    s.chunks = plan->n_update;
+    std::vector<Matrix> all, apart, others;
+    for (int i = 0; i < plan->n_tensors; ++i) {
+        const int64_t n = plan->numel[(size_t)i];
+        if (rows[i] < 0 || (n > 0 && (rows[i] < 1 || n % rows[i] != 0))) return SPLC_EINVAL;
+        if (n == 0) continue;
+        if (rows[i] > kMostSide || n / rows[i] > kMostSide) return SPLC_EINVAL;
+        const Matrix m{0, (int)rows[i], (int)(n / rows[i]), i, 0};
+        all.push_back(m);
+        (split && wide(m) ? apart : others).push_back(m);
+    }
+    if (apart.empty() || 0.85 * estimated(all, 5, 5, 5) <= estimated(apart, 2, 14, 2) + estimated(others, 5, 5, 5)) {
+        apart.clear();
+        others = std::move(all);
+    }
+    add_batches(apart, split, kSquaresAtOnce, s);
+    s.at_once = s.batches.size();
+    add_batches(others, split, kSquares, s);
     return SPLC_OK;
 }
 
@@ -800,66 +925,53 @@ int place(Batch& b, Count count) {
     return b.groups;
 }
 
-// What a launch of `tiles` tiles takes, in times that a compute unit needs for one of 256 x 256: it holds one of those at a time, or
-// two smaller ones.  MI355X, whole calls with many tiles: 0.9B model, FP16X3, 92.5 ms with tiles of 256, 102 of 128, 142 of 64; 8 of
-// 2048 x 5632, FP16, 4.91, 4.97 and 10.3 ms.  Where tiles of 32 x 32 all run at once (one on a compute unit for FP16X3, two for FP16),
-// latency counts, and those are shortest: one of 512 x 512, FP16X3, 126 instead of 163 us with tiles of 64; of 768 x 768, which has
-// more of them, 217 instead of 201.
-enum { LARGE, MIDDLE, SMALL };
-int tile_of(int64_t large, int64_t middle, int64_t small, bool split) {
-    auto rounds = [](int64_t tiles, int64_t at_once) { return (double)((tiles + at_once - 1) / at_once); };
-    const double cost[] = {rounds(large, 256), 0.575 * rounds(middle, 512), (split ? 0.2 : 0.27) * rounds(small, 512)};
-    return (int)(std::min_element(cost, cost + 3) - cost);
-}
-
 // One product of every matrix of the batch.
 template <bool SPLIT, int STEP>
-void product(Batch& b, Factors f, const Result& result, int odd, const float* grad_scale, _Float16* ws, hipStream_t st) {
+void product(Batch& b, const Product& f, const Result& result, int odd, const float* grad_scale, _Float16* ws, hipStream_t st) {
     using Large = Shape<2, 4, 1, 2, 64, SPLIT ? 32 : 64, 2, SPLIT>;
     using Middle = Shape<2, 2, 1, 1, 64, SPLIT ? 32 : 64, 2, SPLIT>;
     using Small = Shape<1, 1, 4, 1, 64, 64, 4, SPLIT>;
     using Tiny = Shape<1, 1, 4, 1, 32, 64, 8, SPLIT>;
     auto launch = [&](auto shape) {
         using S = decltype(shape);
-        const int groups = place(b, STEP == GRAM || STEP == POLYNOMIAL ? S::triangle : S::tiles);
+        const int groups = place(b, STEP == GRAM || STEP == SQUARE ? S::triangle : S::tiles);
         hipLaunchKernelGGL((product_kernel<S, STEP>), dim3((unsigned)(groups + 7) / 8 * 8), dim3(S::kLanes), 0, st, b, f, result, odd,
                            grad_scale, ws);
     };
-    auto count = [&](auto shape) {
-        using S = decltype(shape);
-        return place(b, STEP == GRAM || STEP == POLYNOMIAL ? S::triangle : S::tiles);
-    };
-    if (count(Tiny()) <= (SPLIT ? 256 : 512)) return launch(Tiny());
-    switch (tile_of(count(Large()), count(Middle()), count(Small()), SPLIT)) {
+    switch (tile_of(b.of, b.count, STEP == GRAM || STEP == SQUARE, STEP == GRAM, SPLIT).size) {
         case LARGE: return launch(Large());
         case MIDDLE: return launch(Middle());
-        default: return launch(Small());
+        case SMALL: return launch(Small());
+        default: return launch(Tiny());
     }
 }
 
 template <bool SPLIT>
 void products(Batch& b, const Steps& s, const Result& result, const float* grad_scale, _Float16* ws, hipStream_t st) {
-    for (int k = 0; k < s.count; ++k) {
-        const int odd = k & 1;
-        product<SPLIT, GRAM>(b, s.gram[k], result, odd, grad_scale, ws, st);
-        product<SPLIT, POLYNOMIAL>(b, s.polynomial[k], result, odd, grad_scale, ws, st);
-        if (k + 1 < s.count) product<SPLIT, APPLY>(b, s.apply[k], result, odd, grad_scale, ws, st);
-        else product<SPLIT, LAST>(b, s.apply[k], result, odd, grad_scale, ws, st);
+    int odd = 0;
+    for (const Product& f : s.of) switch (f.step) {
+        case GRAM: product<SPLIT, GRAM>(b, f, result, odd, grad_scale, ws, st); break;
+        case SQUARE: product<SPLIT, SQUARE>(b, f, result, odd, grad_scale, ws, st); break;
+        case APPLY: product<SPLIT, APPLY>(b, f, result, odd, grad_scale, ws, st); odd ^= 1; break;
+        default: product<SPLIT, LAST>(b, f, result, odd, grad_scale, ws, st);
     }
 }
 
 template <class From>
-int orthogonalised(Shapes& shape, int matmul, const Steps& steps, const From& from, const float* grad_scale, const double* inverse,
+int orthogonalised(Shapes& shape, int matmul, const Steps (&steps)[2], const From& from, const float* grad_scale, const double* inverse,
                    const Result& result, _Float16* ws, hipStream_t st) {
-    for (Batch& b : shape.batches) {
+    for (size_t i = 0; i < shape.batches.size(); ++i) {
+        Batch& b = shape.batches[i];
+        const Steps& s = steps[i < shape.at_once];
         const int tiles = place(b, [](const Matrix& m) { return (int64_t)(padded(m.rows) / 64) * (padded(m.cols) / 64); });
-        if (matmul == SPLC_MATMUL_FP16X3) {
-            hipLaunchKernelGGL((scale_kernel<From, true>), dim3((unsigned)tiles), dim3(kThreads), 0, st, b, from, grad_scale, inverse, steps.first, ws);
-            products<true>(b, steps, result, grad_scale, ws, st);
-        } else {
-            hipLaunchKernelGGL((scale_kernel<From, false>), dim3((unsigned)tiles), dim3(kThreads), 0, st, b, from, grad_scale, inverse, steps.first, ws);
-            products<false>(b, steps, result, grad_scale, ws, st);
-        }
+        auto launch = [&](auto split) {
+            constexpr bool SPLIT = decltype(split)::value;
+            hipLaunchKernelGGL((scale_kernel<From, SPLIT>), dim3((unsigned)tiles), dim3(kThreads), 0, st, b, from, grad_scale, inverse, s.first,
+                               ws);
+            products<SPLIT>(b, s, result, grad_scale, ws, st);
+        };
+        if (matmul == SPLC_MATMUL_FP16X3) launch(std::true_type());
+        else launch(std::false_type());
     }
     return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
 }
@@ -879,10 +991,10 @@ Space space(void* ws, const Shapes& s) {
 }
 
 int check_ws(const sparseloco_plan* plan, const int64_t* rows, const double* coefficients, int steps, double eps, int matmul, void* ws,
-             int64_t bytes, Shapes& shape, Steps& s) {
+             int64_t bytes, Shapes& shape, Steps (&s)[2]) {
     const int rc = shapes(plan, rows, matmul, shape);
     if (rc != SPLC_OK) return rc;
-    if (!ranges(coefficients, steps, s) || !finite64(eps) || eps < 0.0 || !ws || bytes < ws_bytes(shape, plan->n_tensors)) return SPLC_EINVAL;
+    if (!steps_of(coefficients, steps, false, s[0]) || (shape.at_once > 0 && !steps_of(coefficients, steps, true, s[1])) || !finite64(eps) || eps < 0.0 || !ws || bytes < ws_bytes(shape, plan->n_tensors)) return SPLC_EINVAL;
     return aligned(ws, 128) ? SPLC_OK : SPLC_EALIGN;
 }
 
@@ -906,7 +1018,7 @@ int sparseloco_orthogonalize(const sparseloco_plan* plan, const int64_t* rows, c
     try {
         if (!plan || !x || !out || replica < 0) return SPLC_EINVAL;
         Shapes shape;
-        Steps s;
+        Steps s[2];
         int rc = check_ws(plan, rows, coefficients, steps, eps, matmul, ws, bytes, shape, s);
         if (rc != SPLC_OK) return rc;
         for (const sparseloco_tensors* t : {x, out}) {
@@ -942,7 +1054,7 @@ int sparseloco_muon_step(const sparseloco_plan* plan, const int64_t* rows, const
         if (!(how->momentum >= 0.0 && how->momentum < 1.0) || !finite((float)(how->lr * how->weight_decay))) return SPLC_EINVAL;
         if (how->adjust != SPLC_MUON_NONE && how->adjust != SPLC_MUON_ASPECT && how->adjust != SPLC_MUON_RMS) return SPLC_EINVAL;
         Shapes shape;
-        Steps s;
+        Steps s[2];
         int rc = check_ws(plan, rows, how->coefficients, how->steps, how->eps, how->matmul, ws, bytes, shape, s);
         if (rc != SPLC_OK) return rc;
         for (const sparseloco_tensors* t : {theta, m, grads, theta_bf16}) {

@@ -54,9 +54,9 @@ def tolerance(m, u, coefficients=USUAL, eps=1e-7):
     return total
 
 
-def agree(got, m, u, want=None, **how):
+def agree(got, m, u, want=None, limit=None, **how):
     want = plain(m, **how) if want is None else want
-    limit = tolerance(m, u, **how)
+    limit = tolerance(m, u, **how) if limit is None else limit
     half = torch.finfo(got.dtype).eps / 2
     off = got.double() - want
     assert bool(torch.isfinite(off).all())
@@ -66,6 +66,44 @@ def agree(got, m, u, want=None, **how):
         lines = off.norm(dim=k)
         share = 8 * limit / math.sqrt(len(lines)) + half * want.norm(dim=k)
         assert bool((lines <= share).all()), (k, int((lines - share).argmax()), float((lines / share).max()))
+
+
+def in_squares(m, u, coefficients=USUAL, eps=1e-7):
+    """The error to expect where up to three steps at a time are taken in squares (A = X X^T; for each step B = b A + c A^2, Q = p Q, A = p A p
+    with p = a + B; X = Q X; the product of the a's at most 64): of these formulas in 64 bits with every result off by independent
+    relative errors of rms 0.41 u, as rounding it to hi + lo makes, and by what fp32 sums add."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    add = 2.0 ** -24 * math.sqrt(3 * max(m.shape) / 16)
+
+    def off(t, sums=None):
+        noise = torch.randn(t.shape, generator=gen, device="cuda", dtype=torch.float64) * 0.41 * u * t.abs()
+        if sums is not None:                                 # rms of the terms' sum
+            noise = noise + torch.randn(t.shape, generator=gen, device="cuda", dtype=torch.float64) * add * sums
+        return t + noise
+
+    def times(x, y, own=0.0, old=0.0):
+        z = x @ y
+        return off(own * old + z, (x.square() @ y.square()).sqrt())
+    x = m.double()
+    x = x.T if x.shape[0] > x.shape[1] else x
+    x = off(x / (x.square().sum().sqrt() + eps))
+    k = 0
+    while k < len(coefficients):
+        count, alpha = 1, coefficients[k][0]
+        while count < 3 and k + count < len(coefficients) and abs(alpha * coefficients[k + count][0]) <= 64:
+            alpha *= coefficients[k + count][0]
+            count += 1
+        g, q, of_one = times(x, x.T), None, 1.0
+        for a, b, c in coefficients[k:k + count]:
+            p = times(c * g, g, b, g)
+            q = p if q is None else times(p, q, 1.0, a * q + of_one * p)
+            of_one *= a
+            t = times(p, g, a, g)
+            g = times(p, t, a, t)
+        x = times(q, x, of_one, x)
+        k += count
+    want = plain(m, coefficients, eps)
+    return float(((x.T if m.shape[0] > m.shape[1] else x) - want).norm())
 
 
 def matrix(rows, cols, kind, seed, dtype=torch.float32):
@@ -134,6 +172,23 @@ def test_other_polynomials(mode):
               [(1.0, 0.0, 0.0)], [(20.0, 3.0, 0.0), (0.05, -0.001, 0.0)], [(0.001, 0.0, 0.5)]):
         B.sparseloco_orthogonalize(plan, [x], [out], ws, coefficients=c, matmul=matmul)
         agree(out, x, u, coefficients=c)
+
+
+@pytest.mark.parametrize("kind", ["noise", "strong"])
+def test_steps_taken_in_squares(kind):
+    """Matrices of 512 rows or more that are half as wide again, wide and tall, beside others in one call; single steps, pairs, triples."""
+    matmul, u = MODES["fp16x3"]
+    shapes = [(512, 768), (700, 600), (520, 1600), (1700, 513), (65, 64), (513, 1025)]
+    x = packed([matrix(r, c, kind, 60 + i) for i, (r, c) in enumerate(shapes)])
+    plan = B.Plan(shapes, 32)
+    ws = B.orthogonalize_workspace(plan, matmul=matmul)
+    for c in (USUAL, USUAL[:1], USUAL[:4], [(1.5, -0.5, 0.0)] * 8, [(8.2, -23.5, 17.3), (4.1, -2.95, 0.545), (1.875, -1.25, 0.375)],
+              [(70.0, -50.0, 0.0), (0.02, 0.0, 0.0)]):
+        out = packed([torch.full_like(t, float("nan")) for t in x])
+        B.sparseloco_orthogonalize(plan, bound(plan, x), bound(plan, out), ws.fill_(255), coefficients=c, matmul=matmul)
+        for t, o in zip(x, out):
+            wide = min(t.shape) >= 512 and 2 * max(t.shape) >= 3 * min(t.shape)
+            agree(o, t, u, limit=in_squares(t, u, c) if wide else None, coefficients=c)
 
 
 @pytest.mark.parametrize("mode", MODES)
