@@ -999,8 +999,8 @@ def _check_ws(ws):
 
 
 def orthogonalize_workspace(plan: Plan, *, matmul: int = SPLC_MATMUL_FP16X3, device="cuda") -> torch.Tensor:
-    """The workspace of sparseloco_orthogonalize and sparseloco_muon_step: up to 20 bytes an element of the 134 million or more that
-    are worked on at once."""
+    """The workspace of sparseloco_orthogonalize and sparseloco_muon_step: 8 to 20 bytes an element of what is worked on at once, up to 16
+    GiB, but one matrix at the least.  A matrix takes as much as one whose sides are the next odd multiples of 64."""
     n = int(lib().sparseloco_orthogonalize_ws_bytes(plan.handle, plan.rows, _integer(matmul, 32, "sparseloco_orthogonalize_ws_bytes")))
     if n < 0:
         raise SparseLoCoError(n, "sparseloco_orthogonalize_ws_bytes")

@@ -30,7 +30,7 @@ using namespace splc;
 constexpr int kThreads = 256;
 constexpr int kPad = 64;                                     // row lengths of the operands are multiples of it, zeros behind the end
 constexpr int kMostMatrices = 128;                           // of a batch: their descriptions are kernel arguments
-constexpr int64_t kBatchElements = (int64_t)1 << 30;         // of a batch, but one matrix at the least
+constexpr int64_t kBatchElements = (int64_t)1 << 33;         // fp16 numbers of a batch's operands (16 GiB), but one matrix at the least
 constexpr int kMostSide = 1 << 22;                           // rows and columns: offsets inside a tile's rows stay in 32 bits
 constexpr int kMostSteps = SPLC_MAX_ORTHO_STEPS;
 
@@ -872,19 +872,19 @@ int64_t ws_bytes(const Shapes& s, int tensors) { return 2 * s.planes + 8 * (s.ch
 // Batches of like size; the longest products first, so that those that are left at the end of a launch are short ones.
 void add_batches(std::vector<Matrix>& all, bool split, int squares, Shapes& s) {
     std::stable_sort(all.begin(), all.end(), [](const Matrix& x, const Matrix& y) { return std::max(x.rows, x.cols) > std::max(y.rows, y.cols); });
-    int64_t total = 0, elements = 0, at = 0;
-    for (const Matrix& m : all) total += (int64_t)m.rows * m.cols;
+    auto size = [&](const Matrix& m) { return split ? Planes<true>::elements(m, squares) : Planes<false>::elements(m, squares); };
+    int64_t total = 0, at = 0;
+    for (const Matrix& m : all) total += size(m);
     const int64_t each = total / std::max<int64_t>(1, (total + kBatchElements - 1) / kBatchElements);
     for (const Matrix& m : all) {
-        if (&m == all.data() || s.batches.back().count == kMostMatrices || elements >= each) {
+        if (&m == all.data() || s.batches.back().count == kMostMatrices || at >= each) {
             s.batches.push_back(Batch{0, 0, {}});
-            elements = at = 0;
+            at = 0;
         }
         Batch& b = s.batches.back();
         b.of[b.count] = m;
         b.of[b.count++].at = at;
-        at += split ? Planes<true>::elements(m, squares) : Planes<false>::elements(m, squares);
-        elements += (int64_t)m.rows * m.cols;
+        at += size(m);
         s.planes = std::max(s.planes, at);
     }
 }

@@ -192,6 +192,23 @@ def test_steps_taken_in_squares(kind):
 
 
 @pytest.mark.parametrize("mode", MODES)
+def test_enough_matrices_for_the_largest_tiles(mode):
+    """Ragged ones, square and tall, so many that products are cut into tiles of 256 and 128."""
+    matmul, u = MODES[mode]
+    shapes = [(1270, 1270)] * 24 + [(2601, 1270)] * 12
+    x = packed([matrix(r, c, "strong", 80 + i) for i, (r, c) in enumerate(shapes)])
+    out = packed([torch.full_like(t, float("nan")) for t in x])
+    plan = B.Plan(shapes, 32)
+    B.sparseloco_orthogonalize(plan, bound(plan, x), bound(plan, out), B.orthogonalize_workspace(plan, matmul=matmul).fill_(255), matmul=matmul)
+    for i in (0, 23, 35):
+        limit = tolerance(x[i], u)
+        agree(out[i], x[i], u, limit=max(limit, in_squares(x[i], u)) if mode == "fp16x3" and i == 35 else limit)
+    for i, t in enumerate(out):
+        o = t.double() if i < 24 else t.T.double()           # O O^T has the squares of the result's singular values, 0.68^2 to 1.21^2
+        assert float((o @ o.T).diagonal().sqrt().max()) < 1.22 and bool(torch.isfinite(o).all())
+
+
+@pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("scale", [1e-30, 1.0, 1e30])
 def test_matrices_whose_result_is_known(mode, scale):
     """c Q with Q's rows orthonormal becomes p(...p(1 / sqrt(n))) Q: permutations and a Hadamard matrix."""
