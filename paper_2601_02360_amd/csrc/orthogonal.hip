@@ -123,6 +123,16 @@ __device__ __forceinline__ void split(float x, _Float16& hi, _Float16& lo) {
 
 // ---------------------------------------------------------------- what is orthogonalised
 
+// Four consecutive elements from `at` on of a run that has n of them, +0 behind its end.
+template <class T>
+__device__ __forceinline__ float4 four(const T* p, uint32_t at, uint32_t n) {
+    if (at + 4 <= n) return widened(cached_load4(p + at));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (at < n) v.x = widened(p[at]);
+    if (at + 1 < n) v.y = widened(p[at + 1]);
+    if (at + 2 < n) v.z = widened(p[at + 2]);
+    return v;
+}
 struct Momentum {
     float beta, rest;
     int nesterov;
@@ -131,16 +141,17 @@ struct Momentum {
 template <class T>
 struct Plain {
     const T* const* x;
-    __device__ __forceinline__ float operator()(int tensor, int64_t at, float) const { return widened(x[tensor][at]); }
+    __device__ __forceinline__ float4 operator()(int tensor, int64_t at, uint32_t n, float) const { return four(x[tensor] + at, 0, n); }
 };
 template <class G>
 struct Update {
     const G* const* grad;
     float* const* m;                                         // the new momentum
     Momentum how;
-    __device__ __forceinline__ float operator()(int tensor, int64_t at, float factor) const {
-        const float moment = m[tensor][at];
-        return how.nesterov ? fmaf(how.beta, moment, how.rest * (factor * widened(grad[tensor][at]))) : moment;
+    __device__ __forceinline__ float one(float moment, float g) const { return how.nesterov ? fmaf(how.beta, moment, how.rest * g) : moment; }
+    __device__ __forceinline__ float4 operator()(int tensor, int64_t at, uint32_t n, float factor) const {
+        const float4 moment = four(m[tensor] + at, 0, n), g = four(grad[tensor] + at, 0, n);
+        return make_float4(one(moment.x, factor * g.x), one(moment.y, factor * g.y), one(moment.z, factor * g.z), one(moment.w, factor * g.w));
     }
 };
 
@@ -158,16 +169,6 @@ __device__ __forceinline__ double group_sum(double x, double* shared) {
     return x;
 }
 
-// Four consecutive elements from `at` on of a chunk that has n of them, +0 behind its end.
-template <class T>
-__device__ __forceinline__ float4 four(const T* p, uint32_t at, uint32_t n) {
-    if (at + 4 <= n) return widened(cached_load4(p + at));
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (at < n) v.x = widened(p[at]);
-    if (at + 1 < n) v.y = widened(p[at + 1]);
-    if (at + 2 < n) v.z = widened(p[at + 2]);
-    return v;
-}
 __device__ __forceinline__ double squares(float4 v, double sum) {
     sum = fma((double)v.x, (double)v.x, sum);
     sum = fma((double)v.y, (double)v.y, sum);
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void momentum_kernel(const ChunkDesc* __r
         auto one = [&](float& moment, float gradient) {
             gradient *= factor;
             moment = fmaf(how.rest, gradient, how.beta * moment);
-            return how.nesterov ? fmaf(how.beta, moment, how.rest * gradient) : moment;
+            return update.one(moment, gradient);
         };
         float4 u;
         u.x = one(x[s].x, g[s].x);
@@ -266,35 +267,52 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Batch, From from, const
     const Matrix m = matrix_of(batch_argument(), (int)blockIdx.x, place);
     const Planes<SPLIT> planes(ws, m);
     const int across = padded(m.cols) / 64, r0 = place / across * 64, c0 = place % across * 64;
-    const int ldc = stride(m.cols), ldr = stride(m.rows), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int ldc = stride(m.cols), ldr = stride(m.rows), line = threadIdx.x / 16, four_of = threadIdx.x % 16 * 4;
     const double scale = inverse[m.tensor] * (double)range;
-    constexpr int kEach = 64 / (kThreads / 64);
-    float x[kEach];
+    constexpr int kEach = 4, kLines = kThreads / 16;         // rows of a lane, four columns of each; then columns, four rows of each
+    float4 x[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        const int r = r0 + wave * kEach + i, c = c0 + lane;
-        x[i] = r < m.rows && c < m.cols ? from(m.tensor, (int64_t)r * m.cols + c, factor) : 0.f;
+        const int r = r0 + line + i * kLines, c = c0 + four_of;
+        x[i] = r < m.rows && c < m.cols ? from(m.tensor, (int64_t)r * m.cols + c, (uint32_t)(m.cols - c < 4 ? m.cols - c : 4), factor)
+                                        : make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    auto split4 = [](const float* v, half4& hi, half4& lo) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            _Float16 h, l;
+            split(v[e], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+    };
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        const int r = r0 + wave * kEach + i, c = c0 + lane;
-        const float scaled = (float)((double)x[i] * scale);
-        tile[wave * kEach + i][lane] = scaled;
-        if (r < m.rows) {
-            _Float16* p = planes.r(0) + planes.place(r, c, ldc);
-            split(scaled, p[0], p[planes.r_lo(m)]);
-        }
+        const int r = r0 + line + i * kLines, c = c0 + four_of;
+        const float v[4] = {(float)((double)x[i].x * scale), (float)((double)x[i].y * scale), (float)((double)x[i].z * scale),
+                            (float)((double)x[i].w * scale)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tile[line + i * kLines][four_of + e] = v[e];
+        if (r >= m.rows) continue;
+        half4 hi, lo;
+        split4(v, hi, lo);
+        _Float16* p = planes.r(0) + planes.place(r, c, ldc);
+        *(half4*)p = hi;
+        *(half4*)(p + planes.r_lo(m)) = lo;
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        const int c = c0 + wave * kEach + i, r = r0 + lane;
+        const int c = c0 + line + i * kLines, r = r0 + four_of;
         if (c >= m.cols) break;
-        _Float16 hi, lo;
-        split(tile[lane][wave * kEach + i], hi, lo);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = tile[four_of + e][line + i * kLines];
+        half4 hi, lo;
+        split4(v, hi, lo);
         _Float16* p = planes.t(0) + planes.place(c, r, ldr);
-        p[0] = hi;
-        if (SPLIT) p[32] = lo;
+        *(half4*)p = hi;
+        if (SPLIT) *(half4*)(p + 32) = lo;
     }
 }
 
