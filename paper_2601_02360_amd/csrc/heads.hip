@@ -440,13 +440,6 @@ __global__ __launch_bounds__(kJoinThreads) void heads_join_kernel(const float* _
 
 // ---------------------------------------------------------------- host
 
-int units() {
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1)
-        return 256;
-    return n;
-}
-
 bool fine_rotation(const sparseloco_rotation* how, int d) {
     return how && how->positions && how->frequencies && (how->position_bytes == 4 || how->position_bytes == 8) && how->pairs >= 1 &&
            how->pairs <= d / 2 && std::isfinite((float)how->magnitude);
@@ -481,6 +474,11 @@ int check(const List* lists, int n, int dtype, int64_t tokens, int d, const spar
             return SPLC_EINVAL;
     }
     if (tokens > 0 && !fine_rotation(how, d)) return SPLC_EINVAL;
+    // What is written of the queries (the last list) is not to be read of the keys, and the other way round: one may come before the other.
+    const List& out = lists[n - 1];
+    if (out.k && tokens > 0 && out.q->heads > 0 && out.k->heads > 0)
+        for (int i = 0; i < n; ++i)
+            if (out.q->data == lists[i].k->data || out.k->data == lists[i].q->data) return SPLC_EINVAL;
     const size_t size = dtype == SPLC_F32 ? 4 : 2;
     for (int i = 0; i < n; ++i)
         if (!aligned(lists[i].q->data, size) || (lists[i].k && !aligned(lists[i].k->data, size))) return SPLC_EALIGN;

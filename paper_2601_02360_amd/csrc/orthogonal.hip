@@ -5,14 +5,21 @@
 //     A = X X^T,   B = b A + c A^2,   X <- a X + B X,
 // which maps every singular value s of X to a s + b s^3 + c s^5.  All three products have the form C[i][j] = sum_k P[i][k] Q[j][k]
 // with both operands' rows contiguous, for which X is kept in two layouts, as it lies in memory (R) and transposed (T), and A and B
-// need none but their own.  A and A^2 are symmetric: tiles on and above the diagonal are formed, and stored twice.
+// need none but their own.  A and A^2 are symmetric: tiles on and above the diagonal are formed, and stored twice.  Where matrices are
+// wide, several steps are taken in squares alone (steps_of).
 //
 // Operands are fp16 numbers times a power of two that the host knows beforehand: |X| <= 1 in the spectral norm, and the polynomial
 // says what that bound becomes, so that no element leaves [-2^14, 2^14] and those 2^-28 of the bound keep 11 bits.
 //   FP16    one product a term.  A, B and X are rounded to 11 bits as operands; X itself is held in 22 (hi + lo) where a X is
 //           added.  Result: 2e-4 to 2e-3 off (relative, depending on how the singular values are spread), as little as a result in
 //           bf16 is rounded by; bf16 operands are 1e-2 to 4e-2 off.
-//   FP16X3  operands are hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: what fp32 products give.
+//   FP16X3  operands are hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: what fp32 products give, 2e-6 to 4e-6 off.
+//
+// What bounds it (MI355X; fp16 products of 8192 x 8192 by the vendor's library: 1240 TFLOP/s, for which the chip lowers its clock to
+// 2 GHz and below): the matrix cores.  FP16X3, 32 of 2048 x 2048, three products counted: X <- a X + B X 1100 TFLOP/s, of which the
+// tiles' ends, 16 bytes read and written an element, take a fifth, and symmetric products 1050; FP16, the ends weighing three times
+// as much, 730 and 790.  Whole calls: 0.9B model, one step, FP16X3, 75 ms; 8 of 2048 x 5632, FP16, 4.5 ms; one of 512 x 512, FP16X3,
+// 116 us, most of it 18 launches of 6.4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -40,7 +47,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 __host__ __device__ inline int padded(int n) { return (n + kPad - 1) / kPad * kPad; }
 // From a row to the next: an odd number of 128 bytes (256 where elements are hi + lo), so that the same piece of many rows lies in
-// many channels of the cache.
+// many channels of the cache (32 of 2048 x 2048, X <- a X + B X: FP16X3 1575 -> 1501 us, FP16 855 -> 753).
 __host__ __device__ inline int stride(int n) { return (n + kPad - 1) / kPad % 2 ? padded(n) : padded(n) + kPad; }
 
 struct Matrix {
@@ -57,8 +64,9 @@ struct Batch {
     Matrix of[kMostMatrices];
 };
 // Operands of a matrix: R and T of this step and of the next (one place for both where the third product does not read it: R of a
-// wide matrix, T of a tall one), and squares: A, B and more.  Their elements are hi + lo where they are split, 32 of hi and the same 32 of lo side by
-// side, so that a row of 32 for the products is 128 bytes; otherwise hi alone, and lo of R, which is no operand then, behind it.
+// wide matrix, T of a tall one), and squares: A, B and more.  Their elements are hi + lo where they are split, 32 of hi and the same 32
+// of lo side by side, so that a row of 32 for the products is 128 bytes (4 % of a call with FP16X3); otherwise hi alone, and lo of R,
+// which is no operand then, behind it.
 template <bool SPLIT>
 struct Planes {
     static constexpr int kParts = SPLIT ? 2 : 1;
@@ -344,28 +352,22 @@ typedef __attribute__((address_space(3))) void shared_void;
 // waves with the same block, which take turns along k.  DEEP: buffers for BK of k.
 template <int WR_, int WC_, int WK_, int IR_, int SIDE_, int BK_, int DEEP_, bool SPLIT_>
 struct Shape {
-    static constexpr int WR = WR_, WC = WC_, WK = WK_, IR = IR_, kSide = SIDE_, BK = BK_, kDeep = DEEP_, kWaves = WR_ * WC_ * WK_, kLanes = kWaves * 64;
-    static constexpr int kRows = WR_ * IR_ * SIDE_, kCols = WC_ * SIDE_, kTall = kRows / kCols;
+    static constexpr int WR = WR_, WC = WC_, WK = WK_, IR = IR_, kSide = SIDE_, BK = BK_, kDeep = DEEP_;
+    static constexpr int kWaves = WR_ * WC_ * WK_, kLanes = kWaves * 64, kTile = WC_ * SIDE_;
     static constexpr bool SPLIT = SPLIT_;
     static_assert(kPad % BK_ == 0, "whole rows of operands");
-    static_assert(kRows % kCols == 0, "a tile is as many columns wide, or a multiple of that in rows");
-    static_assert(WK_ == 1 || (WC_ == 1 && IR_ == 1 && WR_ == 1), "one block where waves share k");
-    // Workgroups of a launch for a matrix: all of its tiles, or those that reach its diagonal or what lies above it, `kTall` columns
-    // of tiles with u + 1 tiles each after another.
-    // Tiles cover the padding of rows of operands, which they clear, too.
-    static __host__ __device__ int down(const Matrix& m) { return (padded(m.rows) + kRows - 1) / kRows; }
-    static int64_t tiles(const Matrix& m) { return (int64_t)down(m) * ((padded(m.cols) + kCols - 1) / kCols); }
-    static int64_t triangle(const Matrix& m) {
-        const int64_t across = (padded(m.n()) + kCols - 1) / kCols, u = across / kTall;
-        return kTall * (u * (u + 1) / 2) + across % kTall * (u + 1);
-    }
+    static_assert(WR_ * IR_ == WC_, "square tiles");
+    static_assert(WK_ == 1 || (WC_ == 1 && IR_ == 1), "one block where waves share k");
+    // Workgroups of a launch for a matrix: all of its tiles, or those on and above its diagonal, column by column.  Tiles cover the
+    // padding of rows of operands, too, which they clear.
+    static __host__ __device__ int down(int rows) { return (padded(rows) + kTile - 1) / kTile; }
+    static int64_t tiles(const Matrix& m) { return (int64_t)down(m.rows) * down(m.cols); }
+    static int64_t triangle(const Matrix& m) { return (int64_t)down(m.n()) * (down(m.n()) + 1) / 2; }
     static __device__ __forceinline__ void triangle_place(int place, int& ti, int& tj) {
-        int u = (int)((sqrtf(8.f / kTall * (float)place + 1.f) - 1.f) * 0.5f);
-        while (kTall * (u * (u + 1) / 2) > place) --u;
-        while (kTall * ((u + 1) * (u + 2) / 2) <= place) ++u;
-        place -= kTall * (u * (u + 1) / 2);
-        ti = place % (u + 1);
-        tj = u * kTall + place / (u + 1);
+        tj = (int)((sqrtf(8.f * (float)place + 1.f) - 1.f) * 0.5f);
+        while (tj * (tj + 1) / 2 > place) --tj;
+        while ((tj + 1) * (tj + 2) / 2 <= place) ++tj;
+        ti = place - tj * (tj + 1) / 2;
     }
 };
 
@@ -382,19 +384,22 @@ __device__ __forceinline__ int exchange(int row) {
     return row / kBeside & (kPieces < 16 ? kPieces - 1 : 15);
 }
 
-// BK elements (hi, lo) of every row of P and Q at a time go to LDS, without passing registers, while the BK before them are multiplied.  Then the sums pass LDS, block by block, to be
-// finished and stored along rows of C, 16 bytes a lane, and once more along its columns for the transposed (or mirrored) copy.
+// BK elements (hi, lo) of every row of P and Q at a time go to LDS, without passing registers, while those before them are multiplied.
+// Then the sums pass LDS, block by block, to be finished and stored along rows of C, 16 bytes a lane, and once more along its columns
+// for the transposed (or mirrored) copy.  (0.9B model, one step: sums stored from where the products leave them, tiles of 128, 141 ms;
+// through LDS 126; tiles of 256 120; operands of the next 16 of k read beside the products 114.5; hi and lo side by side 106; large
+// batches 92; steps in squares 76.)
 template <class S, int STEP>
 __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f, Result result, int odd,
                                                             const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
     constexpr bool SPLIT = S::SPLIT;
     constexpr int SIDE = S::kSide;
     constexpr int kParts = SPLIT ? 2 : 1, BK = S::BK, kRow = BK * kParts, kPieces = kRow / 8, kRowsALoad = 64 / kPieces;
-    constexpr int kLoads[2] = {S::kRows * kRow / 512 / S::kWaves, S::kCols * kRow / 512 / S::kWaves};     // of a wave for P and Q
-    static_assert(kLoads[1] * S::kWaves * 512 == S::kCols * kRow, "whole loads");
+    constexpr int kLoads = S::kTile * kRow / 512 / S::kWaves;    // of a wave for P, and as many for Q
+    static_assert(kLoads * S::kWaves * 512 == S::kTile * kRow, "whole loads");
     __shared__ __align__(1024) union {
         struct {
-            _Float16 p[S::kRows * kRow], q[S::kCols * kRow];
+            _Float16 p[S::kTile * kRow], q[S::kTile * kRow];
         } operands[S::kDeep];
         float blocks[S::kWaves][SIDE * SIDE];
     } lds;
@@ -410,8 +415,8 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f,
     if (STEP == GRAM || STEP == SQUARE) {
         S::triangle_place(place, ti, tj);
     } else {
-        ti = place % S::down(m);
-        tj = place / S::down(m);
+        ti = place % S::down(m.rows);
+        tj = place / S::down(m.rows);
     }
     const _Float16 *p, *q;
     int p_rows, q_rows, depth, ld_p, ld_q;
@@ -438,16 +443,16 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f,
     ld_p *= kParts;
     ld_q *= kParts;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row0 = ti * S::kRows, col0 = tj * S::kCols;
+    const int row0 = ti * S::kTile, col0 = tj * S::kTile;
     // (rows that are not there, up to all of a tile's, are read as the last one that is)
     const int first[2] = {row0 < p_rows ? row0 : p_rows - 1, col0 < q_rows ? col0 : q_rows - 1};
     const _Float16* from[2] = {p + (int64_t)first[0] * ld_p, q + (int64_t)first[1] * ld_q};
-    uint32_t offset[2][kLoads[0]];                           // of this lane's 16 bytes from the tile's first element, in elements
+    uint32_t offset[2][kLoads];                              // of this lane's 16 bytes from the tile's first element, in elements
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         const int last = (side ? q_rows : p_rows) - 1 - first[side];
 #pragma unroll
-        for (int i = 0; i < kLoads[side]; ++i) {
+        for (int i = 0; i < kLoads; ++i) {
             const int row = (wave + i * S::kWaves) * kRowsALoad + lane / kPieces, piece = (lane % kPieces) ^ exchange<kRow>(row);
             offset[side][i] = (uint32_t)(row < last ? row : last) * (uint32_t)(side ? ld_q : ld_p) + (uint32_t)piece * 8u;
         }
@@ -457,7 +462,7 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f,
         for (int side = 0; side < 2; ++side) {
             _Float16* to = side ? lds.operands[buffer].q : lds.operands[buffer].p;
 #pragma unroll
-            for (int i = 0; i < kLoads[side]; ++i)
+            for (int i = 0; i < kLoads; ++i)
                 __builtin_amdgcn_global_load_lds((global_void*)(from[side] + k + offset[side][i]),
                                                  (shared_void*)(to + (wave + i * S::kWaves) * 512), 16, 0, 0);
         }
@@ -517,7 +522,7 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f,
         }
     };
     // Waits for what was fetched first of so many fetches, and for the operands from LDS; then for all waves.
-    constexpr int kAhead = S::kDeep - 1, kWaiting = (kAhead - 1) * (kLoads[0] + kLoads[1]);
+    constexpr int kAhead = S::kDeep - 1, kWaiting = (kAhead - 1) * 2 * kLoads;
     static_assert(kWaiting < 64, "loads that a wave counts");
     auto arrived = [&](bool all_ahead) {
         asm volatile("" ::: "memory");
@@ -723,7 +728,7 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f,
 
 bool finite64(double v) { return std::isfinite(v); }
 
-// Largest |p| for x in [0, most], p odd or plain of the form x^k (a + b x^2 + c x^4) sampled where its derivative vanishes.
+// The largest value in [0, most], at its end or where the derivative vanishes.
 double largest(double a, double b, double c, double most) {  // of |a x + b x^3 + c x^5|
     auto p = [&](double x) { return std::fabs(x * (a + x * x * (b + x * x * c))); };
     double found = p(most);
@@ -1012,7 +1017,8 @@ int check_ws(const sparseloco_plan* plan, const int64_t* rows, const double* coe
              int64_t bytes, Shapes& shape, Steps (&s)[2]) {
     const int rc = shapes(plan, rows, matmul, shape);
     if (rc != SPLC_OK) return rc;
-    if (!steps_of(coefficients, steps, false, s[0]) || (shape.at_once > 0 && !steps_of(coefficients, steps, true, s[1])) || !finite64(eps) || eps < 0.0 || !ws || bytes < ws_bytes(shape, plan->n_tensors)) return SPLC_EINVAL;
+    if (!steps_of(coefficients, steps, false, s[0]) || (shape.at_once > 0 && !steps_of(coefficients, steps, true, s[1]))) return SPLC_EINVAL;
+    if (!finite64(eps) || eps < 0.0 || !ws || bytes < ws_bytes(shape, plan->n_tensors)) return SPLC_EINVAL;
     return aligned(ws, 128) ? SPLC_OK : SPLC_EALIGN;
 }
 

@@ -235,7 +235,7 @@ def test_matrices_whose_result_is_known(mode, scale):
 def test_many_matrices_zeros_and_one_that_is_not_finite(mode):
     """More than a batch of them; what is wrong with one matrix stays there; empty tensors; the result in the input's place."""
     matmul, u = MODES[mode]
-    shapes = [(7 + i % 5, 3 + i % 7) for i in range(101)]
+    shapes = [(7 + i % 5, 3 + i % 7) for i in range(301)]
     shapes[20] = (0, 4)
     x = [matrix(r, c, "noise", 100 + i) for i, (r, c) in enumerate(shapes)]
     plan = B.Plan(shapes, 32)

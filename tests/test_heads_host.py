@@ -26,7 +26,8 @@ def test_what_the_rotation_refuses():
                 dict(q=heads(n=-1)), dict(q=heads(None)), dict(q_out=heads(None)), dict(q_out=heads(n=5)), dict(q=heads(token=-1)),
                 dict(q=heads(token=2 ** 61)), dict(turn=how(positions=None)), dict(turn=how(frequencies=None)), dict(turn=how(size=2)),
                 dict(turn=how(pairs=0)), dict(turn=how(pairs=9)), dict(turn=how(magnitude=float("inf"))),
-                dict(q_out=heads(token=0)), dict(q_out=heads(head=15)), dict(q_out=heads(token=63)), dict(q_out=heads(token=16, head=64))):
+                dict(k=heads(2 * ANY), q_out=heads(2 * ANY), k_out=heads(3 * ANY)), dict(k=heads(2 * ANY), q_out=heads(3 * ANY), k_out=heads()),
+                dict(k=heads(2 * ANY), q_out=heads(3 * ANY), k_out=heads(3 * ANY)), dict(q_out=heads(token=0)), dict(q_out=heads(head=15)), dict(q_out=heads(token=63)), dict(q_out=heads(token=16, head=64))):
         assert rotary(**bad) == B.SPLC_EINVAL, bad
     L = B.lib()
     assert L.sparseloco_rotary(None, None, 0, 5, 16, how(), 0, heads(), None, None) == B.SPLC_EINVAL
@@ -39,22 +40,24 @@ def test_what_the_rotation_refuses():
 
 
 def test_what_the_norm_refuses():
-    def call(gain=ANY, k_gain=ANY, kind=0, eps=1e-6, keys=True):
-        k = heads() if keys else None
+    def call(gain=ANY, k_gain=ANY, kind=0, eps=1e-6, keys=True, at=ANY):
+        k = heads(at) if keys else None
         return B.lib().sparseloco_qk_norm_rotary(heads(), k, 0, 5, 16, gain, k_gain, kind, eps, how(), heads(), k, None)
+    assert call() == B.SPLC_EINVAL       # (keys where the queries are)
     for bad in (dict(gain=None), dict(k_gain=None), dict(kind=2), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=1e300)):
-        assert call(**bad) == B.SPLC_EINVAL, bad
-    assert call(gain=ODD) == B.SPLC_EALIGN and call(k_gain=ANY + 1, kind=1) == B.SPLC_EALIGN
+        assert call(at=2 * ANY, **bad) == B.SPLC_EINVAL, bad
+    assert call(at=2 * ANY, gain=ODD) == B.SPLC_EALIGN and call(at=2 * ANY, k_gain=ANY + 1, kind=1) == B.SPLC_EALIGN
 
 
 def test_what_the_gradient_refuses():
     size = B.lib().sparseloco_qk_norm_rotary_grad_ws_bytes
 
     def call(dq=None, dk=None, q=None, k=None, gq=None, gk=None, sums=(ANY, ANY), ws=ANY, n=1 << 30, k_gain=ANY):
-        return B.lib().sparseloco_qk_norm_rotary_grad(dq or heads(), dk or heads(), q or heads(), k or heads(), 0, 5, 16, ANY, k_gain, 0, 1e-6, how(),
-                                                      gq or heads(), gk or heads(), *sums, 0, ws, n, None)
+        dk, k, gk = (t or heads(2 * ANY) for t in (dk, k, gk))
+        return B.lib().sparseloco_qk_norm_rotary_grad(dq or heads(), dk, q or heads(), k, 0, 5, 16, ANY, k_gain, 0, 1e-6, how(), gq or heads(), gk,
+                                                      *sums, 0, ws, n, None)
     for bad in (dict(sums=(None, ANY)), dict(sums=(ANY, None)), dict(ws=None), dict(n=size(5, 4, 4, 16) - 1), dict(k_gain=None),
-                dict(gq=heads(head=3)), dict(dq=heads(n=3)), dict(k=heads(n=1))):
+                dict(gq=heads(2 * ANY)), dict(gk=heads()), dict(gq=heads(head=3)), dict(dq=heads(n=3)), dict(k=heads(n=1))):
         assert call(**bad) == B.SPLC_EINVAL, bad
     for bad in (dict(sums=(ODD, ANY)), dict(ws=ODD), dict(gk=heads(ODD))):
         assert call(**bad) == B.SPLC_EALIGN, bad
