@@ -336,78 +336,76 @@ __global__ __launch_bounds__(kThreads, grad_waves_a_simd(V)) void heads_grad_ker
     const Mine mine(in_head, share.per_head, share.d, how.r);
     const int64_t items = share.tokens * share.parts;
     __shared__ __align__(16) float gain[kMostDim];
-    for (int side = 0; side < 2; ++side) {                   // queries, then keys: the sums of one gain take registers at a time
-        const View<const T> in = args.x[side], grad = args.dy[side];
-        const View<T> out = args.dx[side];
-        const int runs = (in.heads + at_once - 1) / at_once;
-        __syncthreads();
-        keep_gain(gain, args.gain[side], args.gain_bf16, share.d);
-        __syncthreads();
-        float dw[C][2 * V];
+    const int side = blockIdx.y;                             // queries or keys: the sums of one gain take registers
+    const View<const T> in = args.x[side], grad = args.dy[side];
+    const View<T> out = args.dx[side];
+    const int runs = (in.heads + at_once - 1) / at_once;
+    keep_gain(gain, args.gain[side], args.gain_bf16, share.d);
+    __syncthreads();
+    float dw[C][2 * V];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
-            for (int j = 0; j < 2 * V; ++j) dw[c][j] = 0.f;
-        }
-        for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
-            const int64_t token = item / share.parts;
-            const int part = (int)(item - token * share.parts);
-            Turn<V, C> turn;
-            for (int run = part; run < runs; run += kAhead * share.parts) {
-                typename Mine::Raw raw_x[kAhead], raw_g[kAhead];
+        for (int j = 0; j < 2 * V; ++j) dw[c][j] = 0.f;
+    }
+    for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
+        const int64_t token = item / share.parts;
+        const int part = (int)(item - token * share.parts);
+        Turn<V, C> turn;
+        for (int run = part; run < runs; run += kAhead * share.parts) {
+            typename Mine::Raw raw_x[kAhead], raw_g[kAhead];
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int head = (run + u * share.parts) * at_once + slot;
-                    if (head >= in.heads) continue;
-                    mine.load(in.at + token * in.token + head * in.head, raw_x[u]);
-                    mine.load(grad.at + token * grad.token + head * grad.head, raw_g[u]);
-                }
-                if (run == part) turn.template at<SIDE>(how, token, lane, in_head, share.per_head, share.d, angles[wave]);
+            for (int u = 0; u < kAhead; ++u) {
+                const int head = (run + u * share.parts) * at_once + slot;
+                if (head >= in.heads) continue;
+                mine.load(in.at + token * in.token + head * in.head, raw_x[u]);
+                mine.load(grad.at + token * grad.token + head * grad.head, raw_g[u]);
+            }
+            if (run == part) turn.template at<SIDE>(how, token, lane, in_head, share.per_head, share.d, angles[wave]);
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int head = (run + u * share.parts) * at_once + slot;
-                    if (head >= in.heads) continue;          // (sums below are among the lanes of one head)
-                    float x[C][2 * V], g[C][2 * V], w[C][2 * V];
-                    mine.take(raw_x[u], x);
-                    mine.take(raw_g[u], g);
-                    const float inverse = rsqrtf(fmaf(head_sum(dot(x, x), share.per_head), args.inverse_d, args.eps));
-                    turn.template turn<SIDE, true>(g);
-                    take_gain(mine, gain, w);
+            for (int u = 0; u < kAhead; ++u) {
+                const int head = (run + u * share.parts) * at_once + slot;
+                if (head >= in.heads) continue;          // (sums below are among the lanes of one head)
+                float x[C][2 * V], g[C][2 * V], w[C][2 * V];
+                mine.take(raw_x[u], x);
+                mine.take(raw_g[u], g);
+                const float inverse = rsqrtf(fmaf(head_sum(dot(x, x), share.per_head), args.inverse_d, args.eps));
+                turn.template turn<SIDE, true>(g);
+                take_gain(mine, gain, w);
 #pragma unroll
-                    for (int c = 0; c < C; ++c) {
+                for (int c = 0; c < C; ++c) {
 #pragma unroll
-                        for (int j = 0; j < 2 * V; ++j) {
-                            x[c][j] *= inverse;
-                            dw[c][j] = fmaf(g[c][j], x[c][j], dw[c][j]);
-                            g[c][j] *= w[c][j];
-                        }
+                    for (int j = 0; j < 2 * V; ++j) {
+                        x[c][j] *= inverse;
+                        dw[c][j] = fmaf(g[c][j], x[c][j], dw[c][j]);
+                        g[c][j] *= w[c][j];
                     }
-                    const float mean = head_sum(dot(g, x), share.per_head) * args.inverse_d;
-#pragma unroll
-                    for (int c = 0; c < C; ++c) {
-#pragma unroll
-                        for (int j = 0; j < 2 * V; ++j) x[c][j] = inverse * fmaf(-mean, x[c][j], g[c][j]);
-                    }
-                    mine.store(out.at + token * out.token + head * out.head, x);
                 }
+                const float mean = head_sum(dot(g, x), share.per_head) * args.inverse_d;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+#pragma unroll
+                    for (int j = 0; j < 2 * V; ++j) x[c][j] = inverse * fmaf(-mean, x[c][j], g[c][j]);
+                }
+                mine.store(out.at + token * out.token + head * out.head, x);
             }
         }
+    }
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
-            for (int j = 0; j < 2 * V; ++j) {
-                float sum = dw[c][j];
-                for (int step = share.per_head; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
-                if (slot == 0 && mine.there[c]) sums[wave][j < V ? mine.first[c] + j : mine.second[c] + j - V] = sum;
-            }
+        for (int j = 0; j < 2 * V; ++j) {
+            float sum = dw[c][j];
+            for (int step = share.per_head; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
+            if (slot == 0 && mine.there[c]) sums[wave][j < V ? mine.first[c] + j : mine.second[c] + j - V] = sum;
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < share.d; i += kThreads) {
-            float sum = sums[0][i];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < share.d; i += kThreads) {
+        float sum = sums[0][i];
 #pragma unroll
-            for (int v = 1; v < kWaves; ++v) sum += sums[v][i];
-            args.partial[((int64_t)blockIdx.x * 2 + side) * share.d + i] = sum;
-        }
+        for (int v = 1; v < kWaves; ++v) sum += sums[v][i];
+        args.partial[((int64_t)blockIdx.x * 2 + side) * share.d + i] = sum;
     }
 }
 
@@ -611,7 +609,7 @@ int sparseloco_qk_norm_rotary_grad(const sparseloco_heads* grad_q_out, const spa
             const Backward<T> args{{view<const T>(grad_q_out), view<const T>(grad_k_out)}, {view<const T>(q), view<const T>(k)},
                                    {view<T>(grad_q), view<T>(grad_k)}, {q_gain, k_gain}, gain_dtype == SPLC_BF16, (float)eps,
                                    1.f / (float)head_dim, static_cast<float*>(ws)};
-            hipLaunchKernelGGL((heads_grad_kernel<T, decltype(width)::value, decltype(pairs_side)::value>), dim3(groups), dim3(kThreads),
+            hipLaunchKernelGGL((heads_grad_kernel<T, decltype(width)::value, decltype(pairs_side)::value>), dim3(groups, k ? 2 : 1), dim3(kThreads),
                                0, static_cast<hipStream_t>(stream), args, rotation(how, false), s);
         });
         if (rc != SPLC_OK) return rc;
