@@ -321,7 +321,8 @@ struct Backward {
     const void* gain[2];
     int gain_bf16;
     float eps, inverse_d;
-    float* partial;                                          // [workgroup][2][d]
+    float* partial;                                          // [workgroup][d]
+    int groups[2], parts[2];                                 // workgroups of the queries, then of the keys; shares of a token's heads
 };
 
 template <class T, int V, bool SIDE>
@@ -334,9 +335,10 @@ __global__ __launch_bounds__(kThreads, grad_waves_a_simd(V)) void heads_grad_ker
     const int lane = threadIdx.x & 63, in_head = lane & (share.per_head - 1), slot = lane >> share.lane_bits;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at_once = 64 >> share.lane_bits;
     const Mine mine(in_head, share.per_head, share.d, how.r);
-    const int64_t items = share.tokens * share.parts;
     __shared__ __align__(16) float gain[kMostDim];
-    const int side = blockIdx.y;                             // queries or keys: the sums of one gain take registers
+    const int side = (int)blockIdx.x >= args.groups[0];      // queries or keys: the sums of one gain take registers
+    const int group = side ? blockIdx.x - args.groups[0] : blockIdx.x, groups = args.groups[side], parts = args.parts[side];
+    const int64_t items = share.tokens * parts;
     const View<const T> in = args.x[side], grad = args.dy[side];
     const View<T> out = args.dx[side];
     const int runs = (in.heads + at_once - 1) / at_once;
@@ -348,15 +350,15 @@ __global__ __launch_bounds__(kThreads, grad_waves_a_simd(V)) void heads_grad_ker
 #pragma unroll
         for (int j = 0; j < 2 * V; ++j) dw[c][j] = 0.f;
     }
-    for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += (int64_t)gridDim.x * kWaves) {
-        const int64_t token = item / share.parts;
-        const int part = (int)(item - token * share.parts);
+    for (int64_t item = (int64_t)group * kWaves + wave; item < items; item += (int64_t)groups * kWaves) {
+        const int64_t token = item / parts;
+        const int part = (int)(item - token * parts);
         Turn<V, C> turn;
-        for (int run = part; run < runs; run += kAhead * share.parts) {
+        for (int run = part; run < runs; run += kAhead * parts) {
             typename Mine::Raw raw_x[kAhead], raw_g[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int head = (run + u * share.parts) * at_once + slot;
+                const int head = (run + u * parts) * at_once + slot;
                 if (head >= in.heads) continue;
                 mine.load(in.at + token * in.token + head * in.head, raw_x[u]);
                 mine.load(grad.at + token * grad.token + head * grad.head, raw_g[u]);
@@ -364,7 +366,7 @@ __global__ __launch_bounds__(kThreads, grad_waves_a_simd(V)) void heads_grad_ker
             if (run == part) turn.template at<SIDE>(how, token, lane, in_head, share.per_head, share.d, angles[wave]);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int head = (run + u * share.parts) * at_once + slot;
+                const int head = (run + u * parts) * at_once + slot;
                 if (head >= in.heads) continue;          // (sums below are among the lanes of one head)
                 float x[C][2 * V], g[C][2 * V], w[C][2 * V];
                 mine.take(raw_x[u], x);
@@ -405,21 +407,23 @@ __global__ __launch_bounds__(kThreads, grad_waves_a_simd(V)) void heads_grad_ker
         float sum = sums[0][i];
 #pragma unroll
         for (int v = 1; v < kWaves; ++v) sum += sums[v][i];
-        args.partial[((int64_t)blockIdx.x * 2 + side) * share.d + i] = sum;
+        args.partial[(int64_t)blockIdx.x * share.d + i] = sum;
     }
 }
 
-// Sums of the workgroups' partial sums, 16 channels a workgroup, all of its loads at once.
-__global__ __launch_bounds__(kJoinThreads) void heads_join_kernel(const float* __restrict__ partial, int groups, int d, float* dq_gain,
-                                                                  float* dk_gain, int accumulate) {
+// Sums of the workgroups' partial sums, 16 channels of one gain a workgroup, all of its loads at once.
+__global__ __launch_bounds__(kJoinThreads) void heads_join_kernel(const float* __restrict__ partial, int q_groups, int k_groups, int d,
+                                                                  float* dq_gain, float* dk_gain, int accumulate) {
     constexpr int kParts = kJoinThreads / kJoinRows, kEach = kGradGroups / kParts;
     __shared__ float sums[kJoinThreads];
     const int i = blockIdx.x * kJoinRows + threadIdx.x % kJoinRows, part = threadIdx.x / kJoinRows;
+    const int groups = blockIdx.y ? k_groups : q_groups;
+    if (blockIdx.y) partial += (int64_t)q_groups * d;
     float v[kEach], sum = 0.f;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
         const int g = part + e * kParts;
-        v[e] = i < 2 * d && g < groups ? partial[(int64_t)g * 2 * d + i] : 0.f;
+        v[e] = i < d && g < groups ? partial[(int64_t)g * d + i] : 0.f;
     }
 #pragma unroll
     for (int e = 0; e < kEach; ++e) sum += v[e];
@@ -429,10 +433,8 @@ __global__ __launch_bounds__(kJoinThreads) void heads_join_kernel(const float* _
         if (part < half) sums[threadIdx.x] = sum += sums[threadIdx.x + half * kJoinRows];
         __syncthreads();
     }
-    if (part > 0 || i >= 2 * d) return;
-    float* out = i < d ? dq_gain : dk_gain;
-    if (!out) return;
-    out += i < d ? i : i - d;
+    if (part > 0 || i >= d) return;
+    float* out = (blockIdx.y ? dk_gain : dq_gain) + i;
     *out = accumulate ? *out + sum : sum;
 }
 
@@ -598,24 +600,36 @@ int sparseloco_qk_norm_rotary_grad(const sparseloco_heads* grad_q_out, const spa
     if (!grad_q_gain || (k != nullptr) != (grad_k_gain != nullptr) || !ws) return SPLC_EINVAL;
     if (ws_bytes < sparseloco_qk_norm_rotary_grad_ws_bytes(tokens, q_heads, k_heads, head_dim)) return SPLC_EINVAL;
     if (!aligned(grad_q_gain, 4) || !aligned(grad_k_gain, 4) || !aligned(ws, 4)) return SPLC_EALIGN;
-    uint32_t groups = 0;
+    int groups[2] = {0, 0};
     if (tokens > 0 && q_heads + k_heads > 0) {
         const bool side = how->interleaved != 0;
         const int v = run_of_pairs(dtype, head_dim, how->pairs, side);
         const Shares s = shares(tokens, head_dim, v, q_heads, k_heads);
-        groups = (uint32_t)std::min<int64_t>((tokens * s.parts + kWaves - 1) / kWaves, grad_groups(tokens));
+        // With eight pairs a lane as many workgroups as run at once, 1024, shared out by the heads of either side: 16384 tokens x 32
+        // heads of 128 bf16 channels 85 us, with 1024 for either side 91.  Narrower lanes gain from more of them: 16384 x 24 heads
+        // of 80 fp32 channels 61 us so, 53 with 1024 for either side.
+        const int at_once = 64 / s.per_head;
+        int parts[2] = {1, 1};
+        for (int keys = 0; keys < 2; ++keys) {
+            const int heads = keys ? k_heads : q_heads, runs = (heads + at_once - 1) / at_once;
+            if (heads == 0) continue;
+            parts[keys] = (int)std::min<int64_t>(runs, std::max<int64_t>(1, kFillingWaves / tokens));
+            const int64_t share = v == 8 ? std::max<int64_t>(1, (int64_t)kGradGroups * heads / (q_heads + k_heads)) : kGradGroups;
+            const int64_t most = std::min<int64_t>(grad_groups(tokens), share);
+            groups[keys] = (int)std::min<int64_t>((tokens * parts[keys] + kWaves - 1) / kWaves, most);
+        }
         rc = with_variant(dtype, v, side, [&](auto type, auto width, auto pairs_side) {
             using T = decltype(type);
             const Backward<T> args{{view<const T>(grad_q_out), view<const T>(grad_k_out)}, {view<const T>(q), view<const T>(k)},
                                    {view<T>(grad_q), view<T>(grad_k)}, {q_gain, k_gain}, gain_dtype == SPLC_BF16, (float)eps,
-                                   1.f / (float)head_dim, static_cast<float*>(ws)};
-            hipLaunchKernelGGL((heads_grad_kernel<T, decltype(width)::value, decltype(pairs_side)::value>), dim3(groups, k ? 2 : 1), dim3(kThreads),
+                                   1.f / (float)head_dim, static_cast<float*>(ws), {groups[0], groups[1]}, {parts[0], parts[1]}};
+            hipLaunchKernelGGL((heads_grad_kernel<T, decltype(width)::value, decltype(pairs_side)::value>), dim3((unsigned)(groups[0] + groups[1])), dim3(kThreads),
                                0, static_cast<hipStream_t>(stream), args, rotation(how, false), s);
         });
         if (rc != SPLC_OK) return rc;
     }
-    hipLaunchKernelGGL(heads_join_kernel, dim3((2 * head_dim + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), 0,
-                       static_cast<hipStream_t>(stream), static_cast<const float*>(ws), (int)groups, head_dim, grad_q_gain, grad_k_gain,
+    hipLaunchKernelGGL(heads_join_kernel, dim3((head_dim + kJoinRows - 1) / kJoinRows, k ? 2 : 1), dim3(kJoinThreads), 0,
+                       static_cast<hipStream_t>(stream), static_cast<const float*>(ws), groups[0], groups[1], head_dim, grad_q_gain, grad_k_gain,
                        accumulate);
     return hipGetLastError() == hipSuccess ? SPLC_OK : SPLC_EHIP;
 }
