@@ -524,45 +524,67 @@ __global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f,
     // Waits for what was fetched first of so many fetches, and for the operands from LDS; then for all waves.
     constexpr int kAhead = S::kDeep - 1, kWaiting = (kAhead - 1) * 2 * kLoads;
     static_assert(kWaiting < 64, "loads that a wave counts");
-    auto arrived = [&](bool all_ahead) {
+    auto arrived = [&] {
         asm volatile("" ::: "memory");
-        if (all_ahead) __builtin_amdgcn_s_waitcnt((kWaiting & 15) | kWaiting >> 4 << 14 | 7 << 4);
-        else __builtin_amdgcn_s_waitcnt(7 << 4);
+        __builtin_amdgcn_s_waitcnt((kWaiting & 15) | kWaiting >> 4 << 14 | 7 << 4);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    Operands now, next;
+    auto multiply = [&](const Operands& o) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (i * kRow < depth) fetch(i * kRow, i);
-    arrived(kAhead * kRow <= depth);
-    if (kAhead * kRow < depth) fetch(kAhead * kRow, kAhead);
+        for (int term = SPLIT ? 2 : 0; term >= 0; --term) {
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+#pragma unroll
+                for (int j = 0; j < kJ; ++j)                 // columns of C in a lane's registers, rows over the lanes
+                    sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.y[j][term == 1], o.x[i][term == 2], sum[i][j], 0, 0, 0);
+            }
+        }
+    };
+    // Loads from LDS (and fetches) issue between products, which take the matrix cores longer than that.
+    constexpr int kProducts = kI * kJ * (SPLIT ? 3 : 1), kReads = (kI + kJ) * kParts, kFetches = 2 * kLoads;
+    auto interleave = [&](bool fetches) {
+        constexpr int kFirst = 1;
+#pragma unroll
+        for (int i = 0; i < kProducts; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (fetches && i >= kFirst && i - kFirst < kFetches) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+    };
+    Operands now, next;
+    const int last = depth - kRow;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fetch(i * kRow < last ? i * kRow : last, i);
+    arrived();
+    fetch(kAhead * kRow < last ? kAhead * kRow : last, kAhead);
     load(now, 0, 0);
     // The operands of the next 16 of k come from LDS while those at hand are multiplied, across the barrier too: it says that all waves
-    // have read a buffer to its end, and that the next one has arrived.
-    for (int k = 0, buffer = 0; k < depth; k += kRow) {
-        const int after = buffer + 1 < S::kDeep ? buffer + 1 : 0;
+    // have read a buffer to its end, and that the next one has arrived.  (Behind the end of k the last part is fetched again, so that
+    // what a wave waits for is always as many loads; nothing reads it.)
+    int buffer = 0;
+    for (int k = 0; k < last; k += kRow) {
+        const int after = buffer + 1 < S::kDeep ? buffer + 1 : 0, ahead = k + S::kDeep * kRow;
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
-            if (kk + 1 < kSteps) {
-                load(next, buffer, kk + 1);
-            } else if (k + kRow < depth) {
-                arrived(k + (kAhead + 1) * kRow <= depth);
-                if (k + S::kDeep * kRow < depth) fetch(k + S::kDeep * kRow, buffer);
-                load(next, after, 0);
-            }
-#pragma unroll
-            for (int term = SPLIT ? 2 : 0; term >= 0; --term) {
-#pragma unroll
-                for (int i = 0; i < kI; ++i) {
-#pragma unroll
-                    for (int j = 0; j < kJ; ++j)             // columns of C in a lane's registers, rows over the lanes
-                        sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now.y[j][term == 1], now.x[i][term == 2], sum[i][j], 0, 0, 0);
-                }
-            }
+        for (int kk = 0; kk + 1 < kSteps; ++kk) {
+            load(next, buffer, kk + 1);
+            multiply(now);
+            interleave(false);
             now = next;
         }
+        arrived();
+        fetch(ahead < last ? ahead : last, buffer);
+        load(next, after, 0);
+        multiply(now);
+        interleave(true);
+        now = next;
         buffer = after;
+    }
+#pragma unroll
+    for (int kk = 0; kk < kSteps; ++kk) {
+        if (kk + 1 < kSteps) load(next, buffer, kk + 1);
+        multiply(now);
+        now = next;
     }
     if (STEP == LAST && result.to < 0) {
         float factor;
