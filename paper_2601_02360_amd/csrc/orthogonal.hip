@@ -16,10 +16,10 @@
 //   FP16X3  operands are hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: what fp32 products give, 2e-6 to 4e-6 off.
 //
 // What bounds it (MI355X; fp16 products of 8192 x 8192 by the vendor's library: 1240 TFLOP/s, for which the chip lowers its clock to
-// 2 GHz and below): the matrix cores.  FP16X3, 32 of 2048 x 2048, three products counted: X <- a X + B X 1100 TFLOP/s, of which the
-// tiles' ends, 16 bytes read and written an element, take a fifth, and symmetric products 1050; FP16, the ends weighing three times
-// as much, 730 and 790.  Whole calls: 0.9B model, one step, FP16X3, 75 ms; 8 of 2048 x 5632, FP16, 4.5 ms; one of 512 x 512, FP16X3,
-// 116 us, most of it 18 launches of 6.4 us.
+// 2 GHz and below): the matrix cores.  FP16X3, 32 of 2048 x 2048, three products counted: X <- a X + B X 1490 us or 1107 TFLOP/s, of which
+// the tiles' ends, 16 bytes read and written an element, take a fifth, and symmetric products 840 us, 1105 of the tiles that are formed;
+// FP16, the ends weighing three times as much, 708 us or 776 TFLOP/s, and 340 us or 910.  Whole calls: 0.9B model, one step, FP16X3,
+// 72 ms; 8 of 2048 x 5632, FP16, 4.5 ms; one of 512 x 512, FP16X3, 110 us, most of it 18 launches of 6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -47,7 +47,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 __host__ __device__ inline int padded(int n) { return (n + kPad - 1) / kPad * kPad; }
 // From a row to the next: an odd number of 128 bytes (256 where elements are hi + lo), so that the same piece of many rows lies in
-// many channels of the cache (32 of 2048 x 2048, X <- a X + B X: FP16X3 1575 -> 1501 us, FP16 855 -> 753).
+// many channels of the cache (32 of 2048 x 2048, X <- a X + B X, when this was taken: FP16X3 1575 -> 1501 us, FP16 855 -> 753).
 __host__ __device__ inline int stride(int n) { return (n + kPad - 1) / kPad % 2 ? padded(n) : padded(n) + kPad; }
 
 struct Matrix {
@@ -355,6 +355,7 @@ struct Shape {
     static constexpr int WR = WR_, WC = WC_, WK = WK_, IR = IR_, kSide = SIDE_, BK = BK_, kDeep = DEEP_;
     static constexpr int kWaves = WR_ * WC_ * WK_, kLanes = kWaves * 64, kTile = WC_ * SIDE_;
     static constexpr bool SPLIT = SPLIT_;
+    static constexpr int kBytes = DEEP_ * 2 * kTile * BK_ * (SPLIT_ ? 4 : 2), kWavesASimd = (kWaves + 3) / 4 * (2 * kBytes <= 160 * 1024 ? 2 : 1);
     static_assert(kPad % BK_ == 0, "whole rows of operands");
     static_assert(WR_ * IR_ == WC_, "square tiles");
     static_assert(WK_ == 1 || (WC_ == 1 && IR_ == 1), "one block where waves share k");
@@ -388,10 +389,10 @@ __device__ __forceinline__ int exchange(int row) {
 // Then the sums pass LDS, block by block, to be finished and stored along rows of C, 16 bytes a lane, and once more along its columns
 // for the transposed (or mirrored) copy.  (0.9B model, one step: sums stored from where the products leave them, tiles of 128, 141 ms;
 // through LDS 126; tiles of 256 120; operands of the next 16 of k read beside the products 114.5; hi and lo side by side 106; large
-// batches 92; steps in squares 76.)
+// batches 92; steps in squares 76; loads issued between products 72.)
 template <class S, int STEP>
-__global__ __launch_bounds__(S::kLanes, 2) void product_kernel(Batch, Product f, Result result, int odd,
-                                                            const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
+__global__ __launch_bounds__(S::kLanes, S::kWavesASimd) void product_kernel(Batch, Product f, Result result, int odd,
+                                                                            const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
     constexpr bool SPLIT = S::SPLIT;
     constexpr int SIDE = S::kSide;
     constexpr int kParts = SPLIT ? 2 : 1, BK = S::BK, kRow = BK * kParts, kPieces = kRow / 8, kRowsALoad = 64 / kPieces;
@@ -864,7 +865,7 @@ bool steps_of(const double* coefficients, int steps, bool at_once, Steps& s) {
 // a round), and for a round what was measured.  MI355X, us: 32 of 2048 x 2048, FP16X3, products of 2048 terms, 8 rounds of 256 tiles 1500;
 // 3 of 5630 x 2050, symmetric ones of 2050 and of 5630 terms, a round of 128 tiles 125 and 301; 9 of 768 x 2048, of 768 and 2048 terms, 3
 // rounds of 64 tiles 38 and 72.  Where tiles of 32 x 32 all run at once latency counts, and those are shortest: one of 512 x 512, the
-// whole call, 126 us, with tiles of 64 163; of 768 x 768, which has more of them, 217 and 201.
+// whole call, 110 us, with tiles of 64 155; of 768 x 768, which has more of them, 214 and 184.
 enum { TINY, SMALL, MIDDLE, LARGE };
 struct Tile {
     int size;
@@ -899,8 +900,8 @@ Tile tile_of(const Matrices& all, int count, bool triangle, bool along, bool spl
 
 // Whether matrices that are wide enough take several steps at once (with operands as exact as fp32 only).  In flops of five steps, units
 // of n^3 and m = r n, that is 6 r + 14 instead of 15 r + 5, but 18 launches instead of 15, and apart from the others.  So by what the
-// launches take, where that is 15 % less.  MI355X, ms, apart and together: 9 of 768 x 2048 beside 12 of 768 x 768 1.68 and 1.43, 3 of
-// 5630 x 2050 3.11 and 4.45, the 0.9B model 75.7 and 92.6.
+// launches take, where that is 15 % less.  MI355X, ms, with steps at once and without: 9 of 768 x 2048 beside 12 of 768 x 768 1.36 and
+// 1.46, 3 of 5630 x 2050 2.88 and 4.13, the 0.9B model 71.8 and 87.8.
 bool wide(const Matrix& m) { return 2 * std::max(m.rows, m.cols) >= 3 * m.n(); }
 double estimated(const std::vector<Matrix>& all, int grams, int squares, int applies) {
     auto launch = [&](bool triangle, bool along) { return 2.0 + tile_of(all, (int)all.size(), triangle, along, true).us; };
