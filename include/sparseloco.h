@@ -520,9 +520,10 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
  * tokens and heads, added to what is there with accumulate).  ws: .._ws_bytes(tokens, ..) bytes, 4-byte aligned, need not be
  * cleared; a workspace for more tokens serves fewer.  The same call gives the same bits.
  * Everything is computed in fp32 (squares must not overflow there) and rounded once to dtype (SPLC_F32 or SPLC_BF16, that of all
- * lists).  What is written may be an input of its own side, element for element (q_out: q; grad_q: q or grad_q_out; keys likewise), and
- * must overlap nothing otherwise; its own heads must not overlap one another.  A token or head of zeros has the norm's factor 1 / sqrt(eps); with eps = 0 it becomes NaN.
- * What is not finite stays in its head (and in the gains' gradients).  tokens = 0: nothing but the gains' gradients is written.
+ * lists).  What is written may be an input of its own side, element for element (q_out: q; grad_q: q or grad_q_out; keys likewise),
+ * and must overlap nothing otherwise; its own heads must not overlap one another.  A head of zeros has the norm's factor
+ * 1 / sqrt(eps); with eps = 0 it becomes NaN.  What is not finite stays in its head (and in the gains' gradients).  tokens = 0:
+ * nothing but the gains' gradients is written.
  */
 #define SPLC_MAX_HEAD_DIM 512
 #define SPLC_MAX_HEADS 65536
