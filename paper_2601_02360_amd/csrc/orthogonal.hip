@@ -17,9 +17,11 @@
 //
 // What bounds it (MI355X; fp16 products of 8192 x 8192 by the vendor's library: 1240 TFLOP/s, for which the chip lowers its clock to
 // 2 GHz and below): the matrix cores.  FP16X3, 32 of 2048 x 2048, three products counted: X <- a X + B X 1490 us or 1107 TFLOP/s, of which
-// the tiles' ends, 16 bytes read and written an element, take a fifth, and symmetric products 840 us, 1105 of the tiles that are formed;
-// FP16, the ends weighing three times as much, 708 us or 776 TFLOP/s, and 340 us or 910.  Whole calls: 0.9B model, one step, FP16X3,
-// 72 ms; 8 of 2048 x 5632, FP16, 4.5 ms; one of 512 x 512, FP16X3, 110 us, most of it 18 launches of 6 us.
+// the tiles' ends, 16 bytes read and written an element, take a third, and symmetric products 830 us, 1120 of the tiles that are formed;
+// FP16, whose ends are 10 bytes beside a third of the products, 710 us or 775 TFLOP/s, and 340 us or 910.  It is power that tiles' ends
+// and products share: neither starting workgroups apart, nor loads before stores, nor fewer instructions in the ends brings more than
+// 1 %, and the same launch over other numbers takes 12 % less.  Whole calls: 0.9B model, one step, FP16X3,
+// 71.5 ms; 8 of 2048 x 5632, FP16, 4.5 ms; one of 512 x 512, FP16X3, 107 us, most of it 18 launches of 6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -41,6 +43,8 @@ constexpr int64_t kBatchElements = (int64_t)1 << 33;         // fp16 numbers of 
 constexpr int kMostSide = 1 << 22;                           // rows and columns: offsets inside a tile's rows stay in 32 bits
 constexpr int kMostSteps = SPLC_MAX_ORTHO_STEPS;
 
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef float vfloat2 __attribute__((ext_vector_type(2)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -123,6 +127,15 @@ __device__ __forceinline__ int group_of(int groups) {
     const int left = groups - full * kDies * kRun, each = (left + kDies - 1) / kDies, j = i - full * kRun;
     return j < each && die * each + j < left ? full * kDies * kRun + die * each + j : -1;
 }
+
+// Pairs: a 32-bit word of two fp16 numbers.  What hi leaves is exact, formed by an fma that takes hi as it is (`minus` is -1).
+__device__ __forceinline__ void split2(float x, float y, float minus, half2& hi, half2& lo) {
+    hi = __builtin_convertvector((vfloat2{x, y}), half2);
+    lo = __builtin_convertvector((vfloat2{fmaf((float)hi.x, minus, x), fmaf((float)hi.y, minus, y)}), half2);
+}
+// The lower (upper) halves of two words.
+__device__ __forceinline__ uint32_t lower(uint32_t first, uint32_t second) { return __builtin_amdgcn_perm(second, first, 0x05040100); }
+__device__ __forceinline__ uint32_t upper(uint32_t first, uint32_t second) { return __builtin_amdgcn_perm(second, first, 0x07060302); }
 
 __device__ __forceinline__ void split(float x, _Float16& hi, _Float16& lo) {
     hi = (_Float16)x;
@@ -389,7 +402,7 @@ __device__ __forceinline__ int exchange(int row) {
 // Then the sums pass LDS, block by block, to be finished and stored along rows of C, 16 bytes a lane, and once more along its columns
 // for the transposed (or mirrored) copy.  (0.9B model, one step: sums stored from where the products leave them, tiles of 128, 141 ms;
 // through LDS 126; tiles of 256 120; operands of the next 16 of k read beside the products 114.5; hi and lo side by side 106; large
-// batches 92; steps in squares 76; loads issued between products 72.)
+// batches 92; steps in squares 76; loads issued between products 72; sums ended in pairs of numbers 71.4.)
 template <class S, int STEP>
 __global__ __launch_bounds__(S::kLanes, S::kWavesASimd) void product_kernel(Batch, Product f, Result result, int odd,
                                                                             const float* __restrict__ grad_scale, _Float16* __restrict__ ws) {
@@ -599,11 +612,14 @@ __global__ __launch_bounds__(S::kLanes, S::kWavesASimd) void product_kernel(Batc
                               : result.adjust == SPLC_MUON_RMS  ? 0.2f * sqrtf(fmaxf(rows, cols))
                                                                 : 1.f);
     }
+    float minus = -1.f;
+    asm("" : "+s"(minus));                                   // (an fma with a known -1 would become a conversion and a subtraction)
     __syncthreads();
 #pragma unroll
     for (int half = 0; half < S::IR; ++half) {
         const int block_row = row0 + wave_row + half * SIDE, block_col = col0 + wave_col;
         if (kTriangle && block_row > block_col) continue;    // below the diagonal: another block's mirror image
+        const bool whole = block_row + SIDE <= rows && block_col + SIDE <= cols;
         float* mine = lds.blocks[wave];
         if (S::WK == 1) load_old(block_row, block_col);
 #pragma unroll
@@ -650,31 +666,48 @@ __global__ __launch_bounds__(S::kLanes, S::kWavesASimd) void product_kernel(Batc
             const bool there = row < rows && col < ld;
             if (kOld && there) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = fmaf(f.own, (float)old_hi[pass][e] + (kOldLo ? (float)old_lo[pass][e] : 0.f), v[e]);
+                for (int e = 0; e < 8; ++e) {
+                    if (kOldLo) v[e] = fmaf((float)old_lo[pass][e], f.own, v[e]);
+                    v[e] = fmaf((float)old_hi[pass][e], f.own, v[e]);
+                }
             }
             if (STEP == SQUARE && SPLIT && f.other >= 0 && there) {
                 const _Float16* from_other = planes.square(f.other) + planes.place(row, col, ld);
                 const half8 hi = *(const half8*)from_other, lo = *(const half8*)(from_other + 32);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = fmaf(f.more, (float)hi[e] + (float)lo[e], v[e]);
+                for (int e = 0; e < 8; ++e) v[e] = fmaf((float)hi[e], f.more, fmaf((float)lo[e], f.more, v[e]));
             }
             if (STEP != LAST) {
-                half8 hi, lo;
+                if (!whole) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (!there || col + e >= cols) v[e] = 0.f;
-                    _Float16 h, l;
-                    split(v[e], h, l);
-                    hi[e] = h;
-                    lo[e] = l;
+                    for (int e = 0; e < 8; ++e)
+                        if (!there || col + e >= cols) v[e] = 0.f;
+                }
+                union {
+                    half8 all;
+                    half2 of[4];
+                    uint32_t word[4];
+                } hi, lo;
+                uint32_t word[8];
+                constexpr bool kLo = SPLIT || STEP == APPLY;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (kLo) split2(v[2 * e], v[2 * e + 1], minus, hi.of[e], lo.of[e]);
+                    else hi.of[e] = __builtin_convertvector((vfloat2{v[2 * e], v[2 * e + 1]}), half2);
                 }
                 if (there) {
                     _Float16* dst = to + planes.place(row, col, ld);
-                    *(half8*)dst = hi;
-                    if (SPLIT || STEP == APPLY) *(half8*)(dst + (STEP == APPLY ? r_lo : 32)) = lo;
+                    *(half8*)dst = hi.all;
+                    if (kLo) *(half8*)(dst + (STEP == APPLY ? r_lo : 32)) = lo.all;
+                }
+                // back as a word an element: hi, and lo above it where the transposed copy has it
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t first = hi.word[e / 2], second = SPLIT ? lo.word[e / 2] : 0;
+                    word[e] = SPLIT ? (e % 2 ? upper(first, second) : lower(first, second)) : e % 2 ? first >> 16 : first;
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h) *(float4*)at[h] = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+                for (int h = 0; h < 2; ++h) *(uint4*)at[h] = make_uint4(word[4 * h], word[4 * h + 1], word[4 * h + 2], word[4 * h + 3]);
             } else if (there) {
                 const int64_t place_of = (int64_t)row * m.cols + col;
                 const int count = m.cols - col < 8 ? m.cols - col : 8;
@@ -729,18 +762,14 @@ __global__ __launch_bounds__(S::kLanes, S::kWavesASimd) void product_kernel(Batc
             if (!passes) break;
             const int in_col = (wave_k * kPasses + pass) * kDown + lane % kDown, in_row = lane / kDown * 8;
             const int col = block_col + in_col, row = block_row + in_row;
-            half8 hi, lo;
+            uint32_t word[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                _Float16 h, l;
-                split(mine[in_block<SIDE>(in_row + e, in_col >> 2) + (in_col & 3)], h, l);
-                hi[e] = h;
-                lo[e] = l;
-            }
+            for (int e = 0; e < 8; ++e) word[e] = __float_as_uint(mine[in_block<SIDE>(in_row + e, in_col >> 2) + (in_col & 3)]);
             if (col < cols && row < ld_t) {
                 _Float16* dst = to_t + planes.place(col, row, ld_t);
-                *(half8*)dst = hi;
-                if (SPLIT) *(half8*)(dst + 32) = lo;
+                *(uint4*)dst = make_uint4(lower(word[0], word[1]), lower(word[2], word[3]), lower(word[4], word[5]), lower(word[6], word[7]));
+                if (SPLIT)
+                    *(uint4*)(dst + 32) = make_uint4(upper(word[0], word[1]), upper(word[2], word[3]), upper(word[4], word[5]), upper(word[6], word[7]));
             }
         }
         if (S::IR > 1) __builtin_amdgcn_wave_barrier();
@@ -901,7 +930,7 @@ Tile tile_of(const Matrices& all, int count, bool triangle, bool along, bool spl
 // Whether matrices that are wide enough take several steps at once (with operands as exact as fp32 only).  In flops of five steps, units
 // of n^3 and m = r n, that is 6 r + 14 instead of 15 r + 5, but 18 launches instead of 15, and apart from the others.  So by what the
 // launches take, where that is 15 % less.  MI355X, ms, with steps at once and without: 9 of 768 x 2048 beside 12 of 768 x 768 1.36 and
-// 1.46, 3 of 5630 x 2050 2.88 and 4.13, the 0.9B model 71.8 and 87.8.
+// 1.46, 3 of 5630 x 2050 2.88 and 4.13, the 0.9B model 71.8 and 87.8 (before sums ended in pairs).
 bool wide(const Matrix& m) { return 2 * std::max(m.rows, m.cols) >= 3 * m.n(); }
 double estimated(const std::vector<Matrix>& all, int grams, int squares, int applies) {
     auto launch = [&](bool triangle, bool along) { return 2.0 + tile_of(all, (int)all.size(), triangle, along, true).us; };
