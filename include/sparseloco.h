@@ -441,7 +441,7 @@ int sparseloco_adamw_step_8bit(const sparseloco_plan* plan, const sparseloco_ten
  *     A = X X^T,   X <- a X + (b A + c A^2) X,
  * and out = X.  The singular values s of X become a s + b s^3 + c s^5 each time: with the usual (3.4445, -4.7750, 2.0315), five times,
  * those above 0.002 come to lie between 0.68 and 1.21.  A matrix of zeros stays one (with eps = 0 it becomes NaN).
- *   x, out: fp32 or bf16 bindings; out may be x itself.  coefficients: 3 numbers a step (host), or NULL for the usual ones.
+ *   x, out: fp32 or bf16 bindings; out may be x itself, and must not overlap it otherwise.  coefficients: 3 numbers a step (host), or NULL for the usual ones.
  *   1 <= steps <= SPLC_MAX_ORTHO_STEPS; coefficients up to 1e4 whose polynomials keep the interval that starts as [0, 1] below 1024.
  *   matmul: SPLC_MATMUL_FP16    operands of 11 bits, for results that are held in bf16: 2e-4 to 2e-3 off in the 2-norm
  *           SPLC_MATMUL_FP16X3  operands of 22 bits in three products, as exact as fp32 ones
@@ -520,8 +520,8 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
  * tokens and heads, added to what is there with accumulate).  ws: .._ws_bytes(tokens, ..) bytes, 4-byte aligned, need not be
  * cleared; a workspace for more tokens serves fewer.  The same call gives the same bits.
  * Everything is computed in fp32 (squares must not overflow there) and rounded once to dtype (SPLC_F32 or SPLC_BF16, that of all
- * lists).  What is written may be an input of its own side, element for element (q_out: q; grad_q: q or grad_q_out; keys likewise),
- * and must overlap nothing otherwise; its own heads must not overlap one another.  A head of zeros has the norm's factor
+ * lists).  What is written may be an input of its own side, element for element at the same strides (q_out: q; grad_q: q or
+ * grad_q_out; keys likewise), and must overlap nothing otherwise; its own heads must not overlap one another.  A head of zeros has the norm's factor
  * 1 / sqrt(eps); with eps = 0 it becomes NaN.  What is not finite stays in its head (and in the gains' gradients).  tokens = 0:
  * nothing but the gains' gradients is written.
  */

@@ -483,6 +483,13 @@ int check(const List* lists, int n, int dtype, int64_t tokens, int d, const spar
     if (out.k && tokens > 0 && out.q->heads > 0 && out.k->heads > 0)
         for (int i = 0; i < n; ++i)
             if (out.q->data == lists[i].k->data || out.k->data == lists[i].q->data) return SPLC_EINVAL;
+    // In place is element for element.
+    auto elsewhere = [&](const sparseloco_heads* in, const sparseloco_heads* written) {
+        return in && tokens > 0 && in->heads > 0 && in->data == written->data &&
+               ((tokens > 1 && in->token_stride != written->token_stride) || (in->heads > 1 && in->head_stride != written->head_stride));
+    };
+    for (int i = 0; i < n - 1; ++i)
+        if (elsewhere(lists[i].q, out.q) || elsewhere(lists[i].k, out.k)) return SPLC_EINVAL;
     const size_t size = dtype == SPLC_F32 ? 4 : 2;
     for (int i = 0; i < n; ++i)
         if (!aligned(lists[i].q->data, size) || (lists[i].k && !aligned(lists[i].k->data, size))) return SPLC_EALIGN;

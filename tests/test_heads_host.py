@@ -67,6 +67,20 @@ def test_what_the_gradient_refuses():
     assert sizes == sorted(sizes) and sizes[0] > 0
 
 
+def test_what_is_written_lies_as_the_input_that_it_replaces():
+    """In place is element for element: heads that begin where the input's do, at other strides, would be read after they are written."""
+    by_head = dict(token=16, head=80)                                  # five tokens of a head, then the next head
+    assert rotary(q_out=heads(**by_head)) == B.SPLC_EINVAL
+    assert rotary(q_out=heads(head=32, token=128)) == B.SPLC_EINVAL
+    assert rotary(q=heads(token=0)) == B.SPLC_EINVAL                    # (one token's heads for all, written over)
+    assert rotary(k=heads(2 * ANY), q_out=heads(3 * ANY), k_out=heads(2 * ANY, **by_head)) == B.SPLC_EINVAL
+    for place in ("grad", "in"):
+        lists = [heads(ANY), heads(2 * ANY), heads(3 * ANY), heads(4 * ANY)]
+        out = [heads(ANY if place == "grad" else 3 * ANY, **by_head), heads(5 * ANY)]
+        assert B.lib().sparseloco_qk_norm_rotary_grad(*lists, 0, 5, 16, ANY, ANY, 0, 1e-6, how(), *out, ANY, ANY, 0, ANY, 1 << 30,
+                                                      None) == B.SPLC_EINVAL
+
+
 def test_what_the_binding_refuses():
     q, k = torch.zeros(5, 4, 16), torch.zeros(5, 2, 16)
     positions, f, w = torch.zeros(5, dtype=torch.int32), torch.zeros(8, dtype=torch.float64), torch.zeros(16)
