@@ -441,8 +441,9 @@ int sparseloco_adamw_step_8bit(const sparseloco_plan* plan, const sparseloco_ten
  *     A = X X^T,   X <- a X + (b A + c A^2) X,
  * and out = X.  The singular values s of X become a s + b s^3 + c s^5 each time: with the usual (3.4445, -4.7750, 2.0315), five times,
  * those above 0.002 come to lie between 0.68 and 1.21.  A matrix of zeros stays one (with eps = 0 it becomes NaN).
- *   x, out: fp32 or bf16 bindings; out may be x itself, and must not overlap it otherwise.  coefficients: 3 numbers a step (host), or NULL for the usual ones.
- *   1 <= steps <= SPLC_MAX_ORTHO_STEPS; coefficients up to 1e4 whose polynomials keep the interval that starts as [0, 1] below 1024.
+ *   x, out: fp32 or bf16 bindings; out may be x itself, and must not overlap it otherwise.  coefficients: 3 numbers a step (host), or
+ *   NULL for the usual ones.  1 <= steps <= SPLC_MAX_ORTHO_STEPS; coefficients up to 1e4 whose polynomials keep the interval that
+ *   starts as [0, 1] below 1024.
  *   matmul: SPLC_MATMUL_FP16    operands of 11 bits, for results that are held in bf16: 2e-4 to 2e-3 off in the 2-norm
  *           SPLC_MATMUL_FP16X3  operands of 22 bits in three products, as exact as fp32 ones
  *   accumulation in fp32, norms in fp64.  ws: sparseloco_orthogonalize_ws_bytes(plan, rows, matmul) bytes, 128-byte aligned, need not
