@@ -444,7 +444,8 @@ int sparseloco_adamw_step_8bit(const sparseloco_plan* plan, const sparseloco_ten
  *   x, out: fp32 or bf16 bindings; out may be x itself, and must not overlap it otherwise.  coefficients: 3 numbers a step (host), or
  *   NULL for the usual ones.  1 <= steps <= SPLC_MAX_ORTHO_STEPS; coefficients up to 1e4 whose polynomials keep the interval that
  *   starts as [0, 1] below 1024.
- *   matmul: SPLC_MATMUL_FP16    operands of 11 bits, for results that are held in bf16: 2e-4 to 2e-3 off in the 2-norm
+ *   matmul: SPLC_MATMUL_FP16    operands of 11 bits, for results that are held in bf16: 2e-4 to 3e-3 off in the 2-norm; below 16 rows
+ *                               or columns up to 1.3e-2, since a few singular values may all lie where the polynomials are steep
  *           SPLC_MATMUL_FP16X3  operands of 22 bits in three products, as exact as fp32 ones
  *   accumulation in fp32, norms in fp64.  ws: sparseloco_orthogonalize_ws_bytes(plan, rows, matmul) bytes, 128-byte aligned, need not
  *   be cleared; two calls at once need one each.  The same call gives the same bits; how a product is cut up, and with it the last

@@ -11,8 +11,9 @@
 // Operands are fp16 numbers times a power of two that the host knows beforehand: |X| <= 1 in the spectral norm, and the polynomial
 // says what that bound becomes, so that no element leaves [-2^14, 2^14] and those 2^-28 of the bound keep 11 bits.
 //   FP16    one product a term.  A, B and X are rounded to 11 bits as operands; X itself is held in 22 (hi + lo) where a X is
-//           added.  Result: 2e-4 to 2e-3 off (relative, depending on how the singular values are spread), as little as a result in
-//           bf16 is rounded by; bf16 operands are 1e-2 to 4e-2 off.
+//           added.  Result: 2e-4 to 3e-3 off (relative, depending on how the singular values are spread; 400 each of normal numbers:
+//           64 x 200 2.3e-3 at most, 16 x 56 3.0e-3, 2 x 14 1.2e-2), as little as a result in bf16 is rounded by; bf16 operands are
+//           1e-2 to 4e-2 off.
 //   FP16X3  operands are hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: what fp32 products give, 2e-6 to 4e-6 off.
 //
 // What bounds it (MI355X; fp16 products of 8192 x 8192 by the vendor's library: 1240 TFLOP/s, for which the chip lowers its clock to
