@@ -601,6 +601,11 @@ __global__ __launch_bounds__(S::kLanes, S::kWavesASimd) void product_kernel(Batc
         multiply(now);
         now = next;
     }
+    // The last fetches are still under way, and have to have landed, of all waves, before sums take the operands' place in LDS: a barrier
+    // by itself waits for no load.
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 << 8 | 7 << 4);            // vmcnt(0)
+    asm volatile("" ::: "memory");
     if (STEP == LAST && result.to < 0) {
         float factor;
         if (!gradient_factor(grad_scale, factor)) return;
