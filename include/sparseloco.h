@@ -476,6 +476,12 @@ int sparseloco_orthogonalize(const sparseloco_plan* plan, const int64_t* rows, c
 int sparseloco_muon_step(const sparseloco_plan* plan, const int64_t* rows, const sparseloco_tensors* theta, const sparseloco_tensors* grads,
                          const sparseloco_tensors* m, int replica, const sparseloco_muon* how, const float* grad_scale,
                          const float* decay, const sparseloco_tensors* theta_bf16, void* ws, int64_t ws_bytes, void* stream);
+/*
+ * How the products of so many matrices (rows[i] x columns[i], none empty) are cut up: host logic only, for tests and tuning.  choice (5
+ * numbers a matrix, or NULL): whether it takes several steps at once in squares (1 or 0), its batch, and the sides of its batch's
+ * tiles (32 .. 256) in X X^T, in products of squares, and in those with X.  Returns the bytes of their workspace, or a negative status.
+ */
+int64_t sparseloco_orthogonalize_choice(int n_matrices, const int64_t* rows, const int64_t* columns, int matmul, int* choice);
 
 /*
  * Token embeddings of the split table of section 2.4 (and of a plain one):

@@ -50,7 +50,7 @@ EXPORTS = [
     "sparseloco_embedding_lookup", "sparseloco_embedding_grad_ws_bytes", "sparseloco_embedding_grad",
     "sparseloco_tensors_rebind", "sparseloco_messages_rebind",
     "sparseloco_rotary", "sparseloco_qk_norm_rotary", "sparseloco_qk_norm_rotary_grad_ws_bytes", "sparseloco_qk_norm_rotary_grad",
-    "sparseloco_orthogonalize_ws_bytes", "sparseloco_orthogonalize", "sparseloco_muon_step",
+    "sparseloco_orthogonalize_ws_bytes", "sparseloco_orthogonalize", "sparseloco_muon_step", "sparseloco_orthogonalize_choice",
 ]
 
 SPLC_OP_PROJECT, SPLC_OP_RECONSTRUCT, SPLC_OP_REPROJECT_PASS1, SPLC_OP_REPROJECT_PASS2 = 0, 1, 2, 3
@@ -142,6 +142,7 @@ def lib():
             "sparseloco_adamw_step_8bit": (i32, [vp, vp, vp, i32, vp, vp, vp, vp, ctypes.POINTER(_AdamW), vp, vp, vp, vp]),
             "sparseloco_embedding_lookup": (i32, [vp, vp, i32, vp, i32, vp, i32, f32, vp, i32, i64, i32, vp]),
             "sparseloco_orthogonalize_ws_bytes": (i64, [vp, p64, i32]),
+            "sparseloco_orthogonalize_choice": (i64, [i32, p64, p64, i32, ctypes.POINTER(i32)]),
             "sparseloco_orthogonalize": (i32, [vp, p64, vp, vp, i32, ctypes.POINTER(f64), i32, f64, i32, vp, i64, vp]),
             "sparseloco_muon_step": (i32, [vp, p64, vp, vp, vp, i32, ctypes.POINTER(_Muon), vp, vp, vp, vp, i64, vp]),
             "sparseloco_rotary": (i32, [hp, hp, i32, i64, i32, rp, i32, hp, hp, vp]),
@@ -1023,6 +1024,19 @@ def sparseloco_orthogonalize(plan: Plan, x, out, ws: torch.Tensor, *, coefficien
                                             replica, numbers, steps, float(eps), matmul, ws.data_ptr(), int(ws.numel()), _stream(stream))
     if rc != SPLC_OK:
         raise SparseLoCoError(rc, where)
+
+
+def orthogonalize_choice(shapes, *, matmul: int = SPLC_MATMUL_FP16X3):
+    """([(at_once, batch, gram, squares, products), ...], bytes): for every matrix whether it takes several steps at once in squares, its batch,
+    and the sides of that batch's tiles in X X^T, in products of squares and in those with X; and the workspace's bytes (host logic only)."""
+    where = "sparseloco_orthogonalize_choice"
+    n, sides = len(shapes), [[_integer(x, 64, where) for x in s] for s in shapes]
+    choice = (ctypes.c_int * max(5 * n, 1))()
+    rows, columns = ((ctypes.c_int64 * max(n, 1))(*x) for x in ([r for r, _ in sides], [c for _, c in sides]))
+    size = int(lib().sparseloco_orthogonalize_choice(n, rows, columns, _integer(matmul, 32, where), choice))
+    if size < 0:
+        raise SparseLoCoError(size, where)
+    return [(bool(choice[5 * i]), *choice[5 * i + 1:5 * i + 5]) for i in range(n)], size
 
 
 def sparseloco_muon_step(plan: Plan, theta, grads, m, ws: torch.Tensor, *, lr: float, momentum: float = 0.95, nesterov: bool = True,

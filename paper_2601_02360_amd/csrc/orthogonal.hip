@@ -970,17 +970,17 @@ void add_batches(std::vector<Matrix>& all, bool split, int squares, Shapes& s) {
     }
 }
 
-int shapes(const sparseloco_plan* plan, const int64_t* rows, int matmul, Shapes& s) {
-    if (!plan || !rows || (matmul != SPLC_MATMUL_FP16 && matmul != SPLC_MATMUL_FP16X3)) return SPLC_EINVAL;
+int shapes(const std::vector<int64_t>& numel, const int64_t* rows, int matmul, Shapes& s) {
+    if (!rows || (matmul != SPLC_MATMUL_FP16 && matmul != SPLC_MATMUL_FP16X3)) return SPLC_EINVAL;
     const bool split = matmul == SPLC_MATMUL_FP16X3;
-    s.chunks = plan->n_update;
     std::vector<Matrix> all, apart, others;
-    for (int i = 0; i < plan->n_tensors; ++i) {
-        const int64_t n = plan->numel[(size_t)i];
+    for (size_t i = 0; i < numel.size(); ++i) {
+        const int64_t n = numel[i];
         if (rows[i] < 0 || (n > 0 && (rows[i] < 1 || n % rows[i] != 0))) return SPLC_EINVAL;
         if (n == 0) continue;
         if (rows[i] > kMostSide || n / rows[i] > kMostSide) return SPLC_EINVAL;
-        const Matrix m{0, (int)rows[i], (int)(n / rows[i]), i, 0};
+        s.chunks += (n + kChunk - 1) / kChunk;
+        const Matrix m{0, (int)rows[i], (int)(n / rows[i]), (int)i, 0};
         all.push_back(m);
         (split && wide(m) ? apart : others).push_back(m);
     }
@@ -1073,7 +1073,7 @@ Space space(void* ws, const Shapes& s) {
 
 int check_ws(const sparseloco_plan* plan, const int64_t* rows, const double* coefficients, int steps, double eps, int matmul, void* ws,
              int64_t bytes, Shapes& shape, Steps (&s)[2]) {
-    const int rc = shapes(plan, rows, matmul, shape);
+    const int rc = shapes(plan->numel, rows, matmul, shape);
     if (rc != SPLC_OK) return rc;
     if (!steps_of(coefficients, steps, false, s[0]) || (shape.at_once > 0 && !steps_of(coefficients, steps, true, s[1]))) return SPLC_EINVAL;
     if (!finite64(eps) || eps < 0.0 || !ws || bytes < ws_bytes(shape, plan->n_tensors)) return SPLC_EINVAL;
@@ -1087,8 +1087,39 @@ extern "C" {
 int64_t sparseloco_orthogonalize_ws_bytes(const sparseloco_plan* plan, const int64_t* rows, int matmul) {
     try {
         Shapes s;
-        const int rc = shapes(plan, rows, matmul, s);
+        if (!plan) return SPLC_EINVAL;
+        const int rc = shapes(plan->numel, rows, matmul, s);
         return rc == SPLC_OK ? ws_bytes(s, plan->n_tensors) : rc;
+    } catch (...) {
+        return SPLC_ENOMEM;
+    }
+}
+
+int64_t sparseloco_orthogonalize_choice(int n_matrices, const int64_t* rows, const int64_t* columns, int matmul, int* choice) {
+    try {
+        if (n_matrices < 0 || (n_matrices > 0 && (!rows || !columns))) return SPLC_EINVAL;
+        std::vector<int64_t> numel;
+        for (int i = 0; i < n_matrices; ++i) {
+            if (rows[i] < 1 || rows[i] > kMostSide || columns[i] < 1 || columns[i] > kMostSide) return SPLC_EINVAL;
+            numel.push_back(rows[i] * columns[i]);
+        }
+        Shapes s;
+        const int rc = n_matrices > 0 ? shapes(numel, rows, matmul, s) : SPLC_OK;
+        if (rc != SPLC_OK) return rc;
+        for (size_t i = 0; choice && i < s.batches.size(); ++i) {
+            const Batch& b = s.batches[i];
+            const bool split = matmul == SPLC_MATMUL_FP16X3;
+            const auto side = [&](bool triangle, bool along) { return 32 << tile_of(b.of, b.count, triangle, along, split).size; };
+            for (int m = 0; m < b.count; ++m) {
+                int* of = choice + 5 * (int64_t)b.of[m].tensor;
+                of[0] = i < s.at_once;
+                of[1] = (int)i;
+                of[2] = side(true, true);
+                of[3] = side(true, false);
+                of[4] = side(false, false);
+            }
+        }
+        return ws_bytes(s, n_matrices);
     } catch (...) {
         return SPLC_ENOMEM;
     }

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2601_02360_amd import binding as B
-from test_gpu_orthogonal import MODES, matrix
+from test_gpu_orthogonal import MODES, USUAL, agree, bound, in_squares, matrix, packed, tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,48 @@ def test_the_same_call_gives_the_same_bits(mode, shapes):
     for other in outs[1:]:
         assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
     assert all(bool(torch.isfinite(t).all()) for t in outs[0])
+
+
+def orthogonalised(x, matmul, coefficients):
+    shapes = [tuple(t.shape) for t in x]
+    plan, out = B.Plan(shapes, 32), packed([torch.full_like(t, float("nan")) for t in x])
+    ws = B.orthogonalize_workspace(plan, matmul=matmul)
+    assert ws.numel() == B.orthogonalize_choice(shapes, matmul=matmul)[1]
+    B.sparseloco_orthogonalize(plan, bound(plan, x), bound(plan, out), ws.fill_(255), coefficients=coefficients, matmul=matmul)
+    return out
+
+
+POLYNOMIALS = {
+    "usual": USUAL, "one step": USUAL[:1], "three and one": USUAL[:4], "cubic": [(1.5, -0.5, 0.0)] * 8,
+    "changing": [(8.2, -23.5, 17.3), (4.1, -2.95, 0.545), (1.875, -1.25, 0.375)], "large, then small": [(70.0, -50.0, 0.0), (0.02, 0.0, 0.0)],
+    # 8 x 10 is above 64: a step by itself, then two
+    "cut": [(8.0, -8.0, 0.0), (10.0, -0.8, 0.0), (0.1, 0.0, 0.0)]}
+
+
+@pytest.mark.parametrize("polynomial", POLYNOMIALS)
+@pytest.mark.parametrize("shapes,tiles", [([(70, 2241)], (32, 32, 64)), ([(2241, 70), (70, 2241)] * 24, (64, 64, 128)),
+                                          ([(510, 1021), (1021, 510)] * 8 + [(510, 1021)], (128, 128, 128)),
+                                          ([(900, 1801), (1801, 900)] * 12, (256, 256, 256))],
+                         ids=lambda v: "%d of %dx%d" % (len(v), *v[0]) if isinstance(v, list) else "tiles %d" % v[1])
+def test_steps_in_squares(polynomial, shapes, tiles):
+    """Wide and tall matrices that take several steps at once, with every size of tiles for the products of squares (a third operand
+    among them); single steps, pairs and triples, and where the product of the polynomials' first numbers ends one."""
+    matmul, u = MODES["fp16x3"]
+    assert all(c == (True, 0) + tiles for c in B.orthogonalize_choice(shapes, matmul=matmul)[0])
+    x = packed([matrix(r, c, "noise" if i % 3 else "strong", 200 + i) for i, (r, c) in enumerate(shapes)])
+    for t, o in zip(x, orthogonalised(x, matmul, POLYNOMIALS[polynomial])):
+        agree(o, t, u, limit=in_squares(t, u, POLYNOMIALS[polynomial]), coefficients=POLYNOMIALS[polynomial])
+
+
+@pytest.mark.parametrize("polynomial", POLYNOMIALS)
+def test_steps_in_squares_beside_others(polynomial):
+    """Matrices of both kinds in one call."""
+    matmul, u = MODES["fp16x3"]
+    shapes = [(767, 767)] * 12 + [(767, 2050)] * 9
+    shapes[3], shapes[15] = shapes[15], shapes[3]
+    assert [c[0] for c in B.orthogonalize_choice(shapes, matmul=matmul)[0]] == [c > 767 for _, c in shapes]
+    x = packed([matrix(r, c, "strong", 300 + i) for i, (r, c) in enumerate(shapes)])
+    c = POLYNOMIALS[polynomial]
+    square = tolerance(x[0], u, c)                           # (the others' singular values are spread alike)
+    for t, o in zip(x, orthogonalised(x, matmul, c)):
+        agree(o, t, u, limit=in_squares(t, u, c) if t.shape[1] > 767 else square, coefficients=c)

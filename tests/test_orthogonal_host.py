@@ -65,3 +65,24 @@ def test_what_the_library_refuses():
         B.orthogonalize_workspace(long)
     torch.cuda.synchronize()
     assert all(bool((t == 1).all()) for t in out)
+
+
+def test_how_products_are_cut_up():
+    """The answer is host logic alone; tiles by how many of them there are, and several steps at once where that pays."""
+    choice = B.orthogonalize_choice
+    x3, one = B.SPLC_MATMUL_FP16X3, B.SPLC_MATMUL_FP16
+    assert choice([]) == ([], 128)
+    assert [c[2:] for c in choice([(300, 200)])[0]] == [(32, 32, 32)]
+    assert {c[2:4] for c in choice([(1270, 1270)] * 17)[0]} == {(256, 256)} == {c[2:4] for c in choice([(1270, 1270)] * 17, matmul=one)[0]}
+    for shapes in ([(5630, 2050)] * 3, [(2050, 5630)] * 3, [(768, 2048)] * 9 + [(768, 768)] * 12, [(2048, 5632)] * 48 + [(2048, 2048)] * 64):
+        found, size = choice(shapes)
+        assert [c[0] for c in found] == [r != c for r, c in shapes]
+        other, small = choice(shapes, matmul=one)
+        assert not any(c[0] for c in other) and 0 < small < size
+    many, _ = choice([(3, 5)] * 300)
+    assert [max(c[1] for c in many), min(c[1] for c in many)] == [2, 0] and all(sum(c[1] == i for c in many) <= 128 for i in range(3))
+    L, sides = B.lib(), (ctypes.c_int64 * 2)(4, 4)
+    for n, rows, columns, matmul in ((-1, sides, sides, x3), (2, None, sides, x3), (2, sides, None, x3), (2, sides, sides, B.SPLC_MATMUL_FP32),
+                                     (1, (ctypes.c_int64 * 1)(0), sides, x3), (1, sides, (ctypes.c_int64 * 1)(2 ** 22 + 1), x3)):
+        assert L.sparseloco_orthogonalize_choice(n, rows, columns, matmul, None) == B.SPLC_EINVAL
+    assert L.sparseloco_orthogonalize_choice(2, sides, sides, x3, None) == choice([(4, 4), (4, 4)])[1]
