@@ -1,9 +1,11 @@
 """Orthogonalised matrices on the paths that shapes choose: every size of tiles, and several steps at once in squares."""
+import math
+
 import pytest
 import torch
 
 from paper_2601_02360_amd import binding as B
-from test_gpu_orthogonal import MODES, USUAL, agree, bound, in_squares, matrix, packed, tolerance
+from test_gpu_orthogonal import MODES, USUAL, agree, bound, in_squares, matrix, packed, step_reference, tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +77,47 @@ def test_steps_in_squares_beside_others(polynomial):
     square = tolerance(x[0], u, c)                           # (the others' singular values are spread alike)
     for t, o in zip(x, orthogonalised(x, matmul, c)):
         agree(o, t, u, limit=in_squares(t, u, c) if t.shape[1] > 767 else square, coefficients=c)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("polynomial", ["usual", "changing"])
+def test_symmetric_products_in_the_largest_tiles(mode, polynomial):
+    """X X^T and A^2 in tiles of 256, where a wave has two blocks and those below the diagonal are another's mirror image, ragged."""
+    matmul, u = MODES[mode]
+    shapes = [(1270, 1271 - i % 2) for i in range(17)]
+    assert all(c[2:4] == (256, 256) for c in B.orthogonalize_choice(shapes, matmul=matmul)[0])
+    x = packed([matrix(r, c, "strong", 400 + i) for i, (r, c) in enumerate(shapes)])
+    c = POLYNOMIALS[polynomial]
+    limit = tolerance(x[0], u, c)
+    for t, o in zip(x, orthogonalised(x, matmul, c)):
+        agree(o, t, u, limit=limit, coefficients=c)
+
+
+@pytest.mark.parametrize("mode,shapes", [("fp16x3", [(900, 1801), (1801, 900)] * 12), ("fp16x3", [(1270, 1271)] * 17), ("fp16", [(1270, 1271)] * 17)],
+                         ids=["squares", "fp16x3", "fp16"])
+def test_step_of_large_tiles(mode, shapes):
+    matmul, u = MODES[mode]
+    choice = B.orthogonalize_choice(shapes, matmul=matmul)[0]
+    assert all(c[0] == (len(shapes) == 24) and c[2:4] == (256, 256) for c in choice)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    theta = packed([torch.randn(s, generator=gen, device="cuda") * 0.02 for s in shapes])
+    g = packed([matrix(*s, "strong", 20 + i, torch.bfloat16) for i, s in enumerate(shapes)])
+    m = packed([matrix(*s, "strong", 60 + i) for i, s in enumerate(shapes)])
+    copy = packed([torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in shapes])
+    old = [[t.clone() for t in x] for x in (theta, m)]
+    plan, lr, wd = B.Plan(shapes, 32), 2e-2, 0.25
+    B.sparseloco_muon_step(plan, bound(plan, theta), bound(plan, g), bound(plan, m), B.orthogonalize_workspace(plan, matmul=matmul).fill_(255),
+                           lr=lr, weight_decay=wd, theta_bf16=bound(plan, copy), grad_scale=torch.full((1,), 0.5, device="cuda"), matmul=matmul)
+    limit = None
+    for i in range(len(shapes)):
+        gradient = g[i].double() * 0.5
+        want_m, update, want, f = step_reference(old[0][i], gradient, old[1][i], lr, 0.95, True, wd, B.SPLC_MUON_RMS)
+        assert bool(((m[i].double() - want_m).abs() <= 5 * 2.0 ** -24 * (0.95 * old[1][i].double().abs() + 0.05 * gradient.abs())).all())
+        if choice[i][0]:
+            limit = in_squares(update, u)
+        elif limit is None:
+            limit = tolerance(update, u)
+        off = theta[i].double() - want
+        assert float(off.norm()) <= 4 * limit * lr * f + 2.0 ** -24 * 4 * float(want.norm())
+        assert bool((off.norm(dim=1) <= 8 * limit * lr * f / math.sqrt(shapes[i][0]) + 2.0 ** -22 * want.norm(dim=1)).all())
+        assert torch.equal(copy[i], theta[i].bfloat16())
