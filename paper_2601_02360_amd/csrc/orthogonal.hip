@@ -827,7 +827,10 @@ constexpr int kMostAtOnce = 3, kSquares = 2, kSquaresAtOnce = 5;
 bool steps_of(const double* coefficients, int steps, bool at_once, Steps& s) {
     static const double usual[] = {3.4445, -4.7750, 2.0315};
     if (steps < 1 || steps > kMostSteps) return false;
-    auto range = [](double bound) { return 14 - (int)std::ceil(std::log2(std::max(bound, 1e-3))); };
+    // (a bound may be as small as polynomials that shrink X make it)
+    auto range = [](double bound) { return bound > 0.0 ? 14 - (int)std::ceil(std::log2(bound)) : 14; };
+    // B, or Q without its multiple of 1, beside that multiple: what is 2^-40 of it is nothing to 22 bits, and its range stays near.
+    auto beside = [&](double bound, double one) { return range(std::max(bound, std::ldexp(std::fabs(one), -40))); };
     auto power = [](double v, int exponent) { return (float)std::ldexp(v, exponent); };
     auto at = [&](int k) { return coefficients ? coefficients + 3 * k : usual; };
     double most = 1.0;                                       // bound on the singular values of X
@@ -860,7 +863,7 @@ bool steps_of(const double* coefficients, int steps, bool at_once, Steps& s) {
         alpha = 1.0;
         for (int j = 0; j < count; ++j) {
             const double* p = at(k + j);
-            const int b = range(largest_even(p[1], p[2], most * most));
+            const int b = beside(largest_even(p[1], p[2], most * most), p[0]);
             s.of.push_back({SQUARE, power(p[2], b - 2 * a), power(p[1], b - a), 0.f, 0, 0, 0, -1, (int8_t)in_b});
             if (j == 0) {
                 q = b;
@@ -868,7 +871,7 @@ bool steps_of(const double* coefficients, int steps, bool at_once, Steps& s) {
                 in_b = 3;
                 free = 4;
             } else {
-                const int next_q = range(largest_q[(size_t)j]);
+                const int next_q = beside(largest_q[(size_t)j], alpha * p[0]);
                 s.of.push_back({SQUARE, power(1.0, next_q - b - q), power(p[0], next_q - q), power(alpha, next_q - b), (int8_t)in_b,
                                 (int8_t)in_q, (int8_t)in_q, (int8_t)in_b, (int8_t)free});
                 q = next_q;

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2601_02360_amd import binding as B
-from test_gpu_orthogonal import MODES, USUAL, agree, bound, in_squares, matrix, packed, step_reference, tolerance
+from test_gpu_orthogonal import MODES, USUAL, agree, bound, in_squares, matrix, packed, plain, step_reference, tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +121,29 @@ def test_step_of_large_tiles(mode, shapes):
         assert float(off.norm()) <= 4 * limit * lr * f + 2.0 ** -24 * 4 * float(want.norm())
         assert bool((off.norm(dim=1) <= 8 * limit * lr * f / math.sqrt(shapes[i][0]) + 2.0 ** -22 * want.norm(dim=1)).all())
         assert torch.equal(copy[i], theta[i].bfloat16())
+
+
+# Bounds of X far below 1 on the way: shrunk and grown again, by steps alone and before usual ones, and in the cube of a small X.
+SHRINKING = {
+    "identity": [(1e-4, 0.0, 0.0)] * 3 + [(1e4, 0.0, 0.0)] * 3,
+    "before usual ones": [(1e-3, 0.0, 0.0)] * 2 + [(1e4, 0.0, 0.0), (100.0, 0.0, 0.0)] + USUAL,
+    "cubes": [(1e-3, 0.0, 0.0), (0.0, 1e4, 0.0), (1e4, 0.0, 0.0), (10.0, 0.0, 0.0)],
+    "a little beside 1": [(1.0, 1e-35, 1e-38), (3.0, 0.0, -1e-30)],
+    "far": [(1e-30, 0.0, 0.0)] + [(1e4, 0.0, 0.0)] * 7 + [(100.0, 0.0, 0.0)],
+}
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("polynomial", SHRINKING)
+@pytest.mark.parametrize("rows,columns", [(150, 260), (70, 2241)])
+def test_polynomials_that_shrink(mode, polynomial, rows, columns):
+    """X is held to 22 bits of its bound after every step (the fold over the tolerance that counts the first step's alone: the root of
+    as many roundings as there are steps, and 4 times is allowed: up to 13 steps)."""
+    matmul, u = MODES[mode]
+    c = SHRINKING[polynomial]
+    x = [matrix(rows, columns, "strong", 500)]
+    (out,) = orthogonalised(x, matmul, c)
+    limit = max(tolerance(x[0], u, c), math.sqrt(len(c) + 1) / 4 * 0.41 * 2.0 ** -22 * float(plain(x[0], c).norm()))
+    if B.orthogonalize_choice([(rows, columns)], matmul=matmul)[0][0][0]:
+        limit = max(limit, in_squares(x[0], u, c))
+    agree(out, x[0], u, limit=limit, coefficients=c)
