@@ -521,7 +521,8 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
  * and copies channels 2 pairs .. head_dim - 1.  A pair is channels (i, pairs + i), or (2 i, 2 i + 1) with interleaved.  inverse: by
  * the opposite angle, which is the operator's gradient.
  *   positions: `tokens` int32 or int64 (position_bytes 4 or 8) of any sign; frequencies: radians per position, fp64.  Both device
- *   memory, aligned to their elements.  Angles are formed in fp64, their sine and cosine within 2^-22.
+ *   memory, aligned to their elements.  Sine and cosine are within 2^-22 wherever
+ *   |position * frequency| is below 2^63 radians.
  * sparseloco_qk_norm_rotary norms every head first:
  *     x -> gain x / sqrt(mean(x^2) + eps),      q_gain, k_gain: [head_dim] of gain_dtype
  * sparseloco_qk_norm_rotary_grad is its gradient, from that of its outputs, with respect to q, k and both gains (fp32, sums over

@@ -3,9 +3,10 @@
 //
 // A head of `d` channels is d / 2 pairs: pair i turns by position * frequencies[i] for i < r, and not at all behind.  A lane
 // holds V pairs of a head, L = 2^n lanes a head, 64 / L heads a wave at once; a wave takes a token (or, where there are few,
-// a share of its heads) and keeps the cosines and sines of its pairs for all of the token's heads.  Angles are formed in 64 bits
-// as turns, position * (frequency / 2 pi), of which only the fraction is kept: fp32 would be off by 2^-24 of the whole
-// angle, 1e-2 at position 131072.  Everything else is fp32, rounded once to the tensors' type.
+// a share of its heads) and keeps the cosines and sines of its pairs for all of the token's heads.  Angles are formed as turns,
+// position * (frequency / 2 pi), of which only the fraction is kept: fp32 would be off by 2^-24 of the whole angle, 1e-2 at position
+// 131072, and fp64 by 2^-52 of it, 2^-22 at 2^30 radians; so the quotient and the product are two doubles each, and positions of 64
+// bits too.  Everything else is fp32, rounded once to the tensors' type.
 //
 // What bounds it (MI355X): memory, or the launch.  bf16, heads of 128 channels: 32768 x 40 heads rotated 125 us or 5.4 TB/s, 16384 x 32
 // normed and rotated 55 us or 4.9, their gradient 85 us or 4.7, 5 of them the join; one token of 40 heads 4 us.
@@ -153,6 +154,8 @@ struct Lanes {
     }
 };
 
+constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;    // 1 / (2 pi)
+
 template <int V, int C>
 struct Turn {
     float cos[C][V], sin[C][V];
@@ -161,13 +164,23 @@ struct Turn {
     // accesses in their order.
     template <bool SIDE>
     __device__ __forceinline__ void at(const Rotation& how, int64_t token, int wave_lane, int lane, int per_head, int d, float2* shared) {
-        const double position = how.wide ? (double)static_cast<const int64_t*>(how.positions)[token]
-                                         : (double)static_cast<const int32_t*>(how.positions)[token];
+        double whole, rest = 0.0;                                // together the position
+        if (how.wide) {
+            const int64_t at = static_cast<const int64_t*>(how.positions)[token];
+            const double upper = ldexp((double)(int32_t)(at >> 32), 32), lower = (double)(uint32_t)at;
+            whole = upper + lower;
+            rest = lower - (whole - upper);
+        } else {
+            whole = (double)static_cast<const int32_t*>(how.positions)[token];
+        }
         __builtin_amdgcn_wave_barrier();
         for (int p = wave_lane; p < how.r; p += 64) {
-            const double turns = position * (how.frequencies[p] * 0.15915494309189533577);
+            const double f = how.frequencies[p], g = f * kTurn, g_rest = fma(f, kTurn, -g) + f * kTurnRest;
+            const double product = whole * g, small = fma(whole, g, -product) + fma(whole, g_rest, rest * g);
+            double turns = product - rint(product) + small;
+            turns -= rint(turns);
             float2 v;
-            sincospif(2.f * (float)(turns - rint(turns)), &v.y, &v.x);
+            sincospif(2.f * (float)turns, &v.y, &v.x);
             v.x *= how.magnitude;
             v.y *= how.magnitude * how.sign;
             shared[p] = v;

@@ -328,3 +328,31 @@ def test_frequencies():
     assert math.isclose(m, 0.1 * math.log(4.0) + 1)
     assert torch.allclose(ratio[turns >= 32], torch.ones(1, dtype=torch.float64)) and torch.allclose(ratio[turns <= 1], torch.full((1,), 0.25, dtype=torch.float64))
     assert bool(((ratio > 0.25) & (ratio < 1)).any())
+
+
+def test_positions_far_from_zero():
+    """Sine and cosine of position * frequency, with the angle in decimals: positions of up to 63 bits, both ends among them.  Within 2^-22, and
+    half a step of fp32."""
+    import decimal
+    decimal.getcontext().prec = 70
+    pi = decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899")
+    gen = torch.Generator().manual_seed(0)
+    positions = [0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 53 + 1, 2 ** 63 - 1, -2 ** 63, 2 ** 62 + 12345678901]
+    for bits in range(8, 64):
+        p = int(torch.randint(2 ** 62, (1,), generator=gen)) >> (63 - bits) << 1 | 1
+        positions += [p, -p - 2]
+    f = [1.0, 0.7, float(B.rotary_frequencies(128, device="cpu")[0][1]), 3.0, 2.0 ** -20, 1e-9]
+    # (the unrounded product, in turns; a double of what is left of it is enough)
+    turns = [[decimal.Decimal(p) * decimal.Decimal(x) / (2 * pi) for x in f] for p in positions]
+    angle = torch.tensor([[float((t - t.to_integral_value()) * 2 * pi) for t in row] for row in turns], dtype=torch.float64)
+    frequencies = torch.tensor(f, dtype=torch.float64, device="cuda")
+    for wide in (True, False):
+        kept = [i for i, p in enumerate(positions) if wide or -2 ** 31 <= p < 2 ** 31]
+        at = torch.tensor([positions[i] for i in kept], dtype=torch.int64 if wide else torch.int32, device="cuda")
+        x = torch.zeros(len(kept), 1, 12, device="cuda")
+        x[..., :6] = 1.0
+        out = torch.empty_like(x)
+        B.sparseloco_rotary(x, None, at, frequencies, out, None)
+        for got, want in ((out[:, 0, :6], angle[kept].cos()), (out[:, 0, 6:], angle[kept].sin())):
+            off = (got.double().cpu() - want).abs()
+            assert float(off.max()) <= 2.0 ** -22 + 2.0 ** -24, (positions[kept[int(off.max(1).values.argmax())]], float(off.max()))
