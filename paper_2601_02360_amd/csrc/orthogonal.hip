@@ -961,7 +961,7 @@ void add_batches(std::vector<Matrix>& all, bool split, int squares, Shapes& s) {
     for (const Matrix& m : all) total += size(m);
     const int64_t each = total / std::max<int64_t>(1, (total + kBatchElements - 1) / kBatchElements);
     for (const Matrix& m : all) {
-        if (&m == all.data() || s.batches.back().count == kMostMatrices || at >= each) {
+        if (&m == all.data() || s.batches.back().count == kMostMatrices || at >= each || at + size(m) > kBatchElements) {
             s.batches.push_back(Batch{0, 0, {}});
             at = 0;
         }

@@ -86,3 +86,15 @@ def test_how_products_are_cut_up():
                                      (1, (ctypes.c_int64 * 1)(0), sides, x3), (1, sides, (ctypes.c_int64 * 1)(2 ** 22 + 1), x3)):
         assert L.sparseloco_orthogonalize_choice(n, rows, columns, matmul, None) == B.SPLC_EINVAL
     assert L.sparseloco_orthogonalize_choice(2, sides, sides, x3, None) == choice([(4, 4), (4, 4)])[1]
+
+
+@pytest.mark.parametrize("matmul", [B.SPLC_MATMUL_FP16X3, B.SPLC_MATMUL_FP16])
+@pytest.mark.parametrize("shapes", [[(22000, 22000)] * 4, [(22000, 22000)] * 9, [(40000, 8000)] * 7 + [(20000, 20000)] * 3 + [(60000, 512)] * 40,
+                                    [(30000, 30000)] * 2 + [(9000, 9000)] * 20, [(50000, 50000), (3, 3)], [(4096, 16384)] * 200], ids=str)
+def test_batches_keep_their_bound(matmul, shapes):
+    """16 GiB of operands at once, or one matrix."""
+    choice, size = B.orthogonalize_choice(shapes, matmul=matmul)
+    small = 8 * (len(shapes) + sum(-(-r * c // 4096) for r, c in shapes)) + 128
+    operands = lambda shape: B.orthogonalize_choice([shape], matmul=matmul)[1]
+    assert size <= max([2 ** 34] + [operands(s) for s in shapes]) + small
+    assert sorted({c[1] for c in choice}) == list(range(1 + max(c[1] for c in choice)))
