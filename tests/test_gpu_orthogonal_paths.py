@@ -147,3 +147,21 @@ def test_polynomials_that_shrink(mode, polynomial, rows, columns):
     if B.orthogonalize_choice([(rows, columns)], matmul=matmul)[0][0][0]:
         limit = max(limit, in_squares(x[0], u, c))
     agree(out, x[0], u, limit=limit, coefficients=c)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("share", [1e-4, 1e-5, 1e-7])
+def test_matrices_that_are_small_beside_eps(mode, share):
+    """X = M / (|M| + eps) with |M| a small share of eps: an element is held to 22 bits, but not below 2^-39 of the singular values' bound
+    (half of fp16's smallest number, 2^-25, over the scale of 2^14; 2^-38 once they are between 1 and 2), and five usual steps make 3.4445
+    times as much of that each, 2^-38 * 3.4445^5 * (1 + 1 / 3.4445 + ...) = 2^-38 * 690 an element at the most."""
+    matmul, u = MODES[mode]
+    x = matrix(150, 260, "noise", 600)
+    eps = 2.0 ** -20
+    x *= share * eps / float(x.double().norm())
+    plan, out = B.Plan([x.shape], 32), torch.empty_like(x)
+    B.sparseloco_orthogonalize(plan, [x], [out], B.orthogonalize_workspace(plan, matmul=matmul), matmul=matmul, eps=eps)
+    want = plain(x, eps=eps)
+    # the steps' terms beyond the first are share^2 (their operands' rounding counts as that part of u)
+    off = (out.double() - want).abs()
+    assert float(off.max()) <= 690 * 2.0 ** -38 + (2.0 ** -22 + 8 * u * share ** 2 * 3.4445 ** 10) * float(want.abs().max())
