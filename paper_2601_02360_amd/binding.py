@@ -1205,7 +1205,7 @@ def sparseloco_qk_norm_rotary_grad(grad_q_out: torch.Tensor, grad_k_out: Optiona
                                    ws: torch.Tensor, *, eps: float = 1e-6, interleaved: bool = False, magnitude: float = 1.0,
                                    accumulate: bool = False, stream=None) -> None:
     """The gradient of sparseloco_qk_norm_rotary from that of its outputs and from its inputs: grad_q, grad_k like q, k (they may be
-    grad_q_out, grad_k_out), grad_q_gain, grad_k_gain: [head_dim] fp32, added to what is there with accumulate.  ws:
+    grad_q_out, grad_k_out), grad_q_gain, grad_k_gain: [head_dim] fp32, a buffer each, added to what is there with accumulate.  ws:
     qk_norm_rotary_workspace(tokens or more, ...)."""
     if _done(_native().qk_norm_rotary_grad(grad_q_out, grad_k_out, q, k, q_gain, k_gain, positions, frequencies, grad_q, grad_k,
                                            grad_q_gain, grad_k_gain, ws, eps, 1 if interleaved else 0, magnitude, 1 if accumulate else 0,

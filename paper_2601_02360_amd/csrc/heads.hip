@@ -15,6 +15,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "plan.h"
 #include "sparseloco.h"
@@ -624,6 +625,8 @@ int sparseloco_qk_norm_rotary_grad(const sparseloco_heads* grad_q_out, const spa
     if (!grad_q_gain || (k != nullptr) != (grad_k_gain != nullptr) || !ws) return SPLC_EINVAL;
     if (ws_bytes < sparseloco_qk_norm_rotary_grad_ws_bytes(tokens, q_heads, k_heads, head_dim)) return SPLC_EINVAL;
     if (!aligned(grad_q_gain, 4) || !aligned(grad_k_gain, 4) || !aligned(ws, 4)) return SPLC_EALIGN;
+    // (two workgroups at once add to them)
+    if (k && std::abs(reinterpret_cast<intptr_t>(grad_q_gain) - reinterpret_cast<intptr_t>(grad_k_gain)) < 4 * (intptr_t)head_dim) return SPLC_EINVAL;
     int groups[2] = {0, 0};
     if (tokens > 0 && q_heads + k_heads > 0) {
         const bool side = how->interleaved != 0;

@@ -108,3 +108,15 @@ def test_native_calls_hand_back_what_is_not_plainly_right():
     for name in ("rotary", "qk_norm_rotary", "qk_norm_rotary_grad"):
         for args in ((), (None,), (x,) * 5, (x,) * 17, (None,) * 30, ("0",) * 12):
             assert getattr(native, name)(*args) is None
+
+
+def test_gains_gradients_in_one_place():
+    """Sums of queries and of keys are finished side by side: in one buffer one would be lost, or read too early to be added to."""
+    lists = [heads(ANY * i) for i in range(1, 7)]
+
+    def call(q_sum, k_sum, tokens=5):
+        return B.lib().sparseloco_qk_norm_rotary_grad(*lists[:4], 0, tokens, 16, ANY, ANY, 0, 1e-6, how(), *lists[4:], q_sum, k_sum, 1, 64 * ANY, 1 << 30,
+                                                      None)
+    for tokens in (5, 0):
+        for apart in (-60, -4, 0, 4, 60):
+            assert call(32 * ANY, 32 * ANY + apart, tokens) == B.SPLC_EINVAL, apart
