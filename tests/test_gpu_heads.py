@@ -356,3 +356,27 @@ def test_positions_far_from_zero():
         for got, want in ((out[:, 0, :6], angle[kept].cos()), (out[:, 0, 6:], angle[kept].sin())):
             off = (got.double().cpu() - want).abs()
             assert float(off.max()) <= 2.0 ** -22 + 2.0 ** -24, (positions[kept[int(off.max(1).values.argmax())]], float(off.max()))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("side", [False, True])
+@pytest.mark.parametrize("d,r", [(128, 16), (96, 17), (64, 30), (12, 1)])
+def test_channels_behind_the_pairs_are_copied(dtype, side, d, r):
+    """Whatever they hold: infinities, NaN and zeros of either sign beside them change none."""
+    tokens, positions = 7, torch.tensor([0, 1, 5, 1000, 0, 77, -3], device="cuda")
+    q, _ = lists(tokens, 3, 1, d, dtype, 31, False)
+    odd = torch.tensor([float("inf"), float("-inf"), float("nan"), 0.0, -0.0], device="cuda", dtype=dtype)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    tail = q[..., 2 * r:]
+    put = torch.rand(tail.shape, generator=gen, device="cuda") < 0.2
+    tail[put] = odd[torch.randint(0, 5, (int(put.sum()),), generator=gen, device="cuda")]
+    f, _ = B.rotary_frequencies(2 * r)
+    for inverse in (False, True):
+        out = torch.empty_like(q)
+        B.sparseloco_rotary(q, None, positions, f, out, None, interleaved=side, magnitude=1.5, inverse=inverse)
+        got = out[..., 2 * r:]
+        nan = torch.isnan(tail)
+        bits = torch.int32 if dtype == torch.float32 else torch.int16
+        assert torch.equal(torch.isnan(got), nan)
+        assert torch.equal(got.contiguous().view(bits)[~nan], tail.contiguous().view(bits)[~nan])
+        assert bool(torch.isfinite(out[..., :2 * r]).all())
