@@ -529,8 +529,8 @@ int sparseloco_embedding_grad(const void* grad_out, int grad_dtype, const int32_
  *     x -> gain x / sqrt(mean(x^2) + eps),      q_gain, k_gain: [head_dim] of gain_dtype
  * sparseloco_qk_norm_rotary_grad is its gradient, from that of its outputs, with respect to q, k and both gains (fp32, sums over
  * tokens and heads, added to what is there with accumulate; a buffer each, also where one gain serves both).  ws:
- * .._ws_bytes(tokens, ..) bytes, 4-byte aligned, need not be cleared; a workspace for more tokens serves fewer.  The same call gives the
- * same bits.
+ * .._ws_bytes(tokens, ..) bytes, 4-byte aligned, need not be cleared; a workspace for more tokens serves fewer, two calls at once need
+ * one each.  The same call gives the same bits.
  * Everything is computed in fp32 (squares must not overflow there) and rounded once to dtype (SPLC_F32 or SPLC_BF16, that of all
  * lists).  What is written may be an input of its own side, element for element at the same strides (q_out: q; grad_q: q or
  * grad_q_out; keys likewise), and must overlap nothing otherwise; its own heads must not overlap one another.  A head of zeros has the norm's factor

@@ -279,7 +279,8 @@ struct Forward {
 
 // Loads of so many runs of heads are under way at once, the first of them while the angles are formed.  More cost registers, and with
 // them waves.  16384 x 32 heads of 128 bf16 channels: norm 55 us (4: 72, of one wave less a SIMD), gradient, when both
-// sides were one workgroup's, 96 (2: 109), now 85.
+// sides were one workgroup's, 96 (2: 109), now 85.  (Of the variants that keep to these bounds, two put registers aside in memory, both for
+// eight pairs a lane, half a head apart: the norm one, the gradient three.)
 constexpr int kRunsAhead = 3, kWavesASimd = 5;
 constexpr int grad_runs_ahead(int v) { return v == 8 ? 1 : 2; }
 constexpr int grad_waves_a_simd(int v) { return v == 8 ? 4 : 3; }
@@ -646,8 +647,8 @@ int sparseloco_qk_norm_rotary_grad(const sparseloco_heads* grad_q_out, const spa
         const int v = run_of_pairs(dtype, head_dim, how->pairs, side);
         const Shares s = shares(tokens, head_dim, v, q_heads, k_heads);
         // With eight pairs a lane as many workgroups as run at once, 1024, shared out by the heads of either side: 16384 tokens x 32
-        // heads of 128 bf16 channels 85 us, with 1024 for either side 91.  Narrower lanes gain from more of them: 16384 x 24 heads
-        // of 80 fp32 channels 61 us so, 53 with 1024 for either side.
+        // heads of 128 bf16 channels 85 us, with 1024 for either side 91.  Lanes of fewer pairs, all of fp32 among them, gain from
+        // more: 16384 x 24 heads of 80 fp32 channels 61 us so, 53 with 1024 for either side.
         const int at_once = 64 / s.per_head;
         int parts[2] = {1, 1};
         for (int keys = 0; keys < 2; ++keys) {
