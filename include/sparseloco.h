@@ -446,7 +446,9 @@ int sparseloco_adamw_step_8bit(const sparseloco_plan* plan, const sparseloco_ten
  *   starts as [0, 1] below 1024.
  *   matmul: SPLC_MATMUL_FP16    operands of 11 bits, for results that are held in bf16: 2e-4 to 3e-3 off in the 2-norm; below 16 rows
  *                               or columns up to 1.3e-2, since a few singular values may all lie where the polynomials are steep
- *           SPLC_MATMUL_FP16X3  operands of 22 bits in three products, as exact as fp32 ones
+ *           SPLC_MATMUL_FP16X3  operands of 22 bits in three products, as exact as fp32 ones; where matrices that are half as wide again as
+ *                               they are high (or the other way round) take several steps at once, up to twice fp32's error with the
+ *                               usual coefficients, and 6 times with larger ones
  *           Of either mode: no element of X is held finer than 2^-39 of its singular values' bound (1 at first).  That counts where |M| is
  *           small beside eps: with |M| = 1e-5 eps, elements of a result of the usual steps are off by up to 3e-9.
  *   accumulation in fp32, norms in fp64.  ws: sparseloco_orthogonalize_ws_bytes(plan, rows, matmul) bytes, 128-byte aligned, need not

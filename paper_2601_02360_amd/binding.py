@@ -1013,7 +1013,7 @@ def sparseloco_orthogonalize(plan: Plan, x, out, ws: torch.Tensor, *, coefficien
     """out = X after X = x / (|x| + eps) and, for every (a, b, c) of coefficients, X <- a X + (b A + c A^2) X, A = X X^T on the shorter
     side: every matrix of the plan near to the orthogonal factor of its polar decomposition.  The plan's tensors are matrices as
     given to Plan (leading dimensions folded into rows).  x, out: bindings or lists, fp32 or bf16; out may be x.  matmul:
-    SPLC_MATMUL_FP16X3 (as exact as fp32 products) or SPLC_MATMUL_FP16 (for results held in bf16; not for matrices of a few rows).
+    SPLC_MATMUL_FP16X3 (about as exact as fp32 products) or SPLC_MATMUL_FP16 (for results held in bf16; not for matrices of a few rows).
     ws: orthogonalize_workspace()."""
     where = "sparseloco_orthogonalize"
     steps, numbers = _coefficients(coefficients, where)

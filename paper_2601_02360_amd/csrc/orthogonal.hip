@@ -14,7 +14,8 @@
 //           added.  Result: 2e-4 to 3e-3 off (relative, depending on how the singular values are spread; 400 each of normal numbers:
 //           64 x 200 2.3e-3 at most, 16 x 56 3.0e-3, 2 x 14 1.2e-2), as little as a result in bf16 is rounded by; bf16 operands are
 //           1e-2 to 4e-2 off.
-//   FP16X3  operands are hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: what fp32 products give, 2e-6 to 4e-6 off.
+//   FP16X3  operands are hi + lo, 22 bits, and a product is hi hi + hi lo + lo hi: what fp32 products give, 2e-6 to 4e-6 off, or, where
+//           several steps are taken at once, 2e-6 to 7e-6.
 //
 // What bounds it (MI355X; fp16 products of 8192 x 8192 by the vendor's library: 1240 TFLOP/s, for which the chip lowers its clock to
 // 2 GHz and below): the matrix cores.  FP16X3, 32 of 2048 x 2048, three products counted: X <- a X + B X 1490 us or 1107 TFLOP/s, of which
@@ -820,7 +821,8 @@ struct Steps {
 //     A = X X^T;   for each:  B = b A + c A^2,  Q <- p Q,  A <- p (p A);   X <- Q X,
 // where only the first A and the last product have X's long side.  Q is held without its multiple of 1, alpha, as B is: both are zero
 // where X is small.  alpha is what roundings of Q and of A grow by before they come to X: at most 64, of at most three steps
-// (40 for the usual polynomial; five steps without a new A from X: 60 times the error).
+// (40 for the usual polynomial; five steps without a new A from X: 60 times the error).  900 x 1801, beside fp32 products: usual, normal
+// numbers 2.4e-6 and 2.4e-6 off, with four strong directions 6.6e-6 and 3.5e-6; three polynomials of alpha 63 5.6e-6 and 1.2e-6.
 constexpr double kMostAlpha = 64.0;
 constexpr int kMostAtOnce = 3, kSquares = 2, kSquaresAtOnce = 5;
 
