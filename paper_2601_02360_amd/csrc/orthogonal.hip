@@ -22,8 +22,8 @@
 // the tiles' ends, 12 bytes read and written an element, take a third, and symmetric products 830 us, 1120 of the tiles that are formed;
 // FP16, whose ends are 10 bytes beside a third of the products, 710 us or 775 TFLOP/s, and 340 us or 910.  Ends and products most likely
 // share the chip's power: workgroups that start apart, loads before stores and fewer instructions in the ends bring 1 % or nothing,
-// while the same launch over other numbers takes 12 % less.  Whole calls: 0.9B model, one step, FP16X3, 71.5 ms (74 on another card); 8 of 2048 x 5632, FP16,
-// 4.5 ms; one of 512 x 512, FP16X3, 107 us, most of it 18 launches of 6 us.
+// while the same launch over other numbers takes 12 % less.  Whole calls: 0.9B model, one step, FP16X3, 71.5 ms (74 on another card); 8
+// of 2048 x 5632, FP16, 4.5 ms; one of 512 x 512, FP16X3, 107 us, most of it 18 launches of 6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
